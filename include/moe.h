@@ -34,7 +34,11 @@
 extern "C" {
 #endif
 
-typedef enum { MOE_F32 = 0, MOE_BF16 = 1 } moe_dtype_t;
+typedef enum {
+    MOE_F32 = 0,
+    MOE_BF16 = 1,
+    MOE_MXFP4 = 2 /* of a packed weight handle only: moe_weights_pack_mxfp4 */
+} moe_dtype_t;
 
 typedef enum {
     MOE_OK = 0,
@@ -102,6 +106,38 @@ int moe_permute(const int32_t* idx, int T, int E, int k, const void* x, int d,
  */
 int moe_weights_pack(const void* w1, const void* w3, const void* w2, int E, int d, int f,
                      moe_dtype_t w_dtype, moe_weights_t** out, void* stream);
+
+/*
+ * Expert matrices in 4 bits: OCP Microscaling MXFP4.  An element is four bits (sign, two exponent
+ * bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), and 32 consecutive
+ * elements along the reduction share one scale 2^(s-127), s one byte: 17/32 byte per weight.  A
+ * stack of matrices W [E,K,C] (y = x.W) is held feature by feature,
+ *   codes  [E,C,K/2]   element 2i in the low half of byte i of the feature's run
+ *   scales [E,C,K/32]
+ * moe_mxfp4_quantize: per block of 32 the scale's exponent is that of the largest magnitude less
+ *   2, at least -126 (a block of zeros: that); elements are rounded to nearest, ties to the even
+ *   code, and saturate at 6.  Finite elements (others: unspecified values).
+ * moe_mxfp4_dequantize: the values the codes stand for.  Exact in bf16 and fp32 for scale bytes
+ *   1 .. 252, which is what moe_mxfp4_quantize writes; others are for the caller to avoid here
+ *   and in every call on a handle packed from them (unspecified values).
+ *   w [E,K,C] fp32 or bf16; 1 <= E <= 64, K a multiple of 32 and C any number, up to 2^20;
+ *   no output may overlap an input.
+ * moe_weights_pack_mxfp4: moe_weights_pack for converted matrices (w1, w3: K = d, C = f; w2:
+ *   K = f, C = d; d and f multiples of 64), one device copy in the order the kernels read.
+ * The handle serves moe_expert_ffn, moe_expert_ffn_path (AUTO, STREAM up to 72 rows, GROUPED),
+ * _tokens, _noalloc, _parts (one slab), moe_layer, moe_decode_layer (E up to 64 there, two
+ * launches), moe_decode_block and moe_layer_mxfp4 below.  The products are formed on the bf16
+ * matrix cores from the exact element values; activations and h are treated as with bf16
+ * weights (see moe_expert_ffn).
+ */
+int moe_mxfp4_quantize(const void* w, moe_dtype_t w_dtype, int E, int K, int C, uint8_t* codes, uint8_t* scales,
+                       void* stream);
+int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int E, int K, int C, void* w, moe_dtype_t w_dtype,
+                         void* stream);
+int moe_weights_pack_mxfp4(const uint8_t* w1_codes, const uint8_t* w1_scales, const uint8_t* w3_codes,
+                           const uint8_t* w3_scales, const uint8_t* w2_codes, const uint8_t* w2_scales, int E, int d, int f,
+                           moe_weights_t** out, void* stream);
+
 int moe_weights_free(moe_weights_t* w);
 /* Device bytes held by a packed handle (0 for NULL). HOST query. */
 size_t moe_weights_bytes(const moe_weights_t* w);
@@ -254,6 +290,24 @@ int moe_combine_parts(const float* yg_parts, int n_parts, const int32_t* inv_per
                       float* yg, void* stream);
 
 /*
+ * The whole layer over MXFP4 experts, from tokens and router logits to tokens: moe_route,
+ * moe_permute without rows, the expert FFN and the gate-weighted sum, y rounded once to its type.
+ * Two launches for T <= 16 tokens with T*k <= 64 slots and d <= 4096: the first routes the tokens
+ * in its prologue, the second's workgroups count their parts and the last one of a feature group
+ * adds them (in a fixed order: the same bits on every run).
+ *   W of moe_weights_pack_mxfp4; x [T,d] of x_dtype; logits [T,E] fp32, E the handle's
+ *   idx, weights, counts, offsets, perm, inv_perm: as moe_route / moe_permute, all written
+ *   workspace >= moe_layer_mxfp4_workspace(T, E, k, d, f) bytes, 256-byte aligned
+ *   y [T,d] of y_dtype out.  No output and no byte of the workspace may overlap x or logits.
+ * T == 0 writes counts and offsets only.
+ */
+int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, const float* logits, int T, int k,
+                    int32_t* idx, float* weights, int32_t* counts, int32_t* offsets, int32_t* perm, int32_t* inv_perm,
+                    void* workspace, size_t workspace_bytes, void* y, moe_dtype_t y_dtype, void* stream);
+/* HOST query; 0 for arguments outside the domain. */
+size_t moe_layer_mxfp4_workspace(int T, int E, int k, int d, int f);
+
+/*
  * One decode step of the layer in three launches (Sec. 3.3 "Execution" for a handful of
  * tokens, where every launch is a few percent of the step): the first-projection kernel runs
  * the gating function and the per-expert batching in its prologue and reads the token rows
@@ -263,7 +317,7 @@ int moe_combine_parts(const float* yg_parts, int n_parts, const int32_t* inv_per
  * launches.
  * Same results as moe_route + moe_permute + moe_expert_ffn + moe_combine: index outputs bit
  * for bit, y and yg in the same fixed summation order.
- *   x [T,d] fp32, logits [T,E] fp32; bf16 weights; 1 <= T <= 16, E <= 16, T*k <= 64 and a
+ *   x [T,d] fp32, logits [T,E] fp32; bf16 or MXFP4 weights; 1 <= T <= 16, E <= 16 (MXFP4: 64), T*k <= 64 and a
  *   shape the STREAM family supports (MOE_ERR_UNSUPPORTED otherwise)
  *   idx, weights, counts, offsets, perm, inv_perm: as moe_route / moe_permute, all written
  *   xg [T*k,d] fp32 out or NULL, yg [T*k,d] fp32 out or NULL: written only when given

@@ -9,7 +9,7 @@ from typing import Optional
 
 import torch
 
-MOE_F32, MOE_BF16 = 0, 1
+MOE_F32, MOE_BF16, MOE_MXFP4 = 0, 1, 2
 MOE_FFN_AUTO, MOE_FFN_STREAM, MOE_FFN_GROUPED, MOE_FFN_MID = 0, 1, 2, 3
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -25,7 +25,8 @@ EXPORTS = ("moe_status_string", "moe_route", "moe_permute", "moe_layer", "moe_we
            "moe_rmsnorm", "moe_router_logits", "moe_residual_add", "moe_route_permute",
            "moe_norm_route_permute", "moe_combine_residual", "moe_combine_norm_route_permute",
            "moe_rmsnorm_router_logits", "moe_gate_sums", "moe_gate_sums_stride",
-           "moe_decode_block_supported")
+           "moe_decode_block_supported", "moe_mxfp4_quantize", "moe_mxfp4_dequantize", "moe_weights_pack_mxfp4",
+           "moe_layer_mxfp4", "moe_layer_mxfp4_workspace")
 PROBE_EXPORTS = ("moe_set_ffn_mid_event", "moe_mfma_rate_probe", "moe_hbm_read_probe")
 ORCH_EXPORTS = ("moe_orch_place", "moe_orch_hit_rate", "moe_orch_decide", "moe_orch_cpu_expert_ffn",
                 "moe_orch_layer_create", "moe_orch_layer_free", "moe_orch_calibrate",
@@ -133,6 +134,16 @@ def lib():
         L.moe_gate_sums.restype = C.c_int
         L.moe_gate_sums_stride.argtypes = [i32, i32]
         L.moe_gate_sums_stride.restype = C.c_size_t
+        L.moe_mxfp4_quantize.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp]
+        L.moe_mxfp4_quantize.restype = C.c_int
+        L.moe_mxfp4_dequantize.argtypes = [vp, vp, i32, i32, i32, vp, i32, vp]
+        L.moe_mxfp4_dequantize.restype = C.c_int
+        L.moe_weights_pack_mxfp4.argtypes = [vp] * 6 + [i32] * 3 + [C.POINTER(vp), vp]
+        L.moe_weights_pack_mxfp4.restype = C.c_int
+        L.moe_layer_mxfp4.argtypes = [vp, vp, i32, vp, i32, i32] + [vp] * 7 + [C.c_size_t, vp, i32, vp]
+        L.moe_layer_mxfp4.restype = C.c_int
+        L.moe_layer_mxfp4_workspace.argtypes = [i32] * 5
+        L.moe_layer_mxfp4_workspace.restype = C.c_size_t
         dp = C.POINTER(C.c_double)
         L.moe_orch_place.argtypes = [vp, i32, i32, i32, vp]
         L.moe_orch_hit_rate.argtypes = [vp, vp, i32, i32]
@@ -273,6 +284,73 @@ def moe_weights_pack(w1: torch.Tensor, w3: torch.Tensor, w2: torch.Tensor,
     _check(lib().moe_weights_pack(_ptr(w1), _ptr(w3), _ptr(w2), E, d, f, dt, C.byref(h),
                                   _stream(stream)), "moe_weights_pack")
     return PackedWeights(h.value, E, d, f, dt)
+
+
+def _mxfp4_shape(codes: torch.Tensor, scales: torch.Tensor, what: str):
+    """(E, K, C) of codes [E,C,K/2] and scales [E,C,K/32]."""
+    _dev(codes, torch.uint8, what + " codes")
+    _dev(scales, torch.uint8, what + " scales")
+    if codes.dim() != 3 or scales.dim() != 3 or codes.shape[:2] != scales.shape[:2] or \
+            codes.shape[2] != 16 * scales.shape[2]:
+        raise ValueError(f"{what}: expected codes [E,C,K/2] and scales [E,C,K/32]")
+    _here(codes, scales)
+    return codes.shape[0], 2 * codes.shape[2], codes.shape[1]
+
+
+def _here(*tensors):
+    """The calls run on the current device's stream: its tensors, or none."""
+    dev = _getDevice() if _getDevice is not None else torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def moe_mxfp4_quantize(w: torch.Tensor, codes=None, scales=None, stream=None):
+    """w [E,K,C] (fp32 or bf16, K a multiple of 32 along the reduction) -> MXFP4 (codes uint8
+    [E,C,K/2], scales uint8 [E,C,K/32])."""
+    dt = _act_dtype(w)
+    _dev(w, w.dtype, "w")
+    if w.dim() != 3:
+        raise ValueError("w: expected [E,K,C]")
+    E, K, c = w.shape
+    u8 = dict(dtype=torch.uint8, device=w.device)
+    if codes is None:
+        codes = torch.empty((E, c, K // 2), **u8)
+    if scales is None:
+        scales = torch.empty((E, c, K // 32), **u8)
+    if K % 32 == 0 and _mxfp4_shape(codes, scales, "out") != (E, K, c):
+        raise ValueError("codes and scales must be [E,C,K/2] and [E,C,K/32] of w [E,K,C]")
+    _here(w)
+    _check(lib().moe_mxfp4_quantize(_ptr(w), dt, E, K, c, _ptr(codes), _ptr(scales), _stream(stream)),
+           "moe_mxfp4_quantize")
+    return codes, scales
+
+
+def moe_mxfp4_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.bfloat16, w=None, stream=None):
+    """codes [E,C,K/2], scales [E,C,K/32] -> the values they stand for, [E,K,C] of `dtype` (fp32
+    or bf16, exact in both)."""
+    E, K, c = _mxfp4_shape(codes, scales, "matrix")
+    if w is None:
+        w = torch.empty((E, K, c), dtype=dtype, device=codes.device)
+    elif tuple(w.shape) != (E, K, c):
+        raise ValueError("w must be [E,K,C]")
+    _dev(w, w.dtype, "w")
+    _here(w)
+    _check(lib().moe_mxfp4_dequantize(_ptr(codes), _ptr(scales), E, K, c, _ptr(w), _act_dtype(w), _stream(stream)),
+           "moe_mxfp4_dequantize")
+    return w
+
+
+def moe_weights_pack_mxfp4(w1, w3, w2, stream=None) -> PackedWeights:
+    """A handle over 4-bit expert matrices: w1, w3 and w2 are pairs (codes, scales) as
+    moe_mxfp4_quantize leaves them for w1, w3 [E,d,f] and w2 [E,f,d]."""
+    E, d, f = _mxfp4_shape(*w1, "w1")
+    if _mxfp4_shape(*w3, "w3") != (E, d, f) or _mxfp4_shape(*w2, "w2") != (E, f, d):
+        raise ValueError("the matrices must be w1,w3 [E,d,f] and w2 [E,f,d]")
+    h = C.c_void_p()
+    _check(lib().moe_weights_pack_mxfp4(_ptr(w1[0]), _ptr(w1[1]), _ptr(w3[0]), _ptr(w3[1]), _ptr(w2[0]), _ptr(w2[1]),
+                                        E, d, f, C.byref(h), _stream(stream)), "moe_weights_pack_mxfp4")
+    return PackedWeights(h.value, E, d, f, MOE_MXFP4)
 
 
 def moe_weights_free(w: PackedWeights):
@@ -631,6 +709,52 @@ def moe_layer(W: PackedWeights, x: torch.Tensor, logits: torch.Tensor, k: int,
                 xg=xg, yg=yg, y=y)
 
 
+def moe_layer_mxfp4_workspace(T: int, E: int, k: int, d: int, f: int) -> int:
+    """Bytes of scratch moe_layer_mxfp4 needs (host query)."""
+    return int(lib().moe_layer_mxfp4_workspace(T, E, k, d, f))
+
+
+def moe_layer_mxfp4(W: PackedWeights, x: torch.Tensor, logits: torch.Tensor, k: int, idx=None, weights=None,
+                    out=None, workspace=None, y=None, stream=None) -> dict:
+    """The whole layer over 4-bit experts: x [T,d] (fp32 or bf16), logits fp32 [T,E] -> y [T,d] of
+    x's type unless a y is given.  Two launches for a few tokens (T <= 16, T*k <= 64).  `out` =
+    (counts, offsets, perm, inv_perm)."""
+    _dev(logits, torch.float32, "logits")
+    xdt = _act_dtype(x)
+    _dev(x, x.dtype, "x")
+    T, E = logits.shape
+    d, N, dev = W.d, T * k, x.device
+    if E != W.E or tuple(x.shape) != (T, d):
+        raise ValueError(f"expected x [T,{d}] and logits [T,{W.E}]")
+    _here(x, logits)
+    if not 1 <= k <= min(E, _MAX_K) or N >= _MAX_N:
+        raise MoeError(_INVALID_ARG, "moe_layer_mxfp4")  # before N rows are allocated
+    i32 = dict(dtype=torch.int32, device=dev)
+    if idx is None:
+        idx = torch.empty((T, k), **i32)
+    if weights is None:
+        weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+    if out is None:
+        out = (torch.empty(E, **i32), torch.empty(E + 1, **i32), torch.empty(N, **i32), torch.empty(N, **i32))
+    counts, offsets, perm, inv_perm = out[:4]
+    if workspace is None:
+        workspace = torch.empty(max(moe_layer_mxfp4_workspace(T, E, k, d, W.f), 256), dtype=torch.uint8, device=dev)
+    if y is None:
+        y = torch.empty((T, d), dtype=x.dtype, device=dev)
+    for t, n, dt, what in ((idx, N, torch.int32, "idx"), (weights, N, torch.float32, "weights"),
+                           (counts, E, torch.int32, "counts"), (offsets, E + 1, torch.int32, "offsets"),
+                           (perm, N, torch.int32, "perm"), (inv_perm, N, torch.int32, "inv_perm"),
+                           (y, T * d, y.dtype, "y")):
+        _dev(t, dt, what)
+        if t.numel() < n:
+            raise ValueError(f"{what}: {t.numel()} elements, {n} are written")
+    _check(lib().moe_layer_mxfp4(W.handle, x.data_ptr(), xdt, logits.data_ptr(), T, k, idx.data_ptr(),
+                                 weights.data_ptr(), counts.data_ptr(), offsets.data_ptr(), perm.data_ptr(),
+                                 inv_perm.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                 y.data_ptr(), _act_dtype(y), _stream(stream)), "moe_layer_mxfp4")
+    return dict(idx=idx, w=weights, counts=counts, offsets=offsets, perm=perm, inv_perm=inv_perm, y=y)
+
+
 def moe_route_permute(logits: torch.Tensor, k: int, x: torch.Tensor, idx, weights, out,
                       stream=None):
     """Fused moe_route + moe_permute for T <= 16 (fp32 x); outputs as in the two calls."""
@@ -688,7 +812,7 @@ class StackBuffers:
     one-launch seam between two blocks reads the previous block's while writing the next
     block's; x_alt is the second residual-stream buffer of that seam."""
 
-    def __init__(self, T: int, E: int, k: int, d: int, f: int, device="cuda"):
+    def __init__(self, T: int, E: int, k: int, d: int, f: int, device="cuda", w_dtype: int = MOE_BF16):
         N = T * k
         i32 = dict(dtype=torch.int32, device=device)
         f32 = dict(dtype=torch.float32, device=device)
@@ -705,7 +829,7 @@ class StackBuffers:
                               dtype=torch.uint8, device=device)
         # the second projection's reduction parts (decode kernels; slab 0 is yg otherwise)
         try:
-            plan = moe_expert_ffn_plan(N, E, d, f, MOE_BF16)
+            plan = moe_expert_ffn_plan(N, E, d, f, MOE_MXFP4 if w_dtype == MOE_MXFP4 else MOE_BF16)
         except MoeError:   # a shape only the fp32 kernels serve
             plan = dict(n_parts=1, path=MOE_FFN_STREAM)
         self.max_parts = max(1, plan["n_parts"])
@@ -737,10 +861,10 @@ def moe_stack_forward(layers, x: torch.Tensor, k: int, eps: float = 1e-5, bufs=N
     T, d = x.shape
     W0 = layers[0][0]
     if bufs is None:
-        bufs = StackBuffers(T, W0.E, k, d, W0.f, x.device)
+        bufs = StackBuffers(T, W0.E, k, d, W0.f, x.device, W0.dtype)
     fused_gate = fused and T <= 4 and W0.E <= 16
     seam = seam and fused_gate
-    if seam and W0.dtype == MOE_BF16 and moe_decode_block_supported(T, W0.E, k, d, W0.f):
+    if seam and W0.dtype != MOE_F32 and moe_decode_block_supported(T, W0.E, k, d, W0.f, W0.dtype):
         # at most four routed rows: two launches per block, nothing between two blocks
         moe_gate_sums(x, layers[0][1], bufs.gate_sums[0], stream=stream)
         n_shares = 1
@@ -786,7 +910,7 @@ def moe_stack_forward(layers, x: torch.Tensor, k: int, eps: float = 1e-5, bufs=N
                 moe_rmsnorm(cur, eps, bufs.h, stream=stream)
                 moe_router_logits(bufs.h, w_gate, bufs.logits, stream=stream)
             moe_route(bufs.logits, k, rs["idx"], rs["w"], stream=stream)
-            if fused and bufs.rows_through_perm and W.dtype == MOE_BF16:
+            if fused and bufs.rows_through_perm and W.dtype != MOE_F32:
                 po = rs["perm_out"][:4] + (None,)
                 _, offsets, perm, inv_perm, xg = moe_permute(rs["idx"], W.E, None, out=po,
                                                              stream=stream)

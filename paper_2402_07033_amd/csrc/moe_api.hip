@@ -1,6 +1,7 @@
 // C ABI of libmoe_hip (include/moe.h): argument validation on the host, then
 // dispatch to the kernel launchers.  Nothing is enqueued when validation fails.
 #include "moe_internal.h"
+#include "moe_mx.h"
 
 // mean rows per expert up to which AUTO names MID: no crossover, but the range in which it serves
 // f = 128
@@ -80,6 +81,10 @@ static int ffn_args(const moe_weights_t* W, const void* xg, moe_dtype_t act_dtyp
     bool served;
     if (W->dtype == MOE_F32) {
         served = act_dtype == MOE_F32 && path == MOE_FFN_AUTO && moe_ffn_f32_supported(N, W->E);
+    } else if (W->dtype == MOE_MXFP4) {
+        if (path == MOE_FFN_AUTO) path = moe_mx_auto_path(N, W->E, W->d, W->f);
+        served = path == MOE_FFN_STREAM ? moe_mx_stream_serves(N, W->E, W->d, W->f)
+                                        : path == MOE_FFN_GROUPED && moe_mx_gemm_supported(N, W->E, W->d, W->f);
     } else {
         if (path == MOE_FFN_AUTO) path = moe_ffn_auto_path(N, W->E, W->d, W->f);
         served = path == MOE_FFN_STREAM ? moe_ffn_stream_serves(N, W->E, W->d, W->f)
@@ -120,6 +125,9 @@ static int ffn_launch(const moe_weights_t* W, const void* xg, moe_dtype_t act_dt
     if (N == 0) return MOE_OK;
     if (W->dtype == MOE_F32)
         return moe_ffn_f32_launch(W, (const float*)xg, perm, k, offsets, N, workspace, yg, s);
+    if (W->dtype == MOE_MXFP4)
+        return path == MOE_FFN_STREAM ? moe_mx_stream_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, nullptr, s)
+                                      : moe_mx_gemm_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, s);
     if (path == MOE_FFN_STREAM)
         return moe_ffn_stream_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, nullptr, s);
     return moe_ffn_grouped_launch(path == MOE_FFN_MID, W, xg, act_dtype, perm, k, offsets, N, workspace, yg, s);
@@ -131,6 +139,24 @@ static int ffn_dispatch(const moe_weights_t* W, const void* xg, moe_dtype_t act_
     const int rc = ffn_args(W, xg, act_dtype, offsets, N, workspace, workspace_bytes, yg, path);
     if (rc != MOE_OK) return rc;
     return ffn_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, path, (hipStream_t)stream);
+}
+
+// A routed step over MXFP4 experts; logits null: routed before.
+static MxStep mx_step(const float* logits, int T, int k, int32_t* idx, float* weights, int32_t* counts, int32_t* offsets,
+                      int32_t* perm, int32_t* inv_perm, void* y, moe_dtype_t y_dtype) {
+    MxStep st = {};
+    st.logits = logits;
+    st.T = T;
+    st.k = k;
+    st.idx = idx;
+    st.weights = weights;
+    st.counts = counts;
+    st.offsets = offsets;
+    st.perm = perm;
+    st.inv_perm = inv_perm;
+    st.y = y;
+    st.y_dtype = y_dtype;
+    return st;
 }
 
 extern "C" {
@@ -174,6 +200,45 @@ int moe_weights_pack(const void* w1, const void* w3, const void* w2, int E, int 
     return moe_weights_pack_impl(w1, w3, w2, E, d, f, w_dtype, out, (hipStream_t)stream);
 }
 
+static bool mxfp4_dims_ok(int E, int K, int C) {
+    return E >= 1 && E <= MOE_MAX_E && K >= MX_BLOCK && K % MX_BLOCK == 0 && K <= (1 << 20) && C >= 1 && C <= (1 << 20);
+}
+
+int moe_mxfp4_quantize(const void* w, moe_dtype_t w_dtype, int E, int K, int C, uint8_t* codes, uint8_t* scales,
+                       void* stream) {
+    if (!mxfp4_dims_ok(E, K, C) || (w_dtype != MOE_F32 && w_dtype != MOE_BF16)) return MOE_ERR_INVALID_ARG;
+    if (!w || !codes || !scales || !moe_aligned16(w) || !moe_aligned16(codes) || !moe_aligned16(scales))
+        return MOE_ERR_INVALID_ARG;
+    const size_t n = (size_t)E * K * C, wb = n * (w_dtype == MOE_BF16 ? 2 : 4);
+    if (ranges_overlap(w, wb, codes, n / 2) || ranges_overlap(w, wb, scales, n / MX_BLOCK) ||
+        ranges_overlap(codes, n / 2, scales, n / MX_BLOCK))
+        return MOE_ERR_INVALID_ARG;
+    return moe_mx_quantize_launch(w, w_dtype, E, K, C, codes, scales, (hipStream_t)stream);
+}
+
+int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int E, int K, int C, void* w, moe_dtype_t w_dtype,
+                         void* stream) {
+    if (!mxfp4_dims_ok(E, K, C) || (w_dtype != MOE_F32 && w_dtype != MOE_BF16)) return MOE_ERR_INVALID_ARG;
+    if (!w || !codes || !scales || !moe_aligned16(w) || !moe_aligned16(codes) || !moe_aligned16(scales))
+        return MOE_ERR_INVALID_ARG;
+    const size_t n = (size_t)E * K * C, wb = n * (w_dtype == MOE_BF16 ? 2 : 4);
+    if (ranges_overlap(w, wb, codes, n / 2) || ranges_overlap(w, wb, scales, n / MX_BLOCK)) return MOE_ERR_INVALID_ARG;
+    return moe_mx_dequantize_launch(codes, scales, E, K, C, w, w_dtype, (hipStream_t)stream);
+}
+
+int moe_weights_pack_mxfp4(const uint8_t* w1_codes, const uint8_t* w1_scales, const uint8_t* w3_codes,
+                           const uint8_t* w3_scales, const uint8_t* w2_codes, const uint8_t* w2_scales, int E, int d, int f,
+                           moe_weights_t** out, void* stream) {
+    if (!out) return MOE_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (E < 1 || E > MOE_MAX_E || !dims_ok(d) || !dims_ok(f)) return MOE_ERR_INVALID_ARG;
+    const uint8_t* codes[3] = {w1_codes, w3_codes, w2_codes};
+    const uint8_t* scales[3] = {w1_scales, w3_scales, w2_scales};
+    for (int i = 0; i < 3; i++)
+        if (!codes[i] || !scales[i] || !moe_aligned16(codes[i]) || !moe_aligned16(scales[i])) return MOE_ERR_INVALID_ARG;
+    return moe_mx_pack_impl(codes, scales, E, d, f, out, (hipStream_t)stream);
+}
+
 int moe_weights_free(moe_weights_t* w) { return moe_weights_free_impl(w); }
 
 size_t moe_weights_bytes(const moe_weights_t* w) { return w ? w->bytes : 0; }
@@ -182,10 +247,11 @@ size_t moe_expert_ffn_workspace(int N, int E, int d, int f, moe_dtype_t act_dtyp
     if (N < 0 || N >= MOE_MAX_N || E < 1 || E > MOE_MAX_E || !dims_ok(d) || !dims_ok(f)) return 0;
     if (act_dtype != MOE_F32 && act_dtype != MOE_BF16) return 0;
     size_t need = moe_ffn_f32_workspace(N, E, d, f);
-    const size_t s = moe_ffn_stream_workspace(N, E, d, f);
-    const size_t g = moe_ffn_grouped_workspace(N, E, d, f);
-    if (s > need) need = s;
-    if (g > need) need = g;
+    const size_t other[4] = {moe_ffn_stream_workspace(N, E, d, f), moe_ffn_grouped_workspace(N, E, d, f),
+                             moe_mx_stream_serves(N, E, d, f) ? moe_mx_stream_workspace(N, E, d, f) : 0,
+                             moe_mx_gemm_workspace(N, E, d, f)};
+    for (size_t o : other)
+        if (o > need) need = o;
     return align256(need) + 256;
 }
 
@@ -231,12 +297,17 @@ int moe_expert_ffn_plan(int N, int E, int d, int f, moe_dtype_t w_dtype, int pat
                         moe_ffn_plan_t* plan) {
     if (!plan || N < 0 || N >= MOE_MAX_N || E < 1 || E > MOE_MAX_E || !dims_ok(d) || !dims_ok(f))
         return MOE_ERR_INVALID_ARG;
-    if (w_dtype != MOE_F32 && w_dtype != MOE_BF16) return MOE_ERR_INVALID_ARG;
+    if (w_dtype != MOE_F32 && w_dtype != MOE_BF16 && w_dtype != MOE_MXFP4) return MOE_ERR_INVALID_ARG;
     if (path != MOE_FFN_AUTO && path != MOE_FFN_STREAM && path != MOE_FFN_GROUPED &&
         path != MOE_FFN_MID)
         return MOE_ERR_INVALID_ARG;
     *plan = moe_ffn_plan_t{};
     plan->n_parts = 1;
+    if (w_dtype == MOE_MXFP4) {  // the parts of the second projection are added before the call ends
+        plan->path = path == MOE_FFN_AUTO ? moe_mx_auto_path(N, E, d, f) : path;
+        if (plan->path == MOE_FFN_STREAM) return moe_mx_stream_serves(N, E, d, f) ? MOE_OK : MOE_ERR_UNSUPPORTED;
+        return plan->path == MOE_FFN_GROUPED ? moe_mx_gemm_plan(N, E, d, f, plan) : MOE_ERR_UNSUPPORTED;
+    }
     if (w_dtype == MOE_F32) {
         if (path != MOE_FFN_AUTO) return MOE_ERR_UNSUPPORTED;
         plan->path = MOE_FFN_AUTO;  // the all-fp32 kernels are no family of their own
@@ -303,7 +374,9 @@ int moe_decode_layer(const moe_weights_t* W, const float* x, const float* logits
     if (!moe_aligned16(x) || !moe_aligned16(y) || !moe_aligned16(logits) || !moe_aligned16(idx) ||
         !moe_aligned16(weights) || (xg && !moe_aligned16(xg)) || (yg && !moe_aligned16(yg)))
         return MOE_ERR_INVALID_ARG;
-    if (W->dtype != MOE_BF16 || !moe_ffn_stream_decode_supported(T, W->E, k, W->d, W->f))
+    const bool mx = W->dtype == MOE_MXFP4;
+    if (mx ? !moe_mx_stream_routes(T, W->E, k, W->d, W->f)
+           : W->dtype != MOE_BF16 || !moe_ffn_stream_decode_supported(T, W->E, k, W->d, W->f))
         return MOE_ERR_UNSUPPORTED;
     const int N = T * k;
     if (!workspace || (((uintptr_t)workspace) & 255u)) return MOE_ERR_WORKSPACE;
@@ -314,6 +387,12 @@ int moe_decode_layer(const moe_weights_t* W, const float* x, const float* logits
     if (ranges_overlap(x, xb, xg, nb) || ranges_overlap(x, xb, y, xb) ||
         ranges_overlap(logits, (size_t)T * W->E * 4, weights, (size_t)N * 4))
         return MOE_ERR_INVALID_ARG;
+    if (mx) {
+        MxStep st = mx_step(logits, T, k, idx, weights, counts, offsets, perm, inv_perm, y, MOE_F32);
+        st.xg = xg;
+        st.yg = yg;
+        return moe_mx_stream_launch(W, x, MOE_F32, nullptr, k, nullptr, N, workspace, nullptr, &st, (hipStream_t)stream);
+    }
     const float* parts = nullptr;
     int n_parts = 1;
     size_t stride = 0;
@@ -340,7 +419,9 @@ int moe_decode_block(const moe_weights_t* W, const float* x_in, const float* gat
     if (!moe_aligned16(x_in) || !moe_aligned16(x_out) || !moe_aligned16(logits) ||
         !moe_aligned16(idx) || !moe_aligned16(weights))
         return MOE_ERR_INVALID_ARG;
-    if (W->dtype != MOE_BF16 || !moe_ffn_stream_block_supported(T, W->E, k, W->d, W->f))
+    const bool mx = W->dtype == MOE_MXFP4;
+    if (mx ? !moe_mx_block_supported(T, W->E, k, W->d, W->f)
+           : W->dtype != MOE_BF16 || !moe_ffn_stream_block_supported(T, W->E, k, W->d, W->f))
         return MOE_ERR_UNSUPPORTED;
     if (gate_sums && n_shares > W->d / 16 && n_shares > 1) return MOE_ERR_INVALID_ARG;
     const int N = T * k;
@@ -357,6 +438,20 @@ int moe_decode_block(const moe_weights_t* W, const float* x_in, const float* gat
         ranges_overlap(x_out, xb, gate_sums_next, sb_out) || ranges_overlap(x_out, xb, gate_sums, sb_in) ||
         ranges_overlap(logits, lb, gate_sums_next, sb_out) || ranges_overlap(logits, lb, gate_sums, sb_in))
         return MOE_ERR_INVALID_ARG;
+    if (mx) {
+        MxStep st = mx_step(gate_sums ? nullptr : logits, T, k, idx, weights, counts, offsets, perm, inv_perm, x_out, MOE_F32);
+        st.gate_stride = moe_ffn_stream_gate_stride(T, W->E);
+        if (gate_sums) {
+            st.gate_sums = gate_sums;
+            st.n_shares = n_shares;
+            st.eps = eps;
+            st.logits_out = logits;
+        }
+        st.x_in = x_in;
+        st.w_gate_next = w_gate_next;
+        st.sums_next = gate_sums_next;
+        return moe_mx_stream_launch(W, x_in, MOE_F32, nullptr, k, nullptr, N, workspace, nullptr, &st, (hipStream_t)stream);
+    }
     return moe_ffn_stream_block_launch(W, x_in, gate_sums, n_shares, eps, logits, T, k, idx, weights,
                                        counts, offsets, perm, inv_perm, workspace, x_out, w_gate_next,
                                        gate_sums_next, (hipStream_t)stream);
@@ -408,6 +503,63 @@ int moe_layer(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, int d,
     return T == 0 ? MOE_OK : moe_combine_launch(yg, inv_perm, weights, T, k, W->d, y, s);
 }
 
+// what moe_layer_mxfp4 keeps besides the expert FFN's scratch: the experts' rows, where the GEMM leaves them
+static size_t mx_layer_rows(int N, int d) { return align256((size_t)N * d * sizeof(float)); }
+
+size_t moe_layer_mxfp4_workspace(int T, int E, int k, int d, int f) {
+    if (!tek_ok(T, E, k) || !dims_ok(d) || !dims_ok(f)) return 0;
+    const int N = T * k;
+    const bool stream = moe_mx_auto_path(N, E, d, f) == MOE_FFN_STREAM;
+    return align256(stream ? moe_mx_stream_workspace(N, E, d, f) : mx_layer_rows(N, d) + moe_mx_gemm_workspace(N, E, d, f)) +
+           256;
+}
+
+int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, const float* logits, int T, int k,
+                    int32_t* idx, float* weights, int32_t* counts, int32_t* offsets, int32_t* perm, int32_t* inv_perm,
+                    void* workspace, size_t workspace_bytes, void* y, moe_dtype_t y_dtype, void* stream) {
+    if (!W || W->dtype != MOE_MXFP4) return MOE_ERR_INVALID_ARG;
+    const int E = W->E, d = W->d, f = W->f;
+    if (!tek_ok(T, E, k) || !counts || !offsets) return MOE_ERR_INVALID_ARG;
+    if ((x_dtype != MOE_F32 && x_dtype != MOE_BF16) || (y_dtype != MOE_F32 && y_dtype != MOE_BF16))
+        return MOE_ERR_INVALID_ARG;
+    const int N = T * k;
+    hipStream_t s = (hipStream_t)stream;
+    if (T == 0)
+        return moe_permute_launch(idx, 0, E, k, nullptr, d, x_dtype, counts, offsets, perm, inv_perm, nullptr, s);
+    if (!x || !logits || !idx || !weights || !perm || !inv_perm || !y) return MOE_ERR_INVALID_ARG;
+    if (!moe_aligned16(x) || !moe_aligned16(y) || !moe_aligned16(logits) || !moe_aligned16(idx) ||
+        !moe_aligned16(weights) || !moe_aligned16(perm) || !moe_aligned16(inv_perm))
+        return MOE_ERR_INVALID_ARG;
+    const int path = moe_mx_auto_path(N, E, d, f);
+    if (path == MOE_FFN_GROUPED && !moe_mx_gemm_supported(N, E, d, f)) return MOE_ERR_UNSUPPORTED;
+    if (!workspace || (((uintptr_t)workspace) & 255u)) return MOE_ERR_WORKSPACE;
+    if (workspace_bytes < moe_layer_mxfp4_workspace(T, E, k, d, f)) return MOE_ERR_WORKSPACE;
+    // every workgroup of the first launch may read x and logits while one writes the outputs
+    const size_t td = (size_t)T * d, n4 = (size_t)N * 4, e4 = (size_t)E * 4;
+    const struct { const void* p; size_t bytes; } out[8] = {
+        {idx, n4}, {weights, n4}, {counts, e4}, {offsets, e4 + 4}, {perm, n4}, {inv_perm, n4},
+        {y, td * (y_dtype == MOE_BF16 ? 2 : 4)}, {workspace, workspace_bytes}};
+    for (const auto& o : out)
+        if (ranges_overlap(logits, (size_t)T * E * 4, o.p, o.bytes) ||
+            ranges_overlap(x, td * (x_dtype == MOE_BF16 ? 2 : 4), o.p, o.bytes))
+            return MOE_ERR_INVALID_ARG;
+
+    MxStep st = mx_step(logits, T, k, idx, weights, counts, offsets, perm, inv_perm, y, y_dtype);
+    if (moe_mx_stream_routes(T, E, k, d, f))
+        return moe_mx_stream_launch(W, x, x_dtype, nullptr, k, nullptr, N, workspace, nullptr, &st, s);
+    int rc = moe_route_launch(logits, T, E, k, idx, weights, s);
+    if (rc == MOE_OK)
+        rc = moe_permute_launch(idx, T, E, k, nullptr, 0, x_dtype, counts, offsets, perm, inv_perm, nullptr, s);
+    if (rc != MOE_OK) return rc;
+    if (path == MOE_FFN_STREAM) {
+        st.logits = nullptr;
+        return moe_mx_stream_launch(W, x, x_dtype, perm, k, offsets, N, workspace, nullptr, &st, s);
+    }
+    float* yg = (float*)workspace;
+    rc = moe_mx_gemm_launch(W, x, x_dtype, perm, k, offsets, N, (char*)workspace + mx_layer_rows(N, d), yg, s);
+    return rc != MOE_OK ? rc : moe_mx_combine_launch(yg, inv_perm, weights, T, k, d, y, y_dtype, s);
+}
+
 int moe_rmsnorm(const float* x, int T, int d, float eps, float* h, void* stream) {
     if (T < 0 || !dims_ok(d) || !(eps >= 0.f)) return MOE_ERR_INVALID_ARG;
     if (T == 0) return MOE_OK;
@@ -454,6 +606,7 @@ size_t moe_gate_sums_stride(int T, int E) {
 
 int moe_decode_block_supported(int T, int E, int k, int d, int f, moe_dtype_t w_dtype) {
     if (!tek_ok(T, E, k) || T < 1 || !dims_ok(d) || !dims_ok(f)) return 0;
+    if (w_dtype == MOE_MXFP4) return moe_mx_block_supported(T, E, k, d, f) ? 1 : 0;
     return (w_dtype == MOE_BF16 && moe_ffn_stream_block_supported(T, E, k, d, f)) ? 1 : 0;
 }
 

@@ -35,6 +35,9 @@ struct moe_weights {
     float* w3f;
     float* w2f;
     size_t bytes;
+    // MXFP4: w13 and w2 hold code fragments, these their scales (moe_mx.h)
+    void* s13;
+    void* s2;
 };
 
 static inline bool moe_aligned16(const void* p) { return (((uintptr_t)p) & 15u) == 0; }

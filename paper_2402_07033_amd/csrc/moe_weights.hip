@@ -148,8 +148,8 @@ int moe_weights_free_impl(moe_weights* W) {
     const bool have_cur = hipGetDevice(&cur) == hipSuccess;
     if (have_cur && cur != W->device && hipSetDevice(W->device) != hipSuccess) rc = MOE_ERR_HIP;
     if (hipDeviceSynchronize() != hipSuccess) rc = MOE_ERR_HIP;
-    void* p[5] = {W->w13, W->w2, W->w1f, W->w3f, W->w2f};
-    for (int i = 0; i < 5; i++)
+    void* p[7] = {W->w13, W->w2, W->w1f, W->w3f, W->w2f, W->s13, W->s2};
+    for (int i = 0; i < 7; i++)
         if (p[i] && hipFree(p[i]) != hipSuccess) rc = MOE_ERR_HIP;
     if (have_cur && cur != W->device) (void)hipSetDevice(cur);
     if (rc != MOE_OK) (void)hipGetLastError();

@@ -127,7 +127,7 @@ static int ffn_launch(const moe_weights_t* W, const void* xg, moe_dtype_t act_dt
         return moe_ffn_f32_launch(W, (const float*)xg, perm, k, offsets, N, workspace, yg, s);
     if (W->dtype == MOE_MXFP4)
         return path == MOE_FFN_STREAM ? moe_mx_stream_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, nullptr, s)
-                                      : moe_mx_gemm_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, s);
+                                      : moe_mx_gemm_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, true, nullptr, nullptr, s);
     if (path == MOE_FFN_STREAM)
         return moe_ffn_stream_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, nullptr, s);
     return moe_ffn_grouped_launch(path == MOE_FFN_MID, W, xg, act_dtype, perm, k, offsets, N, workspace, yg, s);
@@ -556,8 +556,12 @@ int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, 
         return moe_mx_stream_launch(W, x, x_dtype, perm, k, offsets, N, workspace, nullptr, &st, s);
     }
     float* yg = (float*)workspace;
-    rc = moe_mx_gemm_launch(W, x, x_dtype, perm, k, offsets, N, (char*)workspace + mx_layer_rows(N, d), yg, s);
-    return rc != MOE_OK ? rc : moe_mx_combine_launch(yg, inv_perm, weights, T, k, d, y, y_dtype, s);
+    const float* slabs = nullptr;
+    int n_parts = 1;
+    rc = moe_mx_gemm_launch(W, x, x_dtype, perm, k, offsets, N, (char*)workspace + mx_layer_rows(N, d), yg,
+                            y_dtype == MOE_F32, &slabs, &n_parts, s);
+    if (rc != MOE_OK) return rc;
+    return moe_mx_combine_launch(slabs, n_parts, (size_t)N * d, inv_perm, weights, T, k, d, y, y_dtype, s);
 }
 
 int moe_rmsnorm(const float* x, int T, int d, float eps, float* h, void* stream) {

@@ -88,6 +88,7 @@ bool moe_mx_gemm_supported(int N, int E, int d, int f);
 size_t moe_mx_gemm_workspace(int N, int E, int d, int f);
 int moe_mx_gemm_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan);
 int moe_mx_gemm_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtype, const int32_t* perm, int k,
-                       const int32_t* offsets, int N, void* ws, float* yg, hipStream_t s);
-int moe_mx_combine_launch(const float* yg, const int32_t* inv_perm, const float* weights, int T, int k, int d, void* y,
-                          moe_dtype_t y_dtype, hipStream_t s);
+                       const int32_t* offsets, int N, void* ws, float* yg, bool y_f32, const float** slabs, int* n_parts,
+                       hipStream_t s);
+int moe_mx_combine_launch(const float* yg, int n_parts, size_t part_stride, const int32_t* inv_perm, const float* weights, int T,
+                          int k, int d, void* y, moe_dtype_t y_dtype, hipStream_t s);

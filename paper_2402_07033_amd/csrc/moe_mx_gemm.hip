@@ -1,17 +1,66 @@
-// Expert FFN over MXFP4 matrices for tens of rows per expert and prompts: a grouped GEMM on the
+// Expert FFN over MXFP4 matrices for several rows per expert and prompts: a grouped GEMM on the
 // bf16 matrix cores.
+//
+// The codes are widened to bf16 in the registers of the wave that multiplies with them (exact, one
+// instruction per two weights, moe_mx.h): a wave owns four fragment rows (64 features) for all rows
+// of its tile, so nothing is widened twice in a workgroup and weights never touch LDS.  The rows
+// come as operand chunks (mx_rows_kernel, and the first projection's epilogue for the second) through
+// a ring of LDS stages that the workgroup's four waves fill with direct-to-LDS loads, one fragment's
+// 128 reduction indices a stage.
+//   * tile: up to RBM blocks of 16 rows of one expert x 256 features; an expert's blocks are dealt
+//     evenly to its tiles, and the loop exists once per number of blocks.
+//   * two workgroups per CU: one's prologue and epilogue run under the other's loop.
+//   * a step waits for its stage, meets the other waves at a barrier (which also frees the stage of
+//     the step before), requests the operands D steps ahead, and multiplies.
+//   * few tiles (second projection): the reduction is cut in S parts, every part a slab of partial
+//     sums, which the combine (or mx_sum_kernel) adds in part order.
+//   * T parts per row: a row of fp32 is three bf16 parts (all 24 bits) where fp32 results are held to
+//     that, else one.
 #include "moe_mx.h"
 #include "moe_frag_pack.h"
 
-#define MXG_RB 4  // 16-row blocks of a tile
+// Rows up to which fp32 operands keep 24 bits.  (Above, as with bf16 weights, rows and h are rounded
+// to bf16: three times the matrix work would bound the call.)
+#define MXG_EXACT_ROWS 72
+#define MXG_WAVES 4
+#define MXG_NF 4   // fragment rows of a wave
+constexpr int mxg_blocks_max(int T) { return T == 3 ? 2 : 8; }  // RBM
+// steps requested ahead, in stages of LDS: 8 KiB .. 64 KiB a workgroup
+constexpr int mxg_depth(int T, int RB) { return RB * T >= 4 ? 1 : RB * T >= 2 ? 2 : 3; }
+constexpr int mxg_lds(int T) {
+    int most = 0;
+    for (int rb = 1; rb <= mxg_blocks_max(T); rb++) {
+        const int b = (mxg_depth(T, rb) + 1) * rb * T * 4096;
+        most = b > most ? b : most;
+    }
+    return most;
+}
 
-// Rows as B operands: block b of 16 rows of an expert, [block][KS][4 j][64 lanes] 16-byte chunks,
+// Eight fp32 values -> their T bf16 parts.
+template <int T>
+__device__ __forceinline__ void mx_parts8(const float (&v)[8], u32x4_t (&o)[T]) {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) r[i] = v[i];
+#pragma unroll
+    for (int t = 0; t < T; t++) {
+        bf16x8_t p;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            p[i] = (__bf16)r[i];
+            r[i] -= (float)p[i];
+        }
+        o[t] = __builtin_bit_cast(u32x4_t, p);
+    }
+}
+
+// Rows as B operands: block b of 16 rows of an expert, [block][KS][4 j][T][64 lanes] 16-byte chunks,
 // lane l of (ks, j): row l % 16, indices ks*128 + 32*(l / 16) + 8j .. +7 (moe_mx.h).  Rows past
-// the expert's last and indices past K are zero.
-template <bool BF16>
+// the expert's last and indices past K are zero.  TH: parts of h.
+template <bool BF16, int T>
 __global__ __launch_bounds__(256) void mx_rows_kernel(const void* __restrict__ x, const int32_t* __restrict__ perm, int k,
                                                       const int32_t* __restrict__ offsets, int E, int N, int K,
-                                                      u32x4_t* __restrict__ xp, u32x4_t* __restrict__ hp, int f) {
+                                                      u32x4_t* __restrict__ xp, u32x4_t* __restrict__ hp, int f, int TH) {
     SegInfo si;
     if (!gg_find_block(offsets, E, N, blockIdx.x, threadIdx.x & 63, si)) return;
     const int KS = mx_frags(K);
@@ -22,26 +71,28 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(const void* __restrict__ x
     if (perm && r < si.rows) src = perm[si.row0 + r] / k;
     for (int i = blockIdx.y * 4 + (threadIdx.x >> 6); i < KS * 4; i += 4 * gridDim.y) {
         const int k0 = (i >> 2) * MX_FRAG_K + kq * MX_BLOCK + (i & 3) * 8;
-        u32x4_t v = {0u, 0u, 0u, 0u};
+        u32x4_t v[T];
+#pragma unroll
+        for (int p = 0; p < T; p++) v[p] = u32x4_t{0u, 0u, 0u, 0u};
         if (r < si.rows && k0 < K) {
             const size_t off = (size_t)src * K + k0;
             if (BF16) {
-                v = *(const u32x4_t*)((const uint16_t*)x + off);
+                v[0] = *(const u32x4_t*)((const uint16_t*)x + off);
             } else {
                 const float4 a = *(const float4*)((const float*)x + off);
                 const float4 b = *(const float4*)((const float*)x + off + 4);
-                v[0] = moe_pack_bf16x2(a.x, a.y);
-                v[1] = moe_pack_bf16x2(a.z, a.w);
-                v[2] = moe_pack_bf16x2(b.x, b.y);
-                v[3] = moe_pack_bf16x2(b.z, b.w);
+                const float f8[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                mx_parts8<T>(f8, v);
             }
         }
-        xp[((size_t)blockIdx.x * KS * 4 + i) * 64 + lane] = v;
+#pragma unroll
+        for (int p = 0; p < T; p++) xp[(((size_t)blockIdx.x * KS * 4 + i) * T + p) * 64 + lane] = v[p];
     }
     // the first projection does not reach the indices of h past f
     if (blockIdx.y == 0 && f % MX_FRAG_K && kq * MX_BLOCK >= f % MX_FRAG_K)
-        hp[((size_t)blockIdx.x * mx_frags(f) * 4 + (mx_frags(f) - 1) * 4 + (threadIdx.x >> 6)) * 64 + lane] =
-            u32x4_t{0u, 0u, 0u, 0u};
+        for (int p = 0; p < TH; p++)
+            hp[(((size_t)blockIdx.x * mx_frags(f) * 4 + (mx_frags(f) - 1) * 4 + (threadIdx.x >> 6)) * TH + p) * 64 + lane] =
+                u32x4_t{0u, 0u, 0u, 0u};
 }
 
 struct MxGemmArgs {
@@ -49,18 +100,29 @@ struct MxGemmArgs {
     const unsigned* wscale;
     const u32x4_t* xp;
     uint16_t* hp;   // up: out
-    float* yg;      // down: out
+    int TH;         // parts of h
+    float* yg;      // down: out, slab 0
+    size_t part_stride;
     const int32_t* offsets;
     int E, N, K, C, NB, KS, KW;
-    int ftiles;
+    int FT;         // feature tiles
+    int S;          // reduction parts
 };
 
-// Tile `t` of RB * 16 rows -> its segment; b: its first block inside the segment.
-template <int RB>
-__device__ __forceinline__ bool mx_find_tile(const int32_t* offsets, int E, int N, int tile, int lane, SegInfo& si, int& b) {
+struct MxTile {
+    SegInfo si;
+    int b0, nblk;   // its blocks inside the segment
+    int ft, part;
+    bool once;      // the expert's only row tile: its weights are read once
+};
+
+// Tile number L of the launch, order expert, then groups of at most 8 row tiles, part and feature
+// tile, row tile; false past the end.  `chunk`: tiles of an XCD.
+template <int RBM>
+__device__ __forceinline__ bool mx_find_tile(const MxGemmArgs& a, int lane, MxTile& ti) {
     int lo, rows;
-    gg_segment_of_lane(offsets, E, N, lane, lo, rows);
-    const int nb = (rows + 15) / 16, nt = (nb + RB - 1) / RB;
+    gg_segment_of_lane(a.offsets, a.E, a.N, lane, lo, rows);
+    const int nb = (rows + 15) / 16, nt = (nb + RBM - 1) / RBM;
     int ib = nb, it = nt;
 #pragma unroll
     for (int dlt = 1; dlt < 64; dlt <<= 1) {
@@ -70,115 +132,258 @@ __device__ __forceinline__ bool mx_find_tile(const int32_t* offsets, int E, int 
             it += vt;
         }
     }
-    const unsigned long long m = __ballot(tile >= it - nt && tile < it);
-    if (m == 0ull) return false;
+    const int FS = a.FT * a.S;
+    const int total = __builtin_amdgcn_readlane(it, 63) * FS;
+    // an XCD takes neighbours of the order, which share operands in its L2
+    const int chunk = (total + 7) / 8, me = blockIdx.x >> 3;
+    const int L = (blockIdx.x & 7) * chunk + me;
+    if (me >= chunk || L >= total) return false;
+    const int base = (it - nt) * FS;
+    const unsigned long long m = __ballot(L >= base && L < base + nt * FS);
     const int e = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(m));
-    si.e = e;
-    si.row0 = __builtin_amdgcn_readlane(lo, e);
-    si.rows = __builtin_amdgcn_readlane(rows, e);
-    si.bbase = __builtin_amdgcn_readlane(ib - nb, e);
-    b = (tile - __builtin_amdgcn_readlane(it - nt, e)) * RB;
+    ti.si.e = e;
+    ti.si.row0 = __builtin_amdgcn_readlane(lo, e);
+    ti.si.rows = __builtin_amdgcn_readlane(rows, e);
+    ti.si.bbase = __builtin_amdgcn_readlane(ib - nb, e);
+    const int tiles = __builtin_amdgcn_readlane(nt, e), blocks = __builtin_amdgcn_readlane(nb, e);
+    int r = L - __builtin_amdgcn_readlane(base, e);
+    const int grp = r / (8 * FS);
+    r -= grp * 8 * FS;
+    const int gw = (tiles - grp * 8) < 8 ? (tiles - grp * 8) : 8;
+    const int fs = r / gw, rt = grp * 8 + r % gw;
+    ti.ft = fs % a.FT;
+    ti.part = fs / a.FT;
+    const int per = blocks / tiles, more = blocks % tiles;
+    ti.b0 = rt * per + (rt < more ? rt : more);
+    ti.nblk = per + (rt < more ? 1 : 0);
+    ti.once = tiles == 1;
     return true;
 }
 
-template <int NMAT, int NBU, int RB>
-__global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs a) {
-    constexpr int NF = NMAT * NBU;
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    SegInfo si;
-    int b0;
-    if (!mx_find_tile<RB>(a.offsets, a.E, a.N, blockIdx.x / a.ftiles, lane, si, b0)) return;
-    const int nblk = (si.rows + 15) / 16 - b0;  // blocks of the tile that are the expert's
-    const int nb0 = ((blockIdx.x % a.ftiles) * 4 + wave) * NBU;
-    if (nb0 >= a.NB) return;
-    const size_t frow = ((size_t)si.e * a.NB + nb0) * NMAT;
-    const u32x4_t* xp = a.xp + (size_t)(si.bbase + b0) * a.KS * 4 * 64 + lane;
+// Buffer descriptor over the 2 GiB from a wave-uniform p on: a request's address is then one lane
+// offset and one scalar.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_rsrc(const void* p) {
+    const unsigned long long v = (unsigned long long)p;
+    const unsigned lo = __builtin_amdgcn_readfirstlane((int)(unsigned)v);
+    const unsigned hi = __builtin_amdgcn_readfirstlane((int)(unsigned)(v >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(((unsigned long long)hi << 32) | lo), 0, (int)0x80000000u, 0x00027000);
+}
+
+// At most n vector-memory requests and no LDS read in flight, then the other waves.
+#define MXG_MEET(n)                                                                \
+    do {                                                                           \
+        __builtin_amdgcn_s_waitcnt(0x0070 | ((n) & 15) | (((n) >> 4) << 14));      \
+        asm volatile("" ::: "memory");                                             \
+        __builtin_amdgcn_s_barrier();                                              \
+        asm volatile("" ::: "memory");                                             \
+    } while (0)
+
+template <int NMAT, int T, int RB>
+__device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& ti, int lane, int wave, unsigned char* smem) {
+    constexpr int NF = MXG_NF, D = mxg_depth(T, RB), NS = D + 1;
+    constexpr int STAGE = RB * T * 4096;
+    constexpr int VREQ = 2 * NF + RB * T;  // requests of a step and wave
+    static_assert((D - 1) * VREQ < 64, "the counter of requests");
+    const int frow0 = (ti.ft * MXG_WAVES + wave) * NF;  // of the expert's NB * NMAT
+    const bool idle = frow0 >= a.NB * NMAT;             // the last feature tile may be short
+    const int k_lo = ti.part * a.KS / a.S, k_hi = (ti.part + 1) * a.KS / a.S;
+    const size_t row = (size_t)ti.si.e * a.NB * NMAT + (idle ? 0 : frow0);
+    const __amdgpu_buffer_rsrc_t rw = mx_rsrc((const char*)a.wfrag + row * a.KS * 1024);
+    const __amdgpu_buffer_rsrc_t rs = mx_rsrc((const char*)a.wscale + row * a.KW * 256);
+    const __amdgpu_buffer_rsrc_t rx = mx_rsrc((const char*)a.xp + (size_t)(ti.si.bbase + ti.b0) * a.KS * (T * 4096));
+
+    u32x4_t q[NS][NF];
+    unsigned sc[NS][NF];
+    auto request = [&](int ks, int slot) __attribute__((always_inline)) {
+        ks = ks < k_hi ? ks : k_hi - 1;  // (past the end: again, so that every step counts the same)
+#pragma unroll
+        for (int r = 0; r < NF; r++) {
+            if (ti.once) q[slot][r] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, (r * a.KS + ks) * 1024, 2));
+            else q[slot][r] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, (r * a.KS + ks) * 1024, 0));
+            sc[slot][r] = __builtin_amdgcn_raw_buffer_load_b32(rs, lane * 4, (r * a.KW + (ks >> 2)) * 256, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < RB * T; i++) {
+            const int c = i * MXG_WAVES + wave;  // chunk of the stage: block c / 4T, (j, part) c % 4T
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rx, (__attribute__((address_space(3))) void*)(smem + slot * STAGE + c * 1024), 16, lane * 16,
+                ((c / (4 * T)) * a.KS + ks) * (T * 4096) + (c % (4 * T)) * 1024, 0, 0);
+        }
+    };
+
     f32x4_t acc[NF][RB];
 #pragma unroll
     for (int r = 0; r < NF; r++)
 #pragma unroll
         for (int b = 0; b < RB; b++) acc[r][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int ks = 0; ks < a.KS; ks++) {
-        u32x4_t q[NF];
-        float scale[NF];
 #pragma unroll
-        for (int r = 0; r < NF; r++) {
-            q[r] = a.wfrag[((frow + r) * a.KS + ks) * 64 + lane];
-            scale[r] = mx_scale(a.wscale[((frow + r) * a.KW + (ks >> 2)) * 64 + lane], ks & 3);
-        }
+    for (int i = 0; i < D; i++) request(k_lo + i, i);
+
+    for (int k = k_lo; k < k_hi; k += NS) {
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            bf16x8_t x[RB];
+        for (int u = 0; u < NS; u++) {
+            if (k + u >= k_hi) break;
+            // this step's requests have arrived, and every wave has read the stage that is refilled now
+            MXG_MEET((D - 1) * VREQ);
+            request(k + u + D, (u + D) % NS);
+            const u32x4_t* st = (const u32x4_t*)(smem + u * STAGE) + lane;
 #pragma unroll
-            for (int b = 0; b < RB; b++)
-                x[b] = __builtin_bit_cast(bf16x8_t, xp[(((size_t)(b < nblk ? b : 0) * a.KS + ks) * 4 + j) * 64]);
-#pragma unroll
-            for (int r = 0; r < NF; r++) {
-                const bf16x8_t w = mx_widen8(q[r][j], scale[r]);
+            for (int j = 0; j < 4; j++) {
+                bf16x8_t x[RB][T];
 #pragma unroll
                 for (int b = 0; b < RB; b++)
-                    acc[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[b], acc[r][b], 0, 0, 0);
+#pragma unroll
+                    for (int t = 0; t < T; t++) x[b][t] = __builtin_bit_cast(bf16x8_t, st[((b * 4 + j) * T + t) * 64]);
+#pragma unroll
+                for (int r = 0; r < NF; r++) {
+                    const bf16x8_t w = mx_widen8(q[u][r][j], mx_scale(sc[u][r] >> (8 * ((k + u) & 3)), 0));
+#pragma unroll
+                    for (int b = 0; b < RB; b++)
+#pragma unroll
+                        for (int t = 0; t < T; t++)
+                            acc[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[b][t], acc[r][b], 0, 0, 0);
+                }
             }
         }
     }
+    // no request for LDS outlives the workgroup
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    if (idle) return;
+
     const int t = lane & 15, kq = lane >> 4;
 #pragma unroll
     for (int b = 0; b < RB; b++) {
-        if (b >= nblk) continue;
 #pragma unroll
-        for (int u = 0; u < NBU; u++) {
-            const int c = (nb0 + u) * 16 + 4 * kq;
+        for (int n = 0; n < NF / NMAT; n++) {
+            const int c = (frow0 / NMAT + n) * 16 + 4 * kq;
             if (NMAT == 2) {
-                // h as the second projection's operand, rounded to bf16 there as the rows are
-                const f32x4_t g = acc[u * NMAT][b], v = acc[u * NMAT + NMAT - 1][b];
+                // h as the second projection's operand
+                const f32x4_t g = acc[n * NMAT][b], v = acc[n * NMAT + NMAT - 1][b];
                 float h[4];
 #pragma unroll
                 for (int i = 0; i < 4; i++) h[i] = g[i] / (1.0f + __expf(-g[i])) * v[i];
-                const size_t chunk = (((size_t)(si.bbase + b0 + b) * mx_frags(a.C) + c / MX_FRAG_K) * 4 + (c % MX_BLOCK) / 8) * 64 +
-                                     (c % MX_FRAG_K) / MX_BLOCK * 16 + t;
-                *(uint2*)(a.hp + chunk * 8 + c % 8) = make_uint2(moe_pack_bf16x2(h[0], h[1]), moe_pack_bf16x2(h[2], h[3]));
+                const size_t chunk = (((size_t)(ti.si.bbase + ti.b0 + b) * mx_frags(a.C) + c / MX_FRAG_K) * 4 + (c % MX_BLOCK) / 8) * a.TH;
+                uint16_t* dst = a.hp + (chunk * 64 + (c % MX_FRAG_K) / MX_BLOCK * 16 + t) * 8 + c % 8;
+                for (int p = 0; p < a.TH; p++) {
+                    *(uint2*)(dst + (size_t)p * 512) = make_uint2(moe_pack_bf16x2(h[0], h[1]), moe_pack_bf16x2(h[2], h[3]));
+#pragma unroll
+                    for (int i = 0; i < 4; i++) h[i] -= moe_bf16_to_f32(moe_bf16_rne(h[i]));
+                }
             } else {
-                const int row = (b0 + b) * 16 + t;
-                if (row < si.rows)
-                    *(float4*)(a.yg + (size_t)(si.row0 + row) * a.C + c) =
-                        make_float4(acc[u][b][0], acc[u][b][1], acc[u][b][2], acc[u][b][3]);
+                const int rr = (ti.b0 + b) * 16 + t;
+                if (rr < ti.si.rows)
+                    *(float4*)(a.yg + ti.part * a.part_stride + (size_t)(ti.si.row0 + rr) * a.C + c) =
+                        make_float4(acc[n][b][0], acc[n][b][1], acc[n][b][2], acc[n][b][3]);
             }
         }
     }
 }
 
+template <int NMAT, int T>
+__global__ __launch_bounds__(64 * MXG_WAVES, 2) void mx_gemm_kernel(MxGemmArgs a) {
+    constexpr int RBM = mxg_blocks_max(T);
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    MxTile ti;
+    if (!mx_find_tile<RBM>(a, lane, ti)) return;
+    switch (ti.nblk) {
+        case 1: mx_gemm_tile<NMAT, T, 1>(a, ti, lane, wave, smem); break;
+        case 2: mx_gemm_tile<NMAT, T, 2>(a, ti, lane, wave, smem); break;
+        default:
+            if constexpr (RBM > 2) {
+                switch (ti.nblk) {
+                    case 3: mx_gemm_tile<NMAT, T, 3>(a, ti, lane, wave, smem); break;
+                    case 4: mx_gemm_tile<NMAT, T, 4>(a, ti, lane, wave, smem); break;
+                    case 5: mx_gemm_tile<NMAT, T, 5>(a, ti, lane, wave, smem); break;
+                    case 6: mx_gemm_tile<NMAT, T, 6>(a, ti, lane, wave, smem); break;
+                    case 7: mx_gemm_tile<NMAT, T, 7>(a, ti, lane, wave, smem); break;
+                    default: mx_gemm_tile<NMAT, T, 8>(a, ti, lane, wave, smem); break;
+                }
+            }
+    }
+}
+
+// yg = slab 0 + slab 1 + ... in that order.
+__global__ __launch_bounds__(256) void mx_sum_kernel(const float4* __restrict__ slabs, size_t n4, int S, float4* __restrict__ yg) {
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (size_t)gridDim.x * 256) {
+        float4 s = slabs[i];
+        for (int p = 1; p < S; p++) {
+            const float4 v = slabs[(size_t)p * n4 + i];
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        yg[i] = s;
+    }
+}
+
+// ------------------------------------------------------------------ host ----
 static inline size_t mxg_align256(size_t v) { return (v + 255) & ~(size_t)255; }
 static inline size_t mxg_blocks(int N, int E) { return (size_t)N / 16 + E; }
 
-bool moe_mx_gemm_supported(int N, int E, int d, int f) {
-    const long long tiles = N / (16 * MXG_RB) + E;
-    return tiles * ((d > f ? d : f) / 16) < (1ll << 31);
+struct MxGemmShape {
+    int tu, td;  // parts of the rows and of h
+    int S;       // reduction parts of the second projection
+    int upper;   // row tiles, at most (of the fewest blocks a tile may have)
+};
+static MxGemmShape mxg_shape(int N, int E, int d, int f, bool x_f32, bool y_f32) {
+    MxGemmShape sh;
+    sh.tu = x_f32 && y_f32 && N <= MXG_EXACT_ROWS ? 3 : 1;
+    sh.td = y_f32 && N <= MXG_EXACT_ROWS ? 3 : 1;
+    // row tiles that there are about: the experts in use, and those of full tiles
+    const int rows = 16 * mxg_blocks_max(sh.td);
+    const int tiles = N / rows + (N < E ? N : E);
+    const int ft = (d / 16 + MXG_WAVES * MXG_NF - 1) / (MXG_WAVES * MXG_NF);
+    int S = 512 / (tiles * ft);
+    const int most = mx_frags(f) / 8;
+    if (S > most) S = most;
+    if (S > 8) S = 8;
+    sh.S = S < 1 ? 1 : S;
+    return sh;
 }
 
-// the rows' and h's operand chunks
+bool moe_mx_gemm_supported(int N, int E, int d, int f) {
+    const long long tiles = N / 32 + E;
+    return tiles * 8 * ((d > f ? d : f) / 16) < (1ll << 31);
+}
+
+// the rows' and h's operand chunks, the second projection's slabs
 size_t moe_mx_gemm_workspace(int N, int E, int d, int f) {
-    return mxg_align256(mxg_blocks(N, E) * mx_frags(d) * 4096) + mxg_align256(mxg_blocks(N, E) * mx_frags(f) * 4096);
+    const MxGemmShape sh = mxg_shape(N, E, d, f, true, true), sb = mxg_shape(N, E, d, f, false, false);
+    const int S = sh.S > sb.S ? sh.S : sb.S;
+    return mxg_align256(mxg_blocks(N, E) * mx_frags(d) * 4096 * sh.tu) +
+           mxg_align256(mxg_blocks(N, E) * mx_frags(f) * 4096 * sh.td) + (S > 1 ? (size_t)S * N * d * 4 : 0);
 }
 
 int moe_mx_gemm_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan) {
     if (!moe_mx_gemm_supported(N, E, d, f)) return MOE_ERR_UNSUPPORTED;
-    plan->up_tile_rows = plan->down_tile_rows = 16 * MXG_RB;
-    plan->up_tile_features = plan->down_tile_features = 256;
+    plan->up_tile_rows = plan->down_tile_rows = 16 * mxg_blocks_max(N <= MXG_EXACT_ROWS ? 3 : 1);
+    plan->up_tile_features = plan->down_tile_features = MXG_WAVES * MXG_NF * 16;
     return MOE_OK;
 }
 
+template <int NMAT, int T>
+static void mxg_go(const MxGemmArgs& a, hipStream_t s) {
+    const unsigned rtiles = (unsigned)(a.N / (16 * mxg_blocks_max(T)) + a.E);
+    const unsigned grid = (rtiles * (unsigned)(a.FT * a.S) + 7) / 8 * 8;
+    hipLaunchKernelGGL((mx_gemm_kernel<NMAT, T>), dim3(grid), dim3(64 * MXG_WAVES), mxg_lds(T), s, a);
+}
+
+// The result in n_parts slabs of [N,d] floats from *slabs on, where the caller asks for them; else yg.
 int moe_mx_gemm_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtype, const int32_t* perm, int k,
-                       const int32_t* offsets, int N, void* ws, float* yg, hipStream_t s) {
+                       const int32_t* offsets, int N, void* ws, float* yg, bool y_f32, const float** slabs, int* n_parts,
+                       hipStream_t s) {
     const int E = W->E, d = W->d, f = W->f;
+    const MxGemmShape sh = mxg_shape(N, E, d, f, act_dtype == MOE_F32, y_f32);
     u32x4_t* xp = (u32x4_t*)ws;
-    u32x4_t* hp = (u32x4_t*)((char*)ws + mxg_align256(mxg_blocks(N, E) * mx_frags(d) * 4096));
+    u32x4_t* hp = (u32x4_t*)((char*)xp + mxg_align256(mxg_blocks(N, E) * mx_frags(d) * 4096 * sh.tu));
+    float* parts = (float*)((char*)hp + mxg_align256(mxg_blocks(N, E) * mx_frags(f) * 4096 * sh.td));
     const dim3 grid((unsigned)mxg_blocks(N, E), (unsigned)((mx_frags(d) + 7) / 8));
     if (act_dtype == MOE_BF16)
-        hipLaunchKernelGGL(mx_rows_kernel<true>, grid, dim3(256), 0, s, x, perm, k, offsets, E, N, d, xp, hp, f);
+        hipLaunchKernelGGL((mx_rows_kernel<true, 1>), grid, dim3(256), 0, s, x, perm, k, offsets, E, N, d, xp, hp, f, sh.td);
+    else if (sh.tu == 1)
+        hipLaunchKernelGGL((mx_rows_kernel<false, 1>), grid, dim3(256), 0, s, x, perm, k, offsets, E, N, d, xp, hp, f, sh.td);
     else
-        hipLaunchKernelGGL(mx_rows_kernel<false>, grid, dim3(256), 0, s, x, perm, k, offsets, E, N, d, xp, hp, f);
-    const unsigned rtiles = (unsigned)(N / (16 * MXG_RB) + E);
+        hipLaunchKernelGGL((mx_rows_kernel<false, 3>), grid, dim3(256), 0, s, x, perm, k, offsets, E, N, d, xp, hp, f, sh.td);
     MxGemmArgs a = {};
     a.offsets = offsets;
     a.E = E; a.N = N;
@@ -186,32 +391,52 @@ int moe_mx_gemm_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtyp
     a.wscale = (const unsigned*)W->s13;
     a.xp = xp;
     a.hp = (uint16_t*)hp;
+    a.TH = sh.td;
     a.K = d; a.C = f; a.NB = f / 16; a.KS = mx_frags(d); a.KW = mx_words(d);
-    a.ftiles = (a.NB + 7) / 8;
-    hipLaunchKernelGGL((mx_gemm_kernel<2, 2, MXG_RB>), dim3(rtiles * a.ftiles), dim3(256), 0, s, a);
+    a.FT = (2 * a.NB + MXG_WAVES * MXG_NF - 1) / (MXG_WAVES * MXG_NF);
+    a.S = 1;
+    if (sh.tu == 1) mxg_go<2, 1>(a, s);
+    else mxg_go<2, 3>(a, s);
     moe_record_mid_event(s);
     a.wfrag = (const u32x4_t*)W->w2;
     a.wscale = (const unsigned*)W->s2;
     a.xp = hp;
-    a.yg = yg;
+    a.yg = sh.S > 1 ? parts : yg;
+    a.part_stride = (size_t)N * d;
     a.K = f; a.C = d; a.NB = d / 16; a.KS = mx_frags(f); a.KW = mx_words(f);
-    a.ftiles = (a.NB + 15) / 16;
-    hipLaunchKernelGGL((mx_gemm_kernel<1, 4, MXG_RB>), dim3(rtiles * a.ftiles), dim3(256), 0, s, a);
+    a.FT = (a.NB + MXG_WAVES * MXG_NF - 1) / (MXG_WAVES * MXG_NF);
+    a.S = sh.S;
+    if (sh.td == 1) mxg_go<1, 1>(a, s);
+    else mxg_go<1, 3>(a, s);
+    if (slabs) {
+        *slabs = a.yg;
+        *n_parts = sh.S;
+    } else if (sh.S > 1) {
+        const size_t n4 = (size_t)N * d / 4;
+        const size_t blocks = (n4 + 255) / 256;
+        hipLaunchKernelGGL(mx_sum_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s,
+                           (const float4*)parts, n4, sh.S, (float4*)yg);
+    }
     return moe_launch_status();
 }
 
-// y[t,:] = sum_j weights[t,j] * yg[inv_perm[t*k+j],:], rounded once to y's type.
+// y[t,:] = sum_j weights[t,j] * (the parts of row inv_perm[t*k+j], in order), rounded once to y's type.
 template <bool BF16>
-__global__ __launch_bounds__(256) void mx_combine_kernel(const float4* __restrict__ yg, const int32_t* __restrict__ inv_perm,
-                                                         const float* __restrict__ weights, int T, int k, int row_chunks,
-                                                         void* __restrict__ y) {
+__global__ __launch_bounds__(256) void mx_combine_kernel(const float4* __restrict__ yg, int n_parts, size_t part4,
+                                                         const int32_t* __restrict__ inv_perm, const float* __restrict__ weights,
+                                                         int T, int k, int row_chunks, void* __restrict__ y) {
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c >= row_chunks) return;
     for (int t = blockIdx.y; t < T; t += gridDim.y) {
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int j = 0; j < k; j++) {
             const float w = weights[(size_t)t * k + j];
-            const float4 v = yg[(size_t)inv_perm[(size_t)t * k + j] * row_chunks + c];
+            const float4* p = yg + (size_t)inv_perm[(size_t)t * k + j] * row_chunks + c;
+            float4 v = *p;
+            for (int i = 1; i < n_parts; i++) {
+                const float4 u = p[i * part4];
+                v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+            }
             acc.x += w * v.x;
             acc.y += w * v.y;
             acc.z += w * v.z;
@@ -223,15 +448,12 @@ __global__ __launch_bounds__(256) void mx_combine_kernel(const float4* __restric
     }
 }
 
-int moe_mx_combine_launch(const float* yg, const int32_t* inv_perm, const float* weights, int T, int k, int d, void* y,
-                          moe_dtype_t y_dtype, hipStream_t s) {
+int moe_mx_combine_launch(const float* yg, int n_parts, size_t part_stride, const int32_t* inv_perm, const float* weights, int T,
+                          int k, int d, void* y, moe_dtype_t y_dtype, hipStream_t s) {
     const int row_chunks = d / 4;
     const dim3 grid((unsigned)((row_chunks + 255) / 256), (unsigned)(T < 65535 ? T : 65535));
-    if (y_dtype == MOE_BF16)
-        hipLaunchKernelGGL(mx_combine_kernel<true>, grid, dim3(256), 0, s, (const float4*)yg, inv_perm, weights, T, k,
-                           row_chunks, y);
-    else
-        hipLaunchKernelGGL(mx_combine_kernel<false>, grid, dim3(256), 0, s, (const float4*)yg, inv_perm, weights, T, k,
-                           row_chunks, y);
+    auto* kernel = y_dtype == MOE_BF16 ? mx_combine_kernel<true> : mx_combine_kernel<false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, (const float4*)yg, n_parts, part_stride / 4, inv_perm, weights, T, k,
+                       row_chunks, y);
     return moe_launch_status();
 }

@@ -3,22 +3,24 @@
 // A few rows per expert are bound by reading each active expert's matrices once, here 17/32
 // byte per weight.  The plan is that of the bf16 kernels (moe_ffn_stream.hip): a wave streams
 // fragments of 16 features by 128 reduction indices with 16-byte-per-lane loads, widens the
-// codes to bf16 in registers (exact, moe_mx.h), and multiplies them with up to 16 rows on
-// v_mfma_f32_16x16x32_bf16, fp32 accumulate; fp32 rows are split into bf16 high and low parts
-// (~2^-16 relative).  The waves of a workgroup split the reduction, one scale word (four
+// codes to bf16 in registers (exact, moe_mx.h), and multiplies them with the rows on
+// v_mfma_f32_16x16x32_bf16, fp32 accumulate; fp32 rows are split into three bf16 parts, which
+// hold all 24 bits.  The waves of a workgroup split the reduction, one scale word (four
 // fragments, 512 indices) each, and keep their slice of the rows in registers over all
 // consecutive units of the same rows; their partial tiles meet in LDS.
 //
-// A unit is (tile of <= 16 rows of one expert, reduction part, group of NBU blocks of 16
-// features); the units are dealt to the workgroups in contiguous, equal ranges.
-//   up   (x.w1, x.w3 -> silu*mul -> h, fp32): one part.  Its prologue may route the tokens and
-//        batch them (up to 64 slots).
+// A unit is (tile of rows of one expert, reduction part, group of NBU blocks of 16 features); the
+// units are dealt to the workgroups in contiguous, equal ranges, and the loads of two units are
+// in flight.
+//   up   (x.w1, x.w3 -> silu*mul -> h): one part.  Its prologue may route the tokens and batch
+//        them (up to 64 slots).  h is fp32, or bf16 where the result is.
 //   down (h.w2): P parts.  Every unit leaves its partial sums in slab [part][N][d]; a counter
 //        per feature group tells the workgroup that finishes the group's last unit, and that
 //        one adds the parts in part order -- and the rows of a token in slot order, weighted,
 //        with the residual and the next block's gating sums if asked for.  The sums' order does
 //        not depend on who is last, so the result does not either.  The layer is two launches.
 #include <atomic>
+#include <type_traits>
 
 #include "moe_mx.h"
 #include "moe_gate_wave.h"
@@ -43,43 +45,44 @@ struct MxArgs {
     unsigned* counters;       // [n_counters], one per feature group of the second projection:
     int n_counters;           // cleared by up, counted by down
     int finish;
+    int h_bf16;               // up: h is bf16
     float* yg;                // FIN_ROWS: out
     MxStep st;
 };
 enum { FIN_NONE = 0, FIN_ROWS = 1, FIN_LAYER = 2 };
 
-// How a tile's rows become the matrix instructions' 16 operand columns.  fp32 rows are a bf16
-// high and a bf16 low part each: with at most 8 rows both parts share one instruction (columns
-// t and t + 8, added in the end), which halves the registers that hold the rows; with up to 16
-// they take one each.
-enum { ROWS_BF16 = 0, ROWS_SPLIT8 = 1, ROWS_SPLIT16 = 2 };
-constexpr int rows_of(int R) { return R == ROWS_SPLIT8 ? 8 : 16; }
-constexpr int terms_of(int R) { return R == ROWS_SPLIT16 ? 2 : 1; }
+// How a tile's rows become the matrix instructions' 16 operand columns.  An fp32 row is three
+// bf16 parts, and 5 rows have all their parts in one instruction (columns t, t + 5, t + 10, added
+// in the end).  More rows of an expert are more tiles: the registers that hold two operands a row
+// would not leave room for two units in flight.
+enum { ROWS_BF16 = 0, ROWS_F32 = 1 };
+constexpr int rows_of(int R) { return R == ROWS_BF16 ? 16 : 5; }
 
 // The wave's slice of the rows: four fragments' worth of reduction indices from fragment ks0.
 template <int R>
-__device__ __forceinline__ void mx_load_act(bf16x8_t (&act)[4][4][terms_of(R)], const void* actp, int K, int row0, int rows,
+__device__ __forceinline__ void mx_load_act(bf16x8_t (&act)[4][4], const void* actp, int K, int row0, int rows,
                                             int ks0, int lane, const int* rowmap, const int32_t* perm, int perm_k,
                                             const float* row_scale) {
 #pragma clang fp contract(off)
-    const int t = lane & (rows_of(R) - 1), kq = lane >> 4;
-    const bool low = R == ROWS_SPLIT8 && (lane & 8);
+    const int c = lane & 15, kq = lane >> 4;
+    const int t = R == ROWS_BF16 ? c : c % rows_of(R), part = R == ROWS_BF16 ? 0 : c / rows_of(R);
+    const bool used = t < rows && part < 3;
     int src_row = row0 + t;
-    if (rowmap && t < rows) src_row = rowmap[row0 + t];
-    if (perm && t < rows) src_row = perm[row0 + t] / perm_k;
+    if (rowmap && used) src_row = rowmap[row0 + t];
+    if (perm && used) src_row = perm[row0 + t] / perm_k;
     float sc = 1.0f;
-    if (R != ROWS_BF16 && row_scale && t < rows) sc = row_scale[src_row];
+    if (R != ROWS_BF16 && row_scale && used) sc = row_scale[src_row];
 #pragma unroll
     for (int s = 0; s < 4; s++) {
         const int k0 = (ks0 + s) * MX_FRAG_K + kq * MX_BLOCK;
-        const bool live = t < rows && k0 < K;
+        const bool live = used && k0 < K;
         const size_t off = (size_t)src_row * K + k0;
         if (R == ROWS_BF16) {
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 u32x4_t v = {0u, 0u, 0u, 0u};
                 if (live) v = *(const u32x4_t*)((const uint16_t*)actp + off + 8 * j);
-                act[s][j][0] = __builtin_bit_cast(bf16x8_t, v);
+                act[s][j] = __builtin_bit_cast(bf16x8_t, v);
             }
             continue;
         }
@@ -92,44 +95,78 @@ __device__ __forceinline__ void mx_load_act(bf16x8_t (&act)[4][4][terms_of(R)], 
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             // the scaled row is rounded to fp32 before the split, as if it had been stored
-            bf16x8_t h, l;
+            bf16x8_t a;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const float v = x[2 * j + i / 4][i % 4] * sc;
-                h[i] = (__bf16)v;
-                l[i] = (__bf16)(v - (float)h[i]);
+                const __bf16 hi = (__bf16)v;
+                const float r = v - (float)hi;
+                const __bf16 mid = (__bf16)r, lo = (__bf16)(r - (float)mid);
+                a[i] = part == 0 ? hi : part == 1 ? mid : lo;
             }
-            act[s][j][0] = low ? l : h;
-            if (R == ROWS_SPLIT16) act[s][j][terms_of(R) - 1] = l;
+            act[s][j] = a;
         }
         // (the requests of more fragments at once would not fit in registers)
-        if (R == ROWS_SPLIT16 || (s & 1)) __builtin_amdgcn_sched_barrier(0);
+        if (s & 1) __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-// Per-expert batching of N <= 64 slots by one wave, as permute_indices_wave with up to 64
-// experts.  Lane e < E gets its expert's rows [lo, lo + cnt).
+// Sum of one wave's partial tile over the columns of a row's parts, for lanes of columns < rows.
+template <int R>
+__device__ __forceinline__ f32x4_t mx_parts_sum(const f32x4_t* p, int lane) {
+    if (R == ROWS_BF16) return p[lane];
+    const int at = (lane & 48) + (lane & 15) % rows_of(R);
+    return p[at] + p[at + 5] + p[at + 10];
+}
+
+// Slabs are written by one workgroup and read by another of the same launch, maybe on another XCD,
+// whose L2 is another: both sides go past the caches that the other does not share, so that
+// neither has to write back or drop a whole cache (device fences by every wave made the second
+// projection of one token 72 us long instead of 21).
+__device__ __forceinline__ void mx_store_shared(float* p, const f32x4_t& v) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    __hip_atomic_store((unsigned long long*)p, __builtin_bit_cast(unsigned long long, f2{v[0], v[1]}), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store((unsigned long long*)p + 1, __builtin_bit_cast(unsigned long long, f2{v[2], v[3]}), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x4_t mx_load_shared(const float* p) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    const f2 a = __builtin_bit_cast(f2, __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    const f2 b = __builtin_bit_cast(f2, __hip_atomic_load((const unsigned long long*)p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    return f32x4_t{a[0], a[1], b[0], b[1]};
+}
+
+// Per-expert batching of N <= 64 slots by one wave, E <= 64: lane p owns slot p and finds the slots
+// of its expert with one ballot per bit of the expert's number.  Lane e < E gets its expert's rows
+// [lo, lo + cnt); s_pos[p]: the slot's position; s_cnt [64]: scratch.
 __device__ __forceinline__ void mx_batch_wave(const int* s_idx, int N, int E, int lane, bool write, const MxStep& st,
-                                              int* s_pos, int& lo, int& cnt) {
-    int e = -1;
-    if (lane < N) {
-        e = s_idx[lane];
-        e = e < 0 ? 0 : (e >= E ? E - 1 : e);
+                                              int* s_pos, int* s_cnt, int& lo, int& cnt) {
+    const bool live = lane < N;
+    const int e = live ? s_idx[lane] : 0;
+    unsigned long long same = __ballot(live);
+#pragma unroll
+    for (int b = 0; b < 6; b++) {
+        const unsigned long long m = __ballot((e >> b) & 1);
+        same &= ((e >> b) & 1) ? m : ~m;
     }
-    const unsigned long long below = (lane == 0) ? 0ull : (~0ull >> (64 - lane));
-    int run = 0, pos = 0;
-    lo = cnt = 0;
-    for (int ee = 0; ee < E; ee++) {
-        const unsigned long long m = __ballot(e == ee);
-        const int c = __popcll(m);
-        if (e == ee) pos = run + __popcll(m & below);
-        if (lane == ee) {
-            cnt = c;
-            lo = run;
-        }
-        run += c;
+    const int rank = __popcll(same & ((lane == 0) ? 0ull : (~0ull >> (64 - lane))));
+    s_cnt[lane] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (live && rank == 0) s_cnt[e] = __popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    cnt = s_cnt[lane];
+    int inc = cnt;
+#pragma unroll
+    for (int dlt = 1; dlt < 64; dlt <<= 1) {
+        const int v = __shfl_up(inc, dlt, 64);
+        if (lane >= dlt) inc += v;
     }
-    if (lane < N) {
+    lo = inc - cnt;
+    const int pos = __shfl(lo, e, 64) + rank;
+    if (live) {
         s_pos[lane] = pos;
         if (write) {
             st.perm[pos] = lane;
@@ -141,31 +178,40 @@ __device__ __forceinline__ void mx_batch_wave(const int* s_idx, int N, int E, in
             st.counts[lane] = cnt;
             st.offsets[lane] = lo;
         }
-        if (lane == 0) st.offsets[E] = run;
+        if (lane == E - 1) st.offsets[E] = inc;
     }
 }
 
-// The workgroup's waves route the tokens, G lanes per token.
-template <int G>
-__device__ __forceinline__ void mx_route(const float* logits, const MxStep& st, int E, int tid, int threads, int* s_idx,
-                                         bool write) {
-    const int gl = tid % G;
-    for (int t0 = 0; t0 < st.T; t0 += threads / G) {
-        const int t = t0 + tid / G;
-        float v = -INFINITY;
-        int e = 0x7fffffff;
-        if (t < st.T && gl < E) {
-            v = logits[(size_t)t * E + gl];
-            e = gl;
+// The workgroup's waves route the tokens, one at a time each: lane e holds expert e's logit, and its
+// rank is the number of logits before it (larger, or equal and of a lower expert).  k rounds of a
+// contest by exchanges between lanes, as in moe_route, take 2.5 us for 64 experts and k = 6; this
+// a fifth.  The weights, which only the writing workgroup needs, are moe_route's to the bit.
+__device__ __forceinline__ void mx_route(const float* logits, const MxStep& st, int E, int wave, int W, int lane, int* s_idx,
+                                         float* s_top, bool write) {
+    for (int t = wave; t < st.T; t += W) {
+        const float v = lane < E ? logits[(size_t)t * E + lane] : -INFINITY;
+        int rank = 0;
+        for (int e = 0; e < E; e++) {
+            const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), e));
+            rank += (lane > e ? o >= v : o > v) ? 1 : 0;
         }
-        int my_i;
-        const float w = route_token<G>(v, e, gl, st.k, my_i);
-        if (t < st.T && gl < st.k) {
-            s_idx[t * st.k + gl] = my_i;
-            if (write) {
-                st.idx[(size_t)t * st.k + gl] = my_i;
-                st.weights[(size_t)t * st.k + gl] = w;
-            }
+        if (lane < st.k) s_idx[t * st.k + lane] = 0;  // (logits that are NaN leave ranks out)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (lane < E && rank < st.k) {
+            s_idx[t * st.k + rank] = lane;
+            s_top[t * st.k + rank] = v;
+        }
+        if (!write) continue;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const float u = lane < st.k ? expf(s_top[t * st.k + lane] - s_top[t * st.k]) : 0.f;
+        float sum = u;
+#pragma unroll
+        for (int m = 1; m < MOE_MAX_K; m <<= 1) sum += __shfl_xor(sum, m, 64);
+        if (lane < st.k) {
+            st.idx[(size_t)t * st.k + lane] = s_idx[t * st.k + lane];
+            st.weights[(size_t)t * st.k + lane] = u / sum;
         }
     }
 }
@@ -177,12 +223,17 @@ __device__ void mx_finish(const MxArgs& a, int g, int tid, int threads, float* s
     const size_t col0 = (size_t)g * NBU * 16;
     auto row_sum = [&](int row, int c4) -> float4 {
         const float* p = a.out + (size_t)row * a.C + col0 + 4 * c4;
-        float4 v = *(const float4*)p;
-        for (int q = 1; q < a.P; q++) {
-            const float4 u = *(const float4*)(p + (size_t)q * a.part_stride);
-            v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+        f32x4_t v = mx_load_shared(p);
+        for (int q = 1; q < a.P; q += 4) {  // four requests at a time, added in order
+            f32x4_t u[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (q + i < a.P) u[i] = mx_load_shared(p + (size_t)(q + i) * a.part_stride);
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (q + i < a.P) v += u[i];
         }
-        return v;
+        return make_float4(v[0], v[1], v[2], v[3]);
     };
     if (a.finish == FIN_ROWS) {
         for (int i = tid; i < a.N * C4; i += threads) {
@@ -239,14 +290,13 @@ __device__ void mx_finish(const MxArgs& a, int g, int tid, int threads, float* s
 template <int NMAT, int NBU, int R, bool GATE>
 __global__ __launch_bounds__(64 * MXS_MAX_WAVES) void mx_stream_kernel(MxArgs a) {
     constexpr bool DOWN = NMAT == 1;
-    constexpr int TERMS = terms_of(R);
     constexpr int NF = NMAT * NBU;  // fragment rows of a unit
-    constexpr int NL = 4 * NF;      // fragment loads per unit and wave, all in flight ahead
     extern __shared__ __align__(16) unsigned char s_raw[];
     f32x4_t* s_red = (f32x4_t*)s_raw;  // [2][W][NF][64]
     __shared__ int s_tiles[MXS_MAX_WAVES][3][MXS_MAX_TILES];
     __shared__ int s_idx[GATE ? MXS_MAX_SLOTS : 1];
-    __shared__ int s_batch[GATE ? MXS_MAX_WAVES : 1][2][MXS_MAX_SLOTS];
+    __shared__ float s_top[GATE ? MXS_MAX_SLOTS : 1];
+    __shared__ int s_batch[GATE ? MXS_MAX_WAVES : 1][3][MXS_MAX_SLOTS];
     __shared__ float s_gate[GATE ? 3 : 1][64];  // the summed shares, 1/rms per token, the logits
     __shared__ float s_gpart[GATE ? MXS_MAX_WAVES : 1][GS_MAX_ITEMS];
     __shared__ unsigned long long s_last;
@@ -298,13 +348,12 @@ __global__ __launch_bounds__(64 * MXS_MAX_WAVES) void mx_stream_kernel(MxArgs a)
             lg = s_gate[2];
             row_scale = s_gate[1];
         }
-        if (a.E <= 16) mx_route<16>(lg, st, a.E, tid, threads, s_idx, blockIdx.x == 0);
-        else mx_route<64>(lg, st, a.E, tid, threads, s_idx, blockIdx.x == 0);
+        mx_route(lg, st, a.E, wave, a.W, lane, s_idx, s_top, blockIdx.x == 0);
         __syncthreads();
         int cnt;
         int* s_pos = s_batch[wave][0];
         int* s_src = s_batch[wave][1];
-        mx_batch_wave(s_idx, a.N, a.E, lane, blockIdx.x == 0 && wave == 0, st, s_pos, lo, cnt);
+        mx_batch_wave(s_idx, a.N, a.E, lane, blockIdx.x == 0 && wave == 0, st, s_pos, s_batch[wave][2], lo, cnt);
         if (lane < a.N) s_src[s_pos[lane]] = lane / st.k;
         hi = lo + cnt;
         rowmap = s_src;
@@ -359,102 +408,106 @@ __global__ __launch_bounds__(64 * MXS_MAX_WAVES) void mx_stream_kernel(MxArgs a)
         return __builtin_nontemporal_load(a.wscale + ((n.row + r) * a.KW + w) * 64 + lane);
     };
 
-    Unit cur = unit_of(u_begin);
-    u32x4_t buf[NL];
-    unsigned sc[NF];
+    Unit unit[2];
+    u32x4_t buf[2][NF][4];
+    unsigned sc[2][NF];
+    auto request = [&](int st, int r) __attribute__((always_inline)) {
+        sc[st][r] = ld_scale(unit[st], r);
 #pragma unroll
-    for (int r = 0; r < NF; r++) {
-        sc[r] = ld_scale(cur, r);
+        for (int s = 0; s < 4; s++) buf[st][r][s] = ld(unit[st], r * 4 + s);
+    };
+    unit[0] = unit_of(u_begin);
 #pragma unroll
-        for (int s = 0; s < 4; s++) buf[r * 4 + s] = ld(cur, r * 4 + s);
+    for (int r = 0; r < NF; r++) request(0, r);
+    unit[1] = unit_of(u_begin + 1 < u_end ? u_begin + 1 : u_begin);
+    if (u_begin + 1 < u_end) {
+#pragma unroll
+        for (int r = 0; r < NF; r++) request(1, r);
     }
 
-    bf16x8_t act[4][4][TERMS];
-    int cur_tile = -1, cur_part = -1, it = 0;
-    for (unsigned u = u_begin; u < u_end; ++u, ++it) {
+    bf16x8_t act[4][4];
+    int cur_tile = -1, cur_part = -1;
+    // unit u, whose loads are in stage st, and the requests of unit u + 2
+    auto process = [&](auto stage, unsigned u) __attribute__((always_inline)) {
+        constexpr int st = decltype(stage)::value;
+        const Unit cur = unit[st];
         const int row0 = s_tr0[cur.tile], rows = s_trn[cur.tile];
         if (cur.tile != cur_tile || cur.part != cur_part) {
             mx_load_act<R>(act, a.act, a.K, row0, rows, cur.word * 4, lane, rowmap, a.row_perm, a.row_k, row_scale);
             cur_tile = cur.tile;
             cur_part = cur.part;
         }
-        const bool has_next = u + 1 < u_end;
-        const Unit next = has_next ? unit_of(u + 1) : cur;
-
-        f32x4_t* red = s_red + (size_t)((it & 1) * a.W + wave) * NF * 64 + lane;
+        const bool more = u + 2 < u_end;
+        if (more) unit[st] = unit_of(u + 2);
+        const int phase = (int)(u - u_begin);  // of the turns and of the two halves of s_red: its parity is st
+        f32x4_t* red = s_red + (size_t)(st * a.W + wave) * NF * 64;
 #pragma unroll
         for (int r = 0; r < NF; r++) {
-            f32x4_t acc[TERMS];
-#pragma unroll
-            for (int t = 0; t < TERMS; t++) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < 4; s++) {
-                const u32x4_t q = buf[r * 4 + s];
-                const float scale = mx_scale(sc[r], s);
+                const u32x4_t q = buf[st][r][s];
+                const float scale = mx_scale(sc[st][r], s);
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
-                    const bf16x8_t w = mx_widen8(q[j], scale);
-#pragma unroll
-                    for (int t = 0; t < TERMS; t++)
-                        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, act[s][j][t], acc[t], 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx_widen8(q[j], scale), act[s][j], acc, 0, 0, 0);
                 }
-                if (has_next) buf[r * 4 + s] = ld(next, r * 4 + s);
             }
-            if (has_next) sc[r] = ld_scale(next, r);
-            f32x4_t v = acc[0];
-            if (TERMS == 2) v += acc[TERMS - 1];
-            red[r * 64] = v;
+            if (more) request(st, r);
+            red[r * 64 + lane] = acc;
         }
         __syncthreads();
         // the waves take turns at the blocks' sums
 #pragma unroll
         for (int b = 0; b < NBU; b++) {
-            if (wave != (it * NBU + b) % a.W) continue;
+            if (wave != (phase * NBU + b) % a.W) continue;
             f32x4_t sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
             for (int w = 0; w < a.W; w++) {
-                const f32x4_t* p = s_red + (size_t)((it & 1) * a.W + w) * NF * 64 + lane;
-                sa += p[b * NMAT * 64];
-                if (NMAT == 2) sb += p[(b * NMAT + NMAT - 1) * 64];
-                if (R == ROWS_SPLIT8) {  // the low parts' columns (lanes of columns 8 .. 15 store nothing)
-                    sa += p[b * NMAT * 64 + (lane & 8 ? 0 : 8)];
-                    if (NMAT == 2) sb += p[(b * NMAT + NMAT - 1) * 64 + (lane & 8 ? 0 : 8)];
-                }
+                const f32x4_t* p = s_red + (size_t)(st * a.W + w) * NF * 64 + b * NMAT * 64;
+                sa += mx_parts_sum<R>(p, lane);
+                if (NMAT == 2) sb += mx_parts_sum<R>(p + 64, lane);
             }
             const int t = lane & 15;
             if (t < rows) {
-                float* dst = a.out + (size_t)cur.part * a.part_stride + (size_t)(row0 + t) * a.C +
-                             ((size_t)cur.g * NBU + b) * 16 + 4 * (lane >> 4);
-                float4 o = make_float4(sa[0], sa[1], sa[2], sa[3]);
+                const size_t at = (size_t)(row0 + t) * a.C + ((size_t)cur.g * NBU + b) * 16 + 4 * (lane >> 4);
                 if (NMAT == 2) {
-                    o.x = o.x / (1.0f + __expf(-o.x)) * sb[0];
-                    o.y = o.y / (1.0f + __expf(-o.y)) * sb[1];
-                    o.z = o.z / (1.0f + __expf(-o.z)) * sb[2];
-                    o.w = o.w / (1.0f + __expf(-o.w)) * sb[3];
+                    float h[4];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) h[i] = sa[i] / (1.0f + __expf(-sa[i])) * sb[i];
+                    if (a.h_bf16)
+                        *(uint2*)((uint16_t*)a.out + at) = make_uint2(moe_pack_bf16x2(h[0], h[1]), moe_pack_bf16x2(h[2], h[3]));
+                    else
+                        *(float4*)(a.out + at) = make_float4(h[0], h[1], h[2], h[3]);
+                } else if (a.finish == FIN_NONE) {
+                    *(float4*)(a.out + at) = make_float4(sa[0], sa[1], sa[2], sa[3]);
+                } else {
+                    mx_store_shared(a.out + (size_t)cur.part * a.part_stride + at, sa);
                 }
-                *(float4*)dst = o;
             }
         }
-        cur = next;
+    };
+    for (unsigned u = u_begin; u < u_end; u += 2) {
+        process(std::integral_constant<int, 0>{}, u);
+        if (u + 1 < u_end) process(std::integral_constant<int, 1>{}, u + 1);
     }
     write_xg();
     if (!DOWN || a.finish == FIN_NONE) return;
 
-    // Publish the slabs, count the units, and finish the groups whose last unit this was.
-    __threadfence();
+    // The slabs' stores have arrived; count the units, and finish the groups whose last unit this was.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     const unsigned need = (unsigned)n_tiles * (unsigned)a.P;
     for (unsigned base = u_begin; base < u_end; base += 64) {
         if (wave == 0) {
             bool last = false;
             if (base + lane < u_end)
-                last = __hip_atomic_fetch_add(a.counters + (base + lane) % groups, 1u, __ATOMIC_ACQ_REL,
+                last = __hip_atomic_fetch_add(a.counters + (base + lane) % groups, 1u, __ATOMIC_RELAXED,
                                               __HIP_MEMORY_SCOPE_AGENT) + 1u == need;
             const unsigned long long m = __ballot(last);
             if (lane == 0) s_last = m;
         }
         __syncthreads();
         unsigned long long m = s_last;
-        __threadfence();
         while (m) {
             const int i = (int)__builtin_ctzll(m);
             m &= m - 1;
@@ -490,7 +543,7 @@ static MxSplit mx_split(int K, bool parts) {
 }
 
 bool moe_mx_stream_serves(int N, int E, int d, int f) {
-    if (mx_words(d) > MXS_MAX_WAVES || N / 8 + E > MXS_MAX_TILES) return false;
+    if (mx_words(d) > MXS_MAX_WAVES || N / rows_of(ROWS_F32) + E > MXS_MAX_TILES) return false;
     return (long long)MXS_MAX_TILES * mx_split(f, true).P * ((d > f ? d : f) / 16) < (1ll << 31);
 }
 
@@ -561,15 +614,13 @@ int moe_mx_stream_launch(const moe_weights* W, const void* x, moe_dtype_t act_dt
     a.counters = counters;
     a.n_counters = W->d / 16;  // a feature group is one block at least
     if (step) a.st = *step;
-    // rows per expert, at most: a token uses an expert once
-    const bool few = N / k <= 8;
+    // A bf16 result is rounded to 8 bits once more, so h is held in as many before it.
+    a.h_bf16 = step && step->y && step->y_dtype == MOE_BF16 && !step->yg;
     int rc;
     if (act_dtype == MOE_BF16)
-        rc = gate ? mx_stream_go<2, 2, ROWS_BF16, true>(a, s) : mx_stream_go<2, 2, ROWS_BF16, false>(a, s);
-    else if (few)
-        rc = gate ? mx_stream_go<2, 2, ROWS_SPLIT8, true>(a, s) : mx_stream_go<2, 2, ROWS_SPLIT8, false>(a, s);
+        rc = gate ? mx_stream_go<2, 1, ROWS_BF16, true>(a, s) : mx_stream_go<2, 1, ROWS_BF16, false>(a, s);
     else
-        rc = gate ? mx_stream_go<2, 1, ROWS_SPLIT16, true>(a, s) : mx_stream_go<2, 1, ROWS_SPLIT16, false>(a, s);
+        rc = gate ? mx_stream_go<2, 1, ROWS_F32, true>(a, s) : mx_stream_go<2, 1, ROWS_F32, false>(a, s);
     if (rc != MOE_OK) return rc;
     moe_record_mid_event(s);
 
@@ -584,5 +635,5 @@ int moe_mx_stream_launch(const moe_weights* W, const void* x, moe_dtype_t act_dt
     a.out = a.finish == FIN_NONE ? yg : slabs;
     a.part_stride = (size_t)N * W->d;
     a.yg = yg;
-    return few ? mx_stream_go<1, 4, ROWS_SPLIT8, false>(a, s) : mx_stream_go<1, 2, ROWS_SPLIT16, false>(a, s);
+    return a.h_bf16 ? mx_stream_go<1, 2, ROWS_BF16, false>(a, s) : mx_stream_go<1, 2, ROWS_F32, false>(a, s);
 }

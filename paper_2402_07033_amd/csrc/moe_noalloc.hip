@@ -60,7 +60,7 @@ int moe_expert_ffn_noalloc(const moe_weights_t* W, const void* xg, moe_dtype_t a
     hipStream_t s = (hipStream_t)stream;
     if (mx)
         return path == MOE_FFN_STREAM ? moe_mx_stream_launch(W, xg, act_dtype, nullptr, 1, offsets, N, ptr, yg, nullptr, s)
-                                      : moe_mx_gemm_launch(W, xg, act_dtype, nullptr, 1, offsets, N, ptr, yg, s);
+                                      : moe_mx_gemm_launch(W, xg, act_dtype, nullptr, 1, offsets, N, ptr, yg, true, nullptr, nullptr, s);
     if (W->dtype == MOE_F32) return moe_ffn_f32_launch(W, (const float*)xg, nullptr, 1, offsets, N, ptr, yg, s);
     if (path == MOE_FFN_STREAM)
         return moe_ffn_stream_launch(W, xg, act_dtype, nullptr, 1, offsets, N, ptr, yg, nullptr, s);

@@ -144,7 +144,10 @@ def test_grouped(d, f, E, N, how, dtype):
     x, x64 = rows(rng, N, d, dtype)
     offsets = split_rows(rng, N, E, how)
     yg = moe.moe_expert_ffn(W, x, cuda(offsets), path=moe.MOE_FFN_GROUPED)
-    want, bound = ref.ffn(x64, offsets, mats, 0.0 if dtype == BF16 else ref.ROUND, ref.ROUND)
+    # up to 72 rows of a result in fp32 nothing is rounded to bf16
+    exact = N <= 72
+    want, bound = ref.ffn(x64, offsets, mats, 0.0 if dtype == BF16 else (ref.SPLIT if exact else ref.ROUND),
+                          ref.SPLIT if exact else ref.ROUND)
     check(yg, want, bound, what=(d, f, E, N, how))
     W.free()
 
@@ -159,10 +162,9 @@ def test_rows_through_perm(T, k):
     logits = cuda(rng.standard_normal((T, 8)).astype(np.float32))
     idx, _ = moe.moe_route(logits, k)
     _, offsets, perm, _, xg = moe.moe_permute(idx, 8, x)
-    # (the gathered call is not told k, so it may take 16-row tiles where the other takes 8)
     a = moe.moe_expert_ffn(W, xg, offsets)
     b = moe.moe_expert_ffn_tokens(W, x, k, perm, offsets)
-    assert torch.equal(a, b) if T * k > 72 or T > 8 or T * k <= 8 else torch.allclose(a, b, rtol=0, atol=1e-4)
+    assert torch.equal(a, b)
     W.free()
 
 
@@ -184,10 +186,10 @@ def test_layer(T, d, f, E, k, xd, yd):
     if E > 4:
         logits[:, 1] = logits[:, 3]  # ties go to the lower index
         logits[:, E - 1] = -30.0     # an expert that nobody takes (unless k says so)
-    stream = T * k <= 72
+    exact = T * k <= 72 and yd == F32
     out = moe.moe_layer_mxfp4(W, x, cuda(logits), k, y=torch.empty((T, d), dtype=yd, device="cuda"))
-    u = 0.0 if xd == BF16 else (ref.SPLIT if stream else ref.ROUND)
-    want = ref.layer(x64, logits, mats, k, u, ref.SPLIT if stream else ref.ROUND)
+    u = 0.0 if xd == BF16 else (ref.SPLIT if exact else ref.ROUND)
+    want = ref.layer(x64, logits, mats, k, u, ref.SPLIT if exact else ref.ROUND)
     for n in ("idx", "counts", "offsets", "perm", "inv_perm"):
         assert np.array_equal(out[n].cpu().numpy(), want[n]), n
     assert np.max(np.abs(out["w"].cpu().numpy() - want["w"])) <= 2.0 ** -20
@@ -258,10 +260,10 @@ def test_stack(T, E, k, d, f):
         out = ref.layer(h, lg.astype(np.float32), mats, k, ref.SPLIT, ref.SPLIT)
         assert np.array_equal(idx[n].cpu().numpy(), out["idx"])
         want = want + out["y"]
-    # each block's bound is of the order 2^-15 of its rows; a later block sees the earlier ones' errors
+    # the norms and sums of a block are fp32 (K * 2^-24 at most, K up to 2048), in three blocks
     for got in (fused, apart):
         err = np.linalg.norm(got.cpu().numpy() - want) / np.linalg.norm(want)
-        assert err <= 3 * 3 * 2.0 ** -15, err
+        assert err <= 2.0 ** -15, err
     for W, *_ in layers:
         W.free()
 
@@ -344,6 +346,6 @@ def test_quantize_then_layer():
     logits = rng.standard_normal((T, E)).astype(np.float32)
     out = moe.moe_layer_mxfp4(W, x, cuda(logits), k)
     mats = [ref.dequantize(*ref.quantize(w)) for w in ws]
-    want = ref.layer(x64, logits, mats, k, 0.0, ref.SPLIT)
+    want = ref.layer(x64, logits, mats, k, 0.0, ref.ROUND)
     check(out["y"], want["y"], want["bound"], BF16)
     W.free()

@@ -18,9 +18,10 @@
 // v_mfma_f32_16x16x32_bf16, whose B operand is then x[row][32*(l/16) + 8j .. +7].  The products
 // of a matrix instruction may be summed in any order of the reduction, so both sides only have
 // to agree.  The scales of four consecutive fragments are one 32-bit word per lane.
-//   codes : [E][C/16][nmat][KS] fragments,     KS = ceil(K / 128) (indices past K: code 0)
+//   codes : [E][C/16][KS][nmat] fragments,      KS = ceil(K / 128) (indices past K: code 0)
 //   scales: [E][C/16][nmat][KW][64 lanes] u32, KW = ceil(KS / 4), byte s = fragment 4w + s
-// with nmat = 2 (w1, w3) for the first projection, 1 for the second.
+// with nmat = 2 (w1, w3) for the first projection, 1 for the second.  (w1 and w3 side by side: a wave
+// that reads both has one stream of addresses.)
 #define MX_BLOCK 32
 #define MX_FRAG_K 128
 

@@ -132,7 +132,7 @@ int moe_mx_dequantize_launch(const uint8_t* codes, const uint8_t* scales, int E,
     return moe_launch_status();
 }
 
-// codes [E][C][K/2] -> fragments [E][C/16][nmat][KS], this launch fills matrix slot `mat`.
+// codes [E][C][K/2] -> fragments [E][C/16][KS][nmat], this launch fills matrix slot `mat`.
 // One thread writes one 16-byte chunk; 16 lanes read 16 features' runs of 64 bytes.
 __global__ __launch_bounds__(256) void mx_pack_codes_kernel(const uint8_t* __restrict__ src, u32x4_t* __restrict__ dst,
                                                             int E, int K, int C, int nmat, int mat) {
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(256) void mx_pack_codes_kernel(const uint8_t* __res
         const size_t k0 = ks * MX_FRAG_K + MX_BLOCK * (lane >> 4);
         u32x4_t v = {0u, 0u, 0u, 0u};
         if (k0 < (size_t)K) v = *(const u32x4_t*)(src + c * (K / 2) + k0 / 2);
-        dst[((enb * nmat + mat) * KS + ks) * 64 + lane] = v;
+        dst[((enb * KS + ks) * nmat + mat) * 64 + lane] = v;
     }
 }
 

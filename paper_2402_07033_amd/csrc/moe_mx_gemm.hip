@@ -16,6 +16,8 @@
 //     sums, which the combine (or mx_sum_kernel) adds in part order.
 //   * T parts per row: a row of fp32 is three bf16 parts (all 24 bits) where fp32 results are held to
 //     that, else one.
+#include <type_traits>
+
 #include "moe_mx.h"
 #include "moe_frag_pack.h"
 
@@ -26,7 +28,12 @@
 #define MXG_NF 4   // fragment rows of a wave
 constexpr int mxg_blocks_max(int T) { return T == 3 ? 2 : 8; }  // RBM
 // steps requested ahead, in stages of LDS: 8 KiB .. 64 KiB a workgroup
-constexpr int mxg_depth(int T, int RB) { return RB * T >= 4 ? 1 : RB * T >= 2 ? 2 : 3; }
+#ifndef MXG_D1
+#define MXG_D1 3
+#define MXG_D2 2
+#define MXG_D4 1
+#endif
+constexpr int mxg_depth(int T, int RB) { return RB * T >= 5 ? 1 : RB * T >= 4 ? MXG_D4 : RB * T >= 2 ? MXG_D2 : MXG_D1; }
 constexpr int mxg_lds(int T) {
     int most = 0;
     for (int rb = 1; rb <= mxg_blocks_max(T); rb++) {
@@ -198,8 +205,9 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& 
         ks = ks < k_hi ? ks : k_hi - 1;  // (past the end: again, so that every step counts the same)
 #pragma unroll
         for (int r = 0; r < NF; r++) {
-            if (ti.once) q[slot][r] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, (r * a.KS + ks) * 1024, 2));
-            else q[slot][r] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, (r * a.KS + ks) * 1024, 0));
+            const int at = ((r / NMAT * a.KS + ks) * NMAT + r % NMAT) * 1024;
+            if (ti.once) q[slot][r] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, at, 2));
+            else q[slot][r] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, at, 0));
             sc[slot][r] = __builtin_amdgcn_raw_buffer_load_b32(rs, lane * 4, (r * a.KW + (ks >> 2)) * 256, 0);
         }
 #pragma unroll
@@ -217,35 +225,53 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& 
 #pragma unroll
         for (int b = 0; b < RB; b++) acc[r][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < D; i++) request(k_lo + i, i);
+    for (int i = 0; i < D; i++) {
+        request(k_lo + i, i);
+        asm volatile("" ::: "memory");  // (two steps' requests of one scale word stay two)
+    }
 
-    for (int k = k_lo; k < k_hi; k += NS) {
+    auto step = [&](int k, auto slot_, auto more_) __attribute__((always_inline)) {
+        constexpr int u = decltype(slot_)::value;
+        constexpr bool more = decltype(more_)::value;  // not one of the last D
+        // this step's requests have arrived, and every wave has read the stage that is refilled now
+        MXG_MEET(more ? (D - 1) * VREQ : 0);
+        if (more) request(k + D, (u + D) % NS);
+        const u32x4_t* st = (const u32x4_t*)(smem + u * STAGE) + lane;
 #pragma unroll
-        for (int u = 0; u < NS; u++) {
-            if (k + u >= k_hi) break;
-            // this step's requests have arrived, and every wave has read the stage that is refilled now
-            MXG_MEET((D - 1) * VREQ);
-            request(k + u + D, (u + D) % NS);
-            const u32x4_t* st = (const u32x4_t*)(smem + u * STAGE) + lane;
+        for (int j = 0; j < 4; j++) {
+            bf16x8_t x[RB][T];
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                bf16x8_t x[RB][T];
+            for (int b = 0; b < RB; b++)
+#pragma unroll
+                for (int t = 0; t < T; t++) x[b][t] = __builtin_bit_cast(bf16x8_t, st[((b * 4 + j) * T + t) * 64]);
+#pragma unroll
+            for (int r = 0; r < NF; r++) {
+                const bf16x8_t w = mx_widen8(q[u][r][j], mx_scale(sc[u][r] >> (8 * (k & 3)), 0));
 #pragma unroll
                 for (int b = 0; b < RB; b++)
 #pragma unroll
-                    for (int t = 0; t < T; t++) x[b][t] = __builtin_bit_cast(bf16x8_t, st[((b * 4 + j) * T + t) * 64]);
-#pragma unroll
-                for (int r = 0; r < NF; r++) {
-                    const bf16x8_t w = mx_widen8(q[u][r][j], mx_scale(sc[u][r] >> (8 * ((k + u) & 3)), 0));
-#pragma unroll
-                    for (int b = 0; b < RB; b++)
-#pragma unroll
-                        for (int t = 0; t < T; t++)
-                            acc[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[b][t], acc[r][b], 0, 0, 0);
-                }
+                    for (int t = 0; t < T; t++)
+                        acc[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[b][t], acc[r][b], 0, 0, 0);
             }
         }
+    };
+    // The loop has no way out between its steps: every wait for a step's operands would have to cover
+    // it.  The steps behind it request nothing: what nobody uses, the compiler leaves out, and the
+    // number of requests that a wait counts on would be another.
+    using std::integral_constant;
+    int k = k_lo;
+    for (; k + NS <= k_hi; k += NS) {
+        step(k, integral_constant<int, 0>{}, integral_constant<bool, true>{});
+        if constexpr (NS > 1) step(k + 1, integral_constant<int, 1>{}, integral_constant<bool, true>{});
+        if constexpr (NS > 2) step(k + 2, integral_constant<int, 2>{}, integral_constant<bool, true>{});
+        if constexpr (NS > 3) step(k + 3, integral_constant<int, 3>{}, integral_constant<bool, true>{});
+        if constexpr (NS > 4) step(k + 4, integral_constant<int, 4>{}, integral_constant<bool, true>{});
+        static_assert(NS <= 5, "steps of the ring");
     }
+    if (k < k_hi) step(k, integral_constant<int, 0>{}, integral_constant<bool, false>{});
+    if constexpr (NS > 2) if (k + 1 < k_hi) step(k + 1, integral_constant<int, 1>{}, integral_constant<bool, false>{});
+    if constexpr (NS > 3) if (k + 2 < k_hi) step(k + 2, integral_constant<int, 2>{}, integral_constant<bool, false>{});
+    if constexpr (NS > 4) if (k + 3 < k_hi) step(k + 3, integral_constant<int, 3>{}, integral_constant<bool, false>{});
     // no request for LDS outlives the workgroup
     __builtin_amdgcn_s_waitcnt(0x0070);
     if (idle) return;

@@ -1,19 +1,19 @@
 // Decode-sized expert FFN and layer over MXFP4 expert matrices for gfx950.
 //
 // A few rows per expert are bound by reading each active expert's matrices once, here 17/32
-// byte per weight.  The plan is that of the bf16 kernels (moe_ffn_stream.hip): a wave streams
-// fragments of 16 features by 128 reduction indices with 16-byte-per-lane loads, widens the
-// codes to bf16 in registers (exact, moe_mx.h), and multiplies them with the rows on
-// v_mfma_f32_16x16x32_bf16, fp32 accumulate; fp32 rows are split into three bf16 parts, which
-// hold all 24 bits.  The waves of a workgroup split the reduction, one scale word (four
-// fragments, 512 indices) each, and keep their slice of the rows in registers over all
-// consecutive units of the same rows; their partial tiles meet in LDS.
+// byte per weight.  A wave streams two rows of fragments (16 features by 128 reduction indices each)
+// with 16-byte-per-lane loads, 16 of them in flight, widens the codes to bf16 in registers (exact,
+// moe_mx.h), and multiplies them with the rows on v_mfma_f32_16x16x32_bf16, fp32 accumulate; fp32 rows
+// are split into three bf16 parts, which hold all 24 bits.  The rows' operands lie in LDS, one copy
+// for the workgroup's 16 waves, and a wave takes its features' whole reduction (or part of it), so
+// that the waves meet only where the rows change.  (With the reduction split over the waves, the
+// rows in registers and the sums joined in LDS behind every 64 KiB the first projection of 2 / 8
+// experts took 30.6 / 89 us, 8 of them in those joins.)
 //
-// A unit is (tile of rows of one expert, reduction part, group of NBU blocks of 16 features); the
-// units are dealt to the workgroups in contiguous, equal ranges, and the loads of two units are
-// in flight.
+// A unit is (tile of rows of one expert, reduction part, group of features): 16 columns of w1 and
+// w3, or 32 of w2.  The units are dealt to the workgroups in contiguous, equal ranges.
 //   up   (x.w1, x.w3 -> silu*mul -> h): one part.  Its prologue may route the tokens and batch
-//        them (up to 64 slots).  h is fp32, or bf16 where the result is.
+//        them (up to 64 slots).  h is left as three bf16 parts, or one where the result is bf16.
 //   down (h.w2): P parts.  Every unit leaves its partial sums in slab [part][N][d]; a counter
 //        per feature group tells the workgroup that finishes the group's last unit, and that
 //        one adds the parts in part order -- and the rows of a token in slot order, weighted,
@@ -27,8 +27,10 @@
 #include "moe_stream_wave.h"
 
 #define MXS_MAX_TILES 128
-#define MXS_MAX_WAVES 8
+#define MXS_WAVES 16
+#define MXS_MAX_WORDS 8  // scale words (512 indices each) of a part: 128 KiB of operands for 16 columns
 #define MXS_MAX_SLOTS 64
+#define MXS_DOWN_COLS 32  // features of a unit of the second projection
 
 struct MxArgs {
     const u32x4_t* wfrag;
@@ -37,92 +39,104 @@ struct MxArgs {
     const int32_t* row_perm;  // or null; else row i of the activations is act[row_perm[i] / row_k]
     int row_k;
     const int32_t* offsets;
-    float* out;               // up: h [N,C]; down: slabs [P][N][C], or yg (finish == FIN_NONE)
+    float* out;               // up: h [h_parts][N,C] bf16; down: slabs [P][N][C], or yg (finish == FIN_NONE)
     size_t part_stride;
     int E, N, K, C;
     int NB, KS, KW;           // 16-feature blocks, fragments and scale words of a reduction
-    int P, W;
+    int P;                    // reduction parts
+    int lds_operands;         // bytes of LDS for the rows' operands; the shared units' sums lie behind
     unsigned* counters;       // [n_counters], one per feature group of the second projection:
     int n_counters;           // cleared by up, counted by down
     int finish;
-    int h_bf16;               // up: h is bf16
+    int h_parts;              // up: bf16 parts of h, 1 or 3
     float* yg;                // FIN_ROWS: out
     MxStep st;
 };
 enum { FIN_NONE = 0, FIN_ROWS = 1, FIN_LAYER = 2 };
 
 // How a tile's rows become the matrix instructions' 16 operand columns.  An fp32 row is three
-// bf16 parts, and 5 rows have all their parts in one instruction (columns t, t + 5, t + 10, added
-// in the end).  More rows of an expert are more tiles: the registers that hold two operands a row
-// would not leave room for two units in flight.
-enum { ROWS_BF16 = 0, ROWS_F32 = 1 };
+// bf16 parts, and 5 rows have all their parts in one instruction (column part * rows + row), which
+// are added in the end.  More rows of an expert are more tiles.  h comes as its parts, [3][N][f],
+// already.
+enum { ROWS_BF16 = 0, ROWS_F32 = 1, ROWS_PARTS = 2 };
 constexpr int rows_of(int R) { return R == ROWS_BF16 ? 16 : 5; }
+constexpr int parts_of(int R) { return R == ROWS_BF16 ? 1 : 3; }
 
-// The wave's slice of the rows: four fragments' worth of reduction indices from fragment ks0.
+// Stages the rows [row0, row0 + rows) of reduction words [w0, w1) as operands, 16-byte chunks
+// [(word, fragment, j, lane / 16)][column]: indices word*512 + fragment*128 + 32*(lane/16) + 8j .. +7.
+// First the requests (up to four chunks a thread), then the operands; chunks beyond are done in turn.
 template <int R>
-__device__ __forceinline__ void mx_load_act(bf16x8_t (&act)[4][4], const void* actp, int K, int row0, int rows,
-                                            int ks0, int lane, const int* rowmap, const int32_t* perm, int perm_k,
-                                            const float* row_scale) {
-#pragma clang fp contract(off)
-    const int c = lane & 15, kq = lane >> 4;
-    const int t = R == ROWS_BF16 ? c : c % rows_of(R), part = R == ROWS_BF16 ? 0 : c / rows_of(R);
-    const bool used = t < rows && part < 3;
-    int src_row = row0 + t;
-    if (rowmap && used) src_row = rowmap[row0 + t];
-    if (perm && used) src_row = perm[row0 + t] / perm_k;
-    float sc = 1.0f;
-    if (R != ROWS_BF16 && row_scale && used) sc = row_scale[src_row];
-#pragma unroll
-    for (int s = 0; s < 4; s++) {
-        const int k0 = (ks0 + s) * MX_FRAG_K + kq * MX_BLOCK;
-        const bool live = used && k0 < K;
-        const size_t off = (size_t)src_row * K + k0;
-        if (R == ROWS_BF16) {
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                u32x4_t v = {0u, 0u, 0u, 0u};
-                if (live) v = *(const u32x4_t*)((const uint16_t*)actp + off + 8 * j);
-                act[s][j] = __builtin_bit_cast(bf16x8_t, v);
-            }
-            continue;
-        }
-        f32x4_t x[8];
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            x[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            if (live) x[j] = *(const f32x4_t*)((const float*)actp + off + 4 * j);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            // the scaled row is rounded to fp32 before the split, as if it had been stored
-            bf16x8_t a;
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float v = x[2 * j + i / 4][i % 4] * sc;
-                const __bf16 hi = (__bf16)v;
-                const float r = v - (float)hi;
-                const __bf16 mid = (__bf16)r, lo = (__bf16)(r - (float)mid);
-                a[i] = part == 0 ? hi : part == 1 ? mid : lo;
-            }
-            act[s][j] = a;
-        }
-        // (the requests of more fragments at once would not fit in registers)
-        if (s & 1) __builtin_amdgcn_sched_barrier(0);
+struct MxStage {
+    u32x4_t raw[4][R == ROWS_F32 ? 2 : 1];
+    float sc[4];
+};
+template <int R>
+struct MxStager {
+    const MxArgs& a;
+    const int* rowmap;
+    const float* row_scale;
+    int row0, rows, w0, chunks;  // chunks: 16-byte chunks of one row (fp32: of one part of it)
+    __device__ __forceinline__ MxStager(const MxArgs& args, const int* rm, const float* rs, int r0, int nr, int wa, int wb)
+        : a(args), rowmap(rm), row_scale(rs), row0(r0), rows(nr), w0(wa), chunks((wb - wa) * 64) {}
+    // item -> (row or part row, chunk of it); consecutive threads take consecutive chunks of a row
+    __device__ __forceinline__ int items() const { return chunks * rows * (R == ROWS_PARTS ? 3 : 1); }
+    __device__ __forceinline__ void request(int item, u32x4_t (&raw)[R == ROWS_F32 ? 2 : 1], float& sc) const {
+        const int rr = item / chunks, c = item % chunks;
+        const int t = rr % rows, part = rr / rows;
+        int src = row0 + t;
+        if (rowmap) src = rowmap[src];
+        else if (a.row_perm) src = a.row_perm[src] / a.row_k;
+        sc = R == ROWS_F32 && row_scale ? row_scale[src] : 1.0f;
+        if (R == ROWS_PARTS) src += part * a.N;
+        const int k0 = w0 * 512 + c * 8;
+        raw[0] = u32x4_t{0u, 0u, 0u, 0u};
+        if (R == ROWS_F32) raw[R == ROWS_F32 ? 1 : 0] = u32x4_t{0u, 0u, 0u, 0u};
+        if (k0 >= a.K) return;
+        const char* p = (const char*)a.act + ((size_t)src * a.K + k0) * (R == ROWS_F32 ? 4 : 2);
+        raw[0] = *(const u32x4_t*)p;
+        if (R == ROWS_F32) raw[R == ROWS_F32 ? 1 : 0] = *(const u32x4_t*)(p + 16);
     }
-}
+    __device__ __forceinline__ void put(int item, const u32x4_t (&raw)[R == ROWS_F32 ? 2 : 1], float sc, u32x4_t* s_b) const {
+#pragma clang fp contract(off)
+        const int nc = rows * parts_of(R);
+        const int rr = item / chunks, c = item % chunks;
+        // c counts 8-index groups along the reduction: fragment c / 16, lane group c / 4 % 4, j c % 4
+        u32x4_t* dst = s_b + (size_t)((c & ~15) + (c & 3) * 4 + ((c >> 2) & 3)) * nc + rr;
+        if (R != ROWS_F32) {
+            *dst = raw[0];
+            return;
+        }
+        bf16x8_t o[3];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            // the scaled row is rounded to fp32 before the split, as if it had been stored
+            const float v = __uint_as_float(raw[R == ROWS_F32 ? i / 4 : 0][i % 4]) * sc;
+            o[0][i] = (__bf16)v;
+            const float r = v - (float)o[0][i];
+            o[1][i] = (__bf16)r;
+            o[2][i] = (__bf16)(r - (float)o[1][i]);
+        }
+#pragma unroll
+        for (int p = 0; p < 3; p++) dst[p * rows] = __builtin_bit_cast(u32x4_t, o[p]);
+    }
+};
 
-// Sum of one wave's partial tile over the columns of a row's parts, for lanes of columns < rows.
+// Sum of an accumulator over the columns of a row's parts, for lanes of columns < rows.
 template <int R>
-__device__ __forceinline__ f32x4_t mx_parts_sum(const f32x4_t* p, int lane) {
-    if (R == ROWS_BF16) return p[lane];
-    const int at = (lane & 48) + (lane & 15) % rows_of(R);
-    return p[at] + p[at + 5] + p[at + 10];
+__device__ __forceinline__ f32x4_t mx_parts_sum(const f32x4_t& v, int rows, int lane) {
+    if (R == ROWS_BF16) return v;
+    f32x4_t o = v;
+#pragma unroll
+    for (int p = 1; p < 3; p++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) o[i] += __shfl(v[i], (lane & 48) + ((lane + p * rows) & 15), 64);
+    return o;
 }
 
 // Slabs are written by one workgroup and read by another of the same launch, maybe on another XCD,
 // whose L2 is another: both sides go past the caches that the other does not share, so that
 // neither has to write back or drop a whole cache (device fences by every wave made the second
-// projection of one token 72 us long instead of 21).
+// projection of one token 72 us long instead of 28).
 __device__ __forceinline__ void mx_store_shared(float* p, const f32x4_t& v) {
     typedef float f2 __attribute__((ext_vector_type(2)));
     __hip_atomic_store((unsigned long long*)p, __builtin_bit_cast(unsigned long long, f2{v[0], v[1]}), __ATOMIC_RELAXED,
@@ -216,120 +230,119 @@ __device__ __forceinline__ void mx_route(const float* logits, const MxStep& st, 
     }
 }
 
-// The group's rows are complete: add the parts, and what the step asks for beyond them.
-template <int NBU>
-__device__ void mx_finish(const MxArgs& a, int g, int tid, int threads, float* s_x) {
-    constexpr int C4 = NBU * 4;  // float4 columns of the group
-    const size_t col0 = (size_t)g * NBU * 16;
-    auto row_sum = [&](int row, int c4) -> float4 {
-        const float* p = a.out + (size_t)row * a.C + col0 + 4 * c4;
-        f32x4_t v = mx_load_shared(p);
-        for (int q = 1; q < a.P; q += 4) {  // four requests at a time, added in order
-            f32x4_t u[4];
+// The groups of `mask` (bit i: group (g0 + i) % groups) are complete: add the parts, and what the
+// step asks for beyond them.  All of them at once: one after the other, each waiting for its own
+// slabs, the last workgroup of an 8-expert step took 12 us.
+__device__ __forceinline__ f32x4_t mx_row_sum(const MxArgs& a, int row, size_t col) {
+    const float* p = a.out + (size_t)row * a.C + col;
+    f32x4_t v = mx_load_shared(p);
+    for (int q = 1; q < a.P; q += 4) {  // four requests at a time, added in order
+        f32x4_t u[4];
 #pragma unroll
-            for (int i = 0; i < 4; i++)
-                if (q + i < a.P) u[i] = mx_load_shared(p + (size_t)(q + i) * a.part_stride);
+        for (int i = 0; i < 4; i++)
+            if (q + i < a.P) u[i] = mx_load_shared(p + (size_t)(q + i) * a.part_stride);
 #pragma unroll
-            for (int i = 0; i < 4; i++)
-                if (q + i < a.P) v += u[i];
-        }
-        return make_float4(v[0], v[1], v[2], v[3]);
-    };
+        for (int i = 0; i < 4; i++)
+            if (q + i < a.P) v += u[i];
+    }
+    return v;
+}
+
+__device__ __forceinline__ void mx_finish(const MxArgs& a, const int* s_group, int n, int tid, float* s_x) {
+    constexpr int C4 = MXS_DOWN_COLS / 4;  // 16-byte columns of a group
     if (a.finish == FIN_ROWS) {
-        for (int i = tid; i < a.N * C4; i += threads) {
-            const int row = i / C4, c4 = i % C4;
-            *(float4*)(a.yg + (size_t)row * a.C + col0 + 4 * c4) = row_sum(row, c4);
+        for (int i = tid; i < n * a.N * C4; i += 64 * MXS_WAVES) {
+            const int c4 = i % C4, row = i / C4 % a.N;
+            const size_t col = (size_t)s_group[i / C4 / a.N] * MXS_DOWN_COLS + 4 * c4;
+            const f32x4_t v = mx_row_sum(a, row, col);
+            *(f32x4_t*)(a.yg + (size_t)row * a.C + col) = v;
         }
         return;
     }
     const MxStep& st = a.st;
     const int T = a.N / st.k;
-    for (int i = tid; i < T * C4; i += threads) {
-        const int t = i / C4, c4 = i % C4;
-        const size_t at = (size_t)t * a.C + col0 + 4 * c4;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = tid; i < n * T * C4; i += 64 * MXS_WAVES) {
+        const int c4 = i % C4, t = i / C4 % T;
+        const size_t col = (size_t)s_group[i / C4 / T] * MXS_DOWN_COLS + 4 * c4;
+        const size_t at = (size_t)t * a.C + col;
+        f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
         for (int j = 0; j < st.k; j++) {
             const float w = st.weights[t * st.k + j];
             int row = st.inv_perm[t * st.k + j];
             row = row < 0 ? 0 : (row >= a.N ? a.N - 1 : row);
-            const float4 v = row_sum(row, c4);
-            if (st.yg) *(float4*)(st.yg + (size_t)row * a.C + col0 + 4 * c4) = v;
-            acc.x += w * v.x;
-            acc.y += w * v.y;
-            acc.z += w * v.z;
-            acc.w += w * v.w;
+            const f32x4_t v = mx_row_sum(a, row, col);
+            if (st.yg) *(f32x4_t*)(st.yg + (size_t)row * a.C + col) = v;
+            acc += w * v;
         }
-        if (st.x_in) {
-            float4 xr = *(const float4*)(st.x_in + at);
-            xr.x += acc.x; xr.y += acc.y; xr.z += acc.z; xr.w += acc.w;
-            acc = xr;
-        }
+        if (st.x_in) acc = *(const f32x4_t*)(st.x_in + at) + acc;
         if (st.y_dtype == MOE_BF16)
-            *(uint2*)((uint16_t*)st.y + at) = make_uint2(moe_pack_bf16x2(acc.x, acc.y), moe_pack_bf16x2(acc.z, acc.w));
+            *(uint2*)((uint16_t*)st.y + at) = make_uint2(moe_pack_bf16x2(acc[0], acc[1]), moe_pack_bf16x2(acc[2], acc[3]));
         else
-            *(float4*)((float*)st.y + at) = acc;
-        if (st.w_gate_next) *(float4*)(s_x + t * NBU * 16 + 4 * c4) = acc;
+            *(f32x4_t*)((float*)st.y + at) = acc;
+        if (st.w_gate_next) *(f32x4_t*)(s_x + (size_t)i * 4) = acc;
     }
     if (!st.w_gate_next) return;
     __syncthreads();
-    // the 16 features' shares of the next block's gating sums
+    // shares of the next block's gating sums, 16 features each
     const int items = T * (a.E + 1);
-    for (int i = tid; i < NBU * items; i += threads) {
-        const int b = i / items, it = i % items;
+    for (int i = tid; i < n * (MXS_DOWN_COLS / 16) * items; i += 64 * MXS_WAVES) {
+        const int it = i % items, b = i / items;  // b: 16 features of the list
         const int t = it / (a.E + 1), ex = it % (a.E + 1);
-        const float* xs = s_x + t * NBU * 16 + b * 16;
-        const float* wg = st.w_gate_next + (col0 + 16 * b) * a.E + ex;
+        const int gi = b / (MXS_DOWN_COLS / 16);
+        const size_t share = (size_t)s_group[gi] * (MXS_DOWN_COLS / 16) + b % (MXS_DOWN_COLS / 16);
+        const float* xs = s_x + ((size_t)gi * T + t) * MXS_DOWN_COLS + b % (MXS_DOWN_COLS / 16) * 16;
+        const float* wg = st.w_gate_next + share * 16 * a.E + ex;
+        float w[16];
+#pragma unroll
+        for (int c = 0; c < 16; c++) w[c] = ex == a.E ? xs[c] : wg[(size_t)c * a.E];
         float v = 0.f;
 #pragma unroll
-        for (int c = 0; c < 16; c++) v = fmaf(xs[c], ex == a.E ? xs[c] : wg[(size_t)c * a.E], v);
-        st.sums_next[((size_t)g * NBU + b) * st.gate_stride + it] = v;
+        for (int c = 0; c < 16; c++) v = fmaf(xs[c], w[c], v);
+        st.sums_next[share * st.gate_stride + it] = v;
     }
-    __syncthreads();  // s_x serves the next group
+    __syncthreads();  // s_x serves the next groups
 }
 
-template <int NMAT, int NBU, int R, bool GATE>
-__global__ __launch_bounds__(64 * MXS_MAX_WAVES) void mx_stream_kernel(MxArgs a) {
-    constexpr bool DOWN = NMAT == 1;
-    constexpr int NF = NMAT * NBU;  // fragment rows of a unit
+template <bool DOWN, int R, bool GATE>
+__global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
     extern __shared__ __align__(16) unsigned char s_raw[];
-    f32x4_t* s_red = (f32x4_t*)s_raw;  // [2][W][NF][64]
-    __shared__ int s_tiles[MXS_MAX_WAVES][3][MXS_MAX_TILES];
+    u32x4_t* s_b = (u32x4_t*)s_raw;  // operands of the rows at hand, see MxStager
+    __shared__ u32x4_t s_zero;       // ... of the columns that no row has
+    __shared__ int s_tiles[3][MXS_MAX_TILES], s_ntiles;
     __shared__ int s_idx[GATE ? MXS_MAX_SLOTS : 1];
     __shared__ float s_top[GATE ? MXS_MAX_SLOTS : 1];
-    __shared__ int s_batch[GATE ? MXS_MAX_WAVES : 1][3][MXS_MAX_SLOTS];
+    __shared__ int s_batch[GATE ? 3 : 1][MXS_MAX_SLOTS];
     __shared__ float s_gate[GATE ? 3 : 1][64];  // the summed shares, 1/rms per token, the logits
-    __shared__ float s_gpart[GATE ? MXS_MAX_WAVES : 1][GS_MAX_ITEMS];
-    __shared__ unsigned long long s_last;
+    __shared__ float s_gpart[GATE ? MXS_WAVES : 1][GS_MAX_ITEMS];
+    __shared__ int s_group[64], s_nlast;
 
-    const int tid = threadIdx.x, lane = tid & 63, threads = blockDim.x;
+    constexpr int THREADS = 64 * MXS_WAVES;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int* s_te = s_tiles[wave][0];
-    int* s_tr0 = s_tiles[wave][1];
-    int* s_trn = s_tiles[wave][2];
 
     if (!DOWN)
-        for (int i = blockIdx.x * threads + tid; i < a.n_counters; i += gridDim.x * threads) a.counters[i] = 0u;
+        for (int i = blockIdx.x * THREADS + tid; i < a.n_counters; i += gridDim.x * THREADS) a.counters[i] = 0u;
+    if (tid == 0) s_zero = u32x4_t{0u, 0u, 0u, 0u};
 
-    int lo = 0, hi = 0;
     const int* rowmap = nullptr;
     const float* row_scale = nullptr;
     if (GATE) {
         const MxStep& st = a.st;
         const float* lg = st.logits;
         if (st.gate_sums) {
-            // every wave adds its part of the shares, then every wave the parts, in wave order
+            // every wave adds its part of the shares, then one the parts, in wave order
             const int items = st.T * (a.E + 1);
-            const int per_w = (st.n_shares + a.W - 1) / a.W;
+            const int per_w = (st.n_shares + MXS_WAVES - 1) / MXS_WAVES;
             const int row0 = wave * per_w;
             const int row1 = (row0 + per_w) < st.n_shares ? (row0 + per_w) : st.n_shares;
-            if (lane < items) s_gpart[wave][lane] = 0.f;
-            float* s_rows = (float*)s_red + wave * (GS_WAVE_ROWS * GS_MAX_ITEMS);
-            gate_add_shares(st.gate_sums, row0, row1, st.gate_stride, items, lane, s_rows, s_gpart[wave]);
+            gate_add_shares(st.gate_sums, row0, row1, st.gate_stride, items, lane,
+                            (float*)s_raw + wave * (GS_WAVE_ROWS * GS_MAX_ITEMS), s_gpart[wave]);
             __syncthreads();
             if (wave == 0) {
                 if (lane < items) {
                     float v = s_gpart[0][lane];
-                    for (int w = 1; w < a.W; w++) v += s_gpart[w][lane];
+#pragma unroll
+                    for (int w = 1; w < MXS_WAVES; w++) v += s_gpart[w][lane];
                     s_gate[0][lane] = v;
                 }
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -348,32 +361,38 @@ __global__ __launch_bounds__(64 * MXS_MAX_WAVES) void mx_stream_kernel(MxArgs a)
             lg = s_gate[2];
             row_scale = s_gate[1];
         }
-        mx_route(lg, st, a.E, wave, a.W, lane, s_idx, s_top, blockIdx.x == 0);
+        mx_route(lg, st, a.E, wave, MXS_WAVES, lane, s_idx, s_top, blockIdx.x == 0);
         __syncthreads();
-        int cnt;
-        int* s_pos = s_batch[wave][0];
-        int* s_src = s_batch[wave][1];
-        mx_batch_wave(s_idx, a.N, a.E, lane, blockIdx.x == 0 && wave == 0, st, s_pos, s_batch[wave][2], lo, cnt);
-        if (lane < a.N) s_src[s_pos[lane]] = lane / st.k;
-        hi = lo + cnt;
-        rowmap = s_src;
-    } else if (lane < a.E) {
-        lo = a.offsets[lane];
-        hi = a.offsets[lane + 1];
+        rowmap = s_batch[1];
     }
+    if (wave == 0) {
+        int lo = 0, hi = 0;
+        if (GATE) {
+            int cnt;
+            mx_batch_wave(s_idx, a.N, a.E, lane, blockIdx.x == 0, a.st, s_batch[0], s_batch[2], lo, cnt);
+            if (lane < a.N) s_batch[1][s_batch[0][lane]] = lane / a.st.k;
+            hi = lo + cnt;
+        } else if (lane < a.E) {
+            lo = a.offsets[lane];
+            hi = a.offsets[lane + 1];
+        }
+        const int n = stream_tile_list<rows_of(R), MXS_MAX_TILES>(lo, hi, a.E, a.N, lane, s_tiles[0], s_tiles[1], s_tiles[2]);
+        if (lane == 0) s_ntiles = n;
+    }
+    __syncthreads();
     auto write_xg = [&]() {
         if (GATE && a.st.xg) {
             const int chunks = a.K / (R == ROWS_BF16 ? 8 : 4);
             for (int i = blockIdx.x; i < a.N; i += gridDim.x) {
                 const u32x4_t* src = (const u32x4_t*)a.act + (size_t)rowmap[i] * chunks;
                 u32x4_t* dst = (u32x4_t*)a.st.xg + (size_t)i * chunks;
-                for (int c = tid; c < chunks; c += threads) dst[c] = src[c];
+                for (int c = tid; c < chunks; c += THREADS) dst[c] = src[c];
             }
         }
     };
-    const int n_tiles = stream_tile_list<rows_of(R), MXS_MAX_TILES>(lo, hi, a.E, a.N, lane, s_te, s_tr0, s_trn);
-    const unsigned groups = (unsigned)(a.NB / NBU);
-    const unsigned total = (unsigned)n_tiles * (unsigned)a.P * groups;  // < 2^31 (host check)
+    const unsigned n_tiles = (unsigned)__builtin_amdgcn_readfirstlane(s_ntiles);
+    const unsigned groups = (unsigned)(DOWN ? a.NB / 2 : a.NB);
+    const unsigned total = n_tiles * (unsigned)a.P * groups;  // < 2^31 (host check)
     const unsigned per = total / gridDim.x, rem = total % gridDim.x;
     const unsigned u_begin = per * blockIdx.x + rem * blockIdx.x / gridDim.x;
     const unsigned u_end = per * (blockIdx.x + 1) + rem * (blockIdx.x + 1) / gridDim.x;
@@ -382,113 +401,194 @@ __global__ __launch_bounds__(64 * MXS_MAX_WAVES) void mx_stream_kernel(MxArgs a)
         return;
     }
 
-    struct Unit {
-        int tile, part, g, word;
-        size_t row;  // fragment row (e, nb, mat) of the unit's first fragment
+    // With so few units that each can have `share` waves, these share its words (behind one another
+    // they would be as many trips to memory): units u_begin + wave / share.
+    const unsigned most = (total + gridDim.x - 1) / gridDim.x;
+    const int share = most * 4 <= MXS_WAVES && a.KW / a.P >= 4 ? 4 : most * 2 <= MXS_WAVES && a.KW / a.P >= 2 ? 2 : 1;
+    const int sub = wave % share;
+    const unsigned u_wave = u_begin + wave / share, u_step = MXS_WAVES / share;
+
+    // A wave's work is one sequence of words: those of its first unit, of the unit u_step further, ...
+    // Word i is in register slot i % 2, and word i + 2 is requested when it has been used.
+    struct Item {
+        unsigned u, seg;  // unit (>= u_end: none), and its tile and part
+        int g, row0, rows, word, w0, wend, part;  // w0: the part's first word, wend: past this wave's last
+        const u32x4_t* p;   // the word's first fragment
+        const unsigned* q;  // its scales
     };
-    auto unit_of = [&](unsigned u) -> Unit {
-        Unit n;
-        n.g = (int)(u % groups);
-        const unsigned tp = u / groups;
-        n.part = (int)(tp % (unsigned)a.P);
-        n.tile = (int)(tp / (unsigned)a.P);
-        n.word = n.part * a.W + wave;
-        n.row = ((size_t)s_te[n.tile] * a.NB + (size_t)n.g * NBU) * NMAT;
+    constexpr int FSTEP = DOWN ? 64 : 128;  // w1 and w3 lie fragment by fragment side by side, w2's blocks one after the other
+    auto first_word = [&](unsigned u) __attribute__((always_inline)) -> Item {
+        Item n;
+        n.u = u;
+        n.seg = u / groups;
+        const unsigned tile = n.seg / (unsigned)a.P;
+        n.g = (int)(u - n.seg * groups);
+        n.part = (int)(n.seg - tile * (unsigned)a.P);
+        n.row0 = __builtin_amdgcn_readfirstlane(s_tiles[1][tile]);
+        n.rows = __builtin_amdgcn_readfirstlane(s_tiles[2][tile]);
+        n.w0 = n.part * a.KW / a.P;
+        const int words = (n.part + 1) * a.KW / a.P - n.w0;
+        n.word = n.w0 + sub * words / share;
+        n.wend = n.w0 + (sub + 1) * words / share;
+        const size_t frow = ((size_t)__builtin_amdgcn_readfirstlane(s_tiles[0][tile]) * groups + (size_t)n.g) * 2;
+        n.p = a.wfrag + frow * a.KS * 64 + (size_t)n.word * (4 * FSTEP);
+        n.q = a.wscale + (frow * a.KW + n.word) * 64;
         return n;
     };
-    // Fragments and words past the reduction's end (a wave whose share is short) are read as the
-    // last one again: their rows' operands are zero.
-    auto ld = [&](const Unit& n, int i) -> u32x4_t {
-        int ks = n.word * 4 + (i & 3);
-        ks = ks < a.KS ? ks : a.KS - 1;
-        return __builtin_nontemporal_load(a.wfrag + ((n.row + (i >> 2)) * a.KS + ks) * 64 + lane);
-    };
-    auto ld_scale = [&](const Unit& n, int r) -> unsigned {
-        const int w = n.word < a.KW ? n.word : a.KW - 1;
-        return __builtin_nontemporal_load(a.wscale + ((n.row + r) * a.KW + w) * 64 + lane);
-    };
-
-    Unit unit[2];
-    u32x4_t buf[2][NF][4];
-    unsigned sc[2][NF];
-    auto request = [&](int st, int r) __attribute__((always_inline)) {
-        sc[st][r] = ld_scale(unit[st], r);
-#pragma unroll
-        for (int s = 0; s < 4; s++) buf[st][r][s] = ld(unit[st], r * 4 + s);
-    };
-    unit[0] = unit_of(u_begin);
-#pragma unroll
-    for (int r = 0; r < NF; r++) request(0, r);
-    unit[1] = unit_of(u_begin + 1 < u_end ? u_begin + 1 : u_begin);
-    if (u_begin + 1 < u_end) {
-#pragma unroll
-        for (int r = 0; r < NF; r++) request(1, r);
-    }
-
-    bf16x8_t act[4][4];
-    int cur_tile = -1, cur_part = -1;
-    // unit u, whose loads are in stage st, and the requests of unit u + 2
-    auto process = [&](auto stage, unsigned u) __attribute__((always_inline)) {
-        constexpr int st = decltype(stage)::value;
-        const Unit cur = unit[st];
-        const int row0 = s_tr0[cur.tile], rows = s_trn[cur.tile];
-        if (cur.tile != cur_tile || cur.part != cur_part) {
-            mx_load_act<R>(act, a.act, a.K, row0, rows, cur.word * 4, lane, rowmap, a.row_perm, a.row_k, row_scale);
-            cur_tile = cur.tile;
-            cur_part = cur.part;
+    auto next_word = [&](const Item& c) __attribute__((always_inline)) -> Item {
+        Item n = c;
+        if (c.word + 1 < c.wend) {
+            n.word++;
+            n.p += 4 * FSTEP;
+            n.q += 64;
+        } else if (c.u + u_step < u_end) {
+            return first_word(c.u + u_step);
+        } else {
+            n.u = u_end;
         }
-        const bool more = u + 2 < u_end;
-        if (more) unit[st] = unit_of(u + 2);
-        const int phase = (int)(u - u_begin);  // of the turns and of the two halves of s_red: its parity is st
-        f32x4_t* red = s_red + (size_t)(st * a.W + wave) * NF * 64;
+        return n;
+    };
+    u32x4_t buf[2][2][4];
+    unsigned sc[2][2];
+    // Fragments past the reduction's end are read as the last one again: their operands are zero.  Behind
+    // the last word one line of it is read again: a request that may not be made would have every wait
+    // for the other slot wait for both.
+    auto request = [&](const Item& n, int slot) __attribute__((always_inline)) {
+        const bool none = n.u >= u_end;
+        const int last = none ? 0 : a.KS - 1 - n.word * 4;
+        const size_t row = none ? 0 : DOWN ? (size_t)a.KS * 64 : 64, srow = none ? 0 : (size_t)a.KW * 64;
 #pragma unroll
-        for (int r = 0; r < NF; r++) {
-            f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+        for (int r = 0; r < 2; r++) {
+            sc[slot][r] = __builtin_nontemporal_load(n.q + r * srow + lane);
 #pragma unroll
-            for (int s = 0; s < 4; s++) {
-                const u32x4_t q = buf[st][r][s];
-                const float scale = mx_scale(sc[st][r], s);
+            for (int s = 0; s < 4; s++)
+                buf[slot][r][s] = __builtin_nontemporal_load(n.p + r * row + (s < last ? s : last) * FSTEP + lane);
+        }
+    };
+
+    // Rows first, weights behind them (requests are answered in order, and the first burst of weights
+    // takes microseconds), then the rows' operands into LDS.
+    unsigned seg = u_begin / groups;
+    auto rows_at = [&](unsigned sg) __attribute__((always_inline)) -> MxStager<R> {
+        const unsigned tile = sg / (unsigned)a.P;
+        const int part = (int)(sg - tile * (unsigned)a.P);
+        return MxStager<R>(a, rowmap, row_scale, __builtin_amdgcn_readfirstlane(s_tiles[1][tile]),
+                           __builtin_amdgcn_readfirstlane(s_tiles[2][tile]), part * a.KW / a.P, (part + 1) * a.KW / a.P);
+    };
+    Item item[2];
+    {
+        const MxStager<R> stager = rows_at(seg);
+        MxStage<R> m;
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx_widen8(q[j], scale), act[s][j], acc, 0, 0, 0);
-                }
-            }
-            if (more) request(st, r);
-            red[r * 64 + lane] = acc;
+        for (int i = 0; i < 4; i++)
+            if (tid + i * THREADS < stager.items()) stager.request(tid + i * THREADS, m.raw[i], m.sc[i]);
+        __builtin_amdgcn_sched_barrier(0);
+        item[0].u = u_end;
+        if (u_wave < u_end) {
+            item[0] = first_word(u_wave);
+            request(item[0], 0);
+            item[1] = next_word(item[0]);
+            request(item[1], 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (tid + i * THREADS < stager.items()) stager.put(tid + i * THREADS, m.raw[i], m.sc[i], s_b);
+        for (int it = tid + 4 * THREADS; it < stager.items(); it += THREADS) {
+            stager.request(it, m.raw[0], m.sc[0]);
+            stager.put(it, m.raw[0], m.sc[0], s_b);
+        }
+    }
+    __syncthreads();
+    const unsigned seg_end = (u_end - 1) / groups;
+    auto next_rows = [&]() __attribute__((always_inline)) {  // by all waves alike
+        const MxStager<R> stager = rows_at(++seg);
+        __syncthreads();
+        for (int it = tid; it < stager.items(); it += THREADS) {
+            u32x4_t raw[R == ROWS_F32 ? 2 : 1];
+            float s1;
+            stager.request(it, raw, s1);
+            stager.put(it, raw, s1, s_b);
         }
         __syncthreads();
-        // the waves take turns at the blocks' sums
+    };
+
+    f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    // a unit's sums are complete: h, yg or the part's slab
+    auto store = [&](const Item& cur) __attribute__((always_inline)) {
+        const f32x4_t sa = mx_parts_sum<R>(acc[0], cur.rows, lane), sb = mx_parts_sum<R>(acc[1], cur.rows, lane);
+        const int col = lane & 15, kq = lane >> 4;
+        if (col >= cur.rows) return;
+        const size_t at = (size_t)(cur.row0 + col) * a.C + (size_t)cur.g * (DOWN ? 32 : 16) + 4 * kq;
+        if (!DOWN) {
+            float h[4];
 #pragma unroll
-        for (int b = 0; b < NBU; b++) {
-            if (wave != (phase * NBU + b) % a.W) continue;
-            f32x4_t sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
-            for (int w = 0; w < a.W; w++) {
-                const f32x4_t* p = s_red + (size_t)(st * a.W + w) * NF * 64 + b * NMAT * 64;
-                sa += mx_parts_sum<R>(p, lane);
-                if (NMAT == 2) sb += mx_parts_sum<R>(p + 64, lane);
+            for (int i = 0; i < 4; i++) h[i] = sa[i] / (1.0f + __expf(-sa[i])) * sb[i];
+            for (int p = 0; p < a.h_parts; p++) {
+                *(uint2*)((uint16_t*)a.out + (size_t)p * a.N * a.C + at) =
+                    make_uint2(moe_pack_bf16x2(h[0], h[1]), moe_pack_bf16x2(h[2], h[3]));
+#pragma unroll
+                for (int i = 0; i < 4; i++) h[i] -= moe_bf16_to_f32(moe_bf16_rne(h[i]));
             }
-            const int t = lane & 15;
-            if (t < rows) {
-                const size_t at = (size_t)(row0 + t) * a.C + ((size_t)cur.g * NBU + b) * 16 + 4 * (lane >> 4);
-                if (NMAT == 2) {
-                    float h[4];
+        } else if (a.finish == FIN_NONE) {
+            *(f32x4_t*)(a.out + at) = sa;
+            *(f32x4_t*)(a.out + at + 16) = sb;
+        } else {
+            mx_store_shared(a.out + (size_t)cur.part * a.part_stride + at, sa);
+            mx_store_shared(a.out + (size_t)cur.part * a.part_stride + at + 16, sb);
+        }
+    };
+    auto process = [&](auto slot_) __attribute__((always_inline)) {
+        constexpr int slot = decltype(slot_)::value;
+        const Item cur = item[slot];
+        const bool live = cur.u < u_end;
+        while (live && seg < cur.seg) next_rows();
+        item[slot] = next_word(item[slot ^ 1]);
+        if (live) {
+            const int nc = cur.rows * parts_of(R), col = lane & 15, kq = lane >> 4;
+            // this lane's operands: its column's, or zeros
+            const bool used = col < nc;
+            const u32x4_t* pb = used ? s_b + (size_t)((cur.word - cur.w0) * 64 + kq) * nc + col : &s_zero;
+            const int step = used ? 4 * nc : 0;
 #pragma unroll
-                    for (int i = 0; i < 4; i++) h[i] = sa[i] / (1.0f + __expf(-sa[i])) * sb[i];
-                    if (a.h_bf16)
-                        *(uint2*)((uint16_t*)a.out + at) = make_uint2(moe_pack_bf16x2(h[0], h[1]), moe_pack_bf16x2(h[2], h[3]));
-                    else
-                        *(float4*)(a.out + at) = make_float4(h[0], h[1], h[2], h[3]);
-                } else if (a.finish == FIN_NONE) {
-                    *(float4*)(a.out + at) = make_float4(sa[0], sa[1], sa[2], sa[3]);
-                } else {
-                    mx_store_shared(a.out + (size_t)cur.part * a.part_stride + at, sa);
+            for (int s = 0; s < 4; s++) {
+                bf16x8_t x[4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) x[j] = __builtin_bit_cast(bf16x8_t, pb[(s * 4 + j) * step]);
+#pragma unroll
+                for (int r = 0; r < 2; r++) {
+                    const float scale = mx_scale(sc[slot][r], s);
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx_widen8(buf[slot][r][s][j], scale), x[j], acc[r], 0, 0, 0);
                 }
             }
         }
+        request(item[slot], slot);
+        if (share > 1 || !live || cur.word + 1 < cur.wend) return;
+        store(cur);
+        acc[0] = acc[1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     };
-    for (unsigned u = u_begin; u < u_end; u += 2) {
-        process(std::integral_constant<int, 0>{}, u);
-        if (u + 1 < u_end) process(std::integral_constant<int, 1>{}, u + 1);
+    const Item first = item[0];
+    while (item[0].u < u_end) {  // (without a way out between the slots, which the waits would have to cover)
+        process(std::integral_constant<int, 0>{});
+        process(std::integral_constant<int, 1>{});
+    }
+    while (seg < seg_end) next_rows();
+    if (share > 1) {  // a unit a wave at most: the first of its waves adds the others' sums, in order
+        f32x4_t* s_part = (f32x4_t*)(s_raw + a.lds_operands);
+        if (sub > 0) {
+            s_part[((wave - wave / share - 1) * 2 + 0) * 64 + lane] = acc[0];
+            s_part[((wave - wave / share - 1) * 2 + 1) * 64 + lane] = acc[1];
+        }
+        __syncthreads();
+        if (sub == 0 && first.u < u_end) {
+            for (int w = 0; w < share - 1; w++) {
+                acc[0] += s_part[((wave - wave / share + w) * 2 + 0) * 64 + lane];
+                acc[1] += s_part[((wave - wave / share + w) * 2 + 1) * 64 + lane];
+            }
+            store(first);
+        }
     }
     write_xg();
     if (!DOWN || a.finish == FIN_NONE) return;
@@ -496,23 +596,20 @@ __global__ __launch_bounds__(64 * MXS_MAX_WAVES) void mx_stream_kernel(MxArgs a)
     // The slabs' stores have arrived; count the units, and finish the groups whose last unit this was.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    const unsigned need = (unsigned)n_tiles * (unsigned)a.P;
+    const unsigned need = n_tiles * (unsigned)a.P;
     for (unsigned base = u_begin; base < u_end; base += 64) {
         if (wave == 0) {
             bool last = false;
+            const unsigned g = (base + lane) % groups;
             if (base + lane < u_end)
-                last = __hip_atomic_fetch_add(a.counters + (base + lane) % groups, 1u, __ATOMIC_RELAXED,
-                                              __HIP_MEMORY_SCOPE_AGENT) + 1u == need;
+                last = __hip_atomic_fetch_add(a.counters + g, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u == need;
             const unsigned long long m = __ballot(last);
-            if (lane == 0) s_last = m;
+            if (last) s_group[__popcll(m & ((1ull << lane) - 1))] = (int)g;
+            if (lane == 0) s_nlast = __popcll(m);
         }
         __syncthreads();
-        unsigned long long m = s_last;
-        while (m) {
-            const int i = (int)__builtin_ctzll(m);
-            m &= m - 1;
-            mx_finish<NBU>(a, (int)((base + i) % groups), tid, threads, (float*)s_red);
-        }
+        const int n = s_nlast;
+        if (n) mx_finish(a, s_group, n, tid, (float*)s_raw);
         __syncthreads();
     }
 }
@@ -520,42 +617,29 @@ __global__ __launch_bounds__(64 * MXS_MAX_WAVES) void mx_stream_kernel(MxArgs a)
 // ------------------------------------------------------------------ host ----
 static inline size_t mx_align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-// Waves and parts of a reduction: every wave takes one scale word of every part.
-struct MxSplit {
-    int W, P;
-};
-static MxSplit mx_split(int K, bool parts) {
-    const int KW = mx_words(K);
-    MxSplit s = {KW, 1};
-    if (KW <= MXS_MAX_WAVES || !parts) return s;
-    // as many full waves as possible, then the fewest idle ones
-    int best = -1;
-    for (int w = MXS_MAX_WAVES; w >= 4; w--) {
-        const int p = (KW + w - 1) / w;
-        const int score = KW * 1000 / (p * w) * 16 + w;
-        if (score > best) {
-            best = score;
-            s.W = w;
-            s.P = p;
-        }
-    }
-    return s;
+// Parts of the second projection: the operands of a part fit in LDS, and few rows (on at most as many
+// experts) give every CU two units, of two words at least.
+static int mx_parts(int N, int d, int f) {
+    const int KW = mx_words(f);
+    int P = (KW + MXS_MAX_WORDS - 1) / MXS_MAX_WORDS;
+    while (P * 2 <= KW && (long long)N * (d / MXS_DOWN_COLS) * P < 2 * 256) P++;
+    return P;
 }
 
 bool moe_mx_stream_serves(int N, int E, int d, int f) {
-    if (mx_words(d) > MXS_MAX_WAVES || N / rows_of(ROWS_F32) + E > MXS_MAX_TILES) return false;
-    return (long long)MXS_MAX_TILES * mx_split(f, true).P * ((d > f ? d : f) / 16) < (1ll << 31);
+    if (mx_words(d) > MXS_MAX_WORDS || N / rows_of(ROWS_F32) + E > MXS_MAX_TILES) return false;
+    return (long long)MXS_MAX_TILES * mx_parts(1, d, f) * ((d > f ? d : f) / 16) < (1ll << 31);
 }
 
-// The rows up to which streaming is taken (16 rows a pass); the GEMM above it.
+// The rows up to which streaming is taken; the GEMM above it.
 int moe_mx_auto_path(int N, int E, int d, int f) {
     return N <= 72 && moe_mx_stream_serves(N, E, d, f) ? MOE_FFN_STREAM : MOE_FFN_GROUPED;
 }
 
-// counters, h [N,f] fp32, the second projection's slabs [P][N,d] fp32
+// counters, h [3][N,f] bf16, the second projection's slabs [P][N,d] fp32
 size_t moe_mx_stream_workspace(int N, int E, int d, int f) {
     (void)E;
-    return mx_align256((size_t)d / 16 * 4) + mx_align256((size_t)N * f * 4) + (size_t)mx_split(f, true).P * N * d * 4;
+    return mx_align256((size_t)d / MXS_DOWN_COLS * 4) + mx_align256((size_t)N * f * 6) + (size_t)mx_parts(N, d, f) * N * d * 4;
 }
 
 bool moe_mx_stream_routes(int T, int E, int k, int d, int f) {
@@ -565,39 +649,40 @@ bool moe_mx_stream_routes(int T, int E, int k, int d, int f) {
 bool moe_mx_block_supported(int T, int E, int k, int d, int f) {
     if (!moe_mx_stream_routes(T, E, k, d, f)) return false;
     if (T * k > 4 || E > 16 || T * (E + 1) > GS_MAX_ITEMS) return false;
-    return d / 16 <= GS_WAVE_ROWS * mx_split(d, false).W;
+    return d / 16 <= GS_WAVE_ROWS * MXS_WAVES;
 }
 
-template <int NMAT, int NBU, int R, bool GATE>
-static int mx_stream_go(const MxArgs& a, hipStream_t s) {
-    const void* fn = (const void*)mx_stream_kernel<NMAT, NBU, R, GATE>;
-    size_t lds = (size_t)2 * a.W * NMAT * NBU * 64 * sizeof(f32x4_t);
-    if (GATE && lds < (size_t)a.W * GS_WAVE_ROWS * GS_MAX_ITEMS * 4) lds = (size_t)a.W * GS_WAVE_ROWS * GS_MAX_ITEMS * 4;
-    // workgroups per CU, per device and number of waves: 0 = not asked yet.  Threads that race
-    // here ask the same question and store the same answer.
-    static std::atomic<int> occ_cache[MOE_MAX_DEVICES][MXS_MAX_WAVES + 1];
+template <bool DOWN, int R, bool GATE>
+static int mx_stream_go(const MxArgs& a, int rows_max, hipStream_t s) {
+    const void* fn = (const void*)mx_stream_kernel<DOWN, R, GATE>;
+    // operands of a tile's rows, at most; the shares of the gating sums; the finished rows of a block step
+    const int rows = rows_max < rows_of(R) ? rows_max : rows_of(R);
+    const int words = (a.KW + a.P - 1) / a.P;
+    size_t lds = (size_t)words * 1024 * rows * parts_of(R);
+    if (GATE && a.st.gate_sums && lds < (size_t)MXS_WAVES * GS_WAVE_ROWS * GS_MAX_ITEMS * 4)
+        lds = (size_t)MXS_WAVES * GS_WAVE_ROWS * GS_MAX_ITEMS * 4;
+    if (DOWN && a.st.w_gate_next && lds < (size_t)64 * 4 * MXS_DOWN_COLS * 4) lds = (size_t)64 * 4 * MXS_DOWN_COLS * 4;
+    MxArgs args = a;
+    args.lds_operands = (int)lds;
+    lds += 12 * 2 * 64 * sizeof(f32x4_t);  // of at most 4 units, 3 waves each
+    static std::atomic<bool> attr_set[MOE_MAX_DEVICES];
     const int dev = moe_current_device();
     if (dev < 0) return MOE_ERR_HIP;
-    int occ = occ_cache[dev][a.W].load(std::memory_order_relaxed);
-    if (occ == 0) {
-        MOE_HIP_TRY(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024));
-        MOE_HIP_TRY(hipOccupancyMaxActiveBlocksPerMultiprocessor(&occ, fn, 64 * a.W, lds));
-        occ = occ < 1 ? 1 : (occ > 4 ? 4 : occ);
-        occ_cache[dev][a.W].store(occ, std::memory_order_relaxed);
+    if (!attr_set[dev].load(std::memory_order_relaxed)) {
+        MOE_HIP_TRY(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 152 * 1024));
+        attr_set[dev].store(true, std::memory_order_relaxed);
     }
-    MxArgs args = a;
     void* params[1] = {(void*)&args};
-    MOE_HIP_TRY(hipLaunchKernel(fn, dim3((unsigned)(moe_num_cus() * occ)), dim3(64 * a.W), params, lds, s));
+    MOE_HIP_TRY(hipLaunchKernel(fn, dim3((unsigned)moe_num_cus()), dim3(64 * MXS_WAVES), params, lds, s));
     return moe_launch_status();
 }
 
 int moe_mx_stream_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtype, const int32_t* perm, int k,
                          const int32_t* offsets, int N, void* ws, float* yg, const MxStep* step, hipStream_t s) {
-    const MxSplit up_split = mx_split(W->d, false), down_split = mx_split(W->f, true);
     const bool gate = step && (step->logits || step->gate_sums);
     unsigned* counters = (unsigned*)ws;
-    float* h = (float*)((char*)ws + mx_align256((size_t)W->d / 16 * 4));
-    float* slabs = (float*)((char*)h + mx_align256((size_t)N * W->f * 4));
+    uint16_t* h = (uint16_t*)((char*)ws + mx_align256((size_t)W->d / MXS_DOWN_COLS * 4));
+    float* slabs = (float*)((char*)h + mx_align256((size_t)N * W->f * 6));
     if (step) offsets = step->offsets;
 
     MxArgs a = {};
@@ -607,20 +692,22 @@ int moe_mx_stream_launch(const moe_weights* W, const void* x, moe_dtype_t act_dt
     a.row_perm = gate ? nullptr : perm;
     a.row_k = k;
     a.offsets = offsets;
-    a.out = h;
+    a.out = (float*)h;
     a.E = W->E; a.N = N; a.K = W->d; a.C = W->f;
     a.NB = W->f / 16; a.KS = mx_frags(W->d); a.KW = mx_words(W->d);
-    a.W = up_split.W; a.P = 1;
+    a.P = 1;
     a.counters = counters;
-    a.n_counters = W->d / 16;  // a feature group is one block at least
+    a.n_counters = W->d / MXS_DOWN_COLS;
     if (step) a.st = *step;
     // A bf16 result is rounded to 8 bits once more, so h is held in as many before it.
-    a.h_bf16 = step && step->y && step->y_dtype == MOE_BF16 && !step->yg;
+    a.h_parts = step && step->y_dtype == MOE_BF16 && !step->yg ? 1 : 3;
+    // rows of a tile, at most.  (A token uses an expert once, but logits that are NaN may say otherwise.)
+    const int rows_max = N;
     int rc;
     if (act_dtype == MOE_BF16)
-        rc = gate ? mx_stream_go<2, 1, ROWS_BF16, true>(a, s) : mx_stream_go<2, 1, ROWS_BF16, false>(a, s);
+        rc = gate ? mx_stream_go<false, ROWS_BF16, true>(a, rows_max, s) : mx_stream_go<false, ROWS_BF16, false>(a, rows_max, s);
     else
-        rc = gate ? mx_stream_go<2, 1, ROWS_F32, true>(a, s) : mx_stream_go<2, 1, ROWS_F32, false>(a, s);
+        rc = gate ? mx_stream_go<false, ROWS_F32, true>(a, rows_max, s) : mx_stream_go<false, ROWS_F32, false>(a, rows_max, s);
     if (rc != MOE_OK) return rc;
     moe_record_mid_event(s);
 
@@ -630,10 +717,11 @@ int moe_mx_stream_launch(const moe_weights* W, const void* x, moe_dtype_t act_dt
     a.row_perm = nullptr;
     a.K = W->f; a.C = W->d;
     a.NB = W->d / 16; a.KS = mx_frags(W->f); a.KW = mx_words(W->f);
-    a.W = down_split.W; a.P = down_split.P;
+    a.P = mx_parts(N, W->d, W->f);
     a.finish = step ? FIN_LAYER : (a.P > 1 ? FIN_ROWS : FIN_NONE);
     a.out = a.finish == FIN_NONE ? yg : slabs;
     a.part_stride = (size_t)N * W->d;
     a.yg = yg;
-    return a.h_bf16 ? mx_stream_go<1, 2, ROWS_BF16, false>(a, s) : mx_stream_go<1, 2, ROWS_F32, false>(a, s);
+    return a.h_parts == 1 ? mx_stream_go<true, ROWS_BF16, false>(a, rows_max, s)
+                          : mx_stream_go<true, ROWS_PARTS, false>(a, rows_max, s);
 }

@@ -4,10 +4,31 @@
 // decode kernel that routes in its own prologue (moe_ffn_stream.hip).  Device code only.
 #pragma once
 
+#include <type_traits>
+
 #include "moe_internal.h"
 
 #define GATE_WAVE_MAX_E 16   // experts: 16 lanes hold one token's logits
 #define GATE_WAVE_MAX_N 64   // slots (tokens x k): one lane per slot
+
+// Maximum over the wave's 64 lanes, in every lane (NaN only if all are), without the LDS: inside a row of
+// 16 lanes by DPP, across rows by the two lane swaps.
+__device__ __forceinline__ float wave_max(float v) {
+    auto dpp = [](float a, auto ctrl) {
+        const int x = __builtin_bit_cast(int, a);
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(x, x, decltype(ctrl)::value, 0xF, 0xF, false));
+    };
+    v = fmaxf(v, dpp(v, std::integral_constant<int, 0xB1>{}));   // quad_perm 1,0,3,2
+    v = fmaxf(v, dpp(v, std::integral_constant<int, 0x4E>{}));   // quad_perm 2,3,0,1
+    v = fmaxf(v, dpp(v, std::integral_constant<int, 0x141>{}));  // row_half_mirror
+    v = fmaxf(v, dpp(v, std::integral_constant<int, 0x140>{}));  // row_mirror
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    v = fmaxf(__builtin_bit_cast(float, (unsigned)a[0]), __builtin_bit_cast(float, (unsigned)a[1]));
+    const unsigned w = __builtin_bit_cast(unsigned, v);
+    const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return fmaxf(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
+}
 
 // The contest for the token whose logits the group's G lanes hold (lane gl: expert e = gl with logit v, or -inf and
 // INT_MAX): returns the weight of the group's gl-th winner, my_i, for lanes gl < k.

@@ -37,6 +37,15 @@ __device__ __forceinline__ float mx_scale(unsigned word, int s) {
     return __uint_as_float(((word >> (8 * s)) & 0xFFu) << 23);
 }
 
+// Buffer descriptor over the 2 GiB from a wave-uniform p on: a request's address is then one lane
+// offset and one scalar.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_rsrc(const void* p) {
+    const unsigned long long v = (unsigned long long)p;
+    const unsigned lo = __builtin_amdgcn_readfirstlane((int)(unsigned)v);
+    const unsigned hi = __builtin_amdgcn_readfirstlane((int)(unsigned)(v >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(((unsigned long long)hi << 32) | lo), 0, (int)0x80000000u, 0x00027000);
+}
+
 // Eight codes and their scale -> eight bf16 operands, in the order of the codes.
 __device__ __forceinline__ bf16x8_t mx_widen8(unsigned codes, float scale) {
     const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);

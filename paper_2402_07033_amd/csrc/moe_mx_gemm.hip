@@ -31,7 +31,7 @@ constexpr int mxg_blocks_max(int T) { return T == 3 ? 2 : 8; }  // RBM
 #ifndef MXG_D1
 #define MXG_D1 3
 #define MXG_D2 2
-#define MXG_D4 1
+#define MXG_D4 2
 #endif
 constexpr int mxg_depth(int T, int RB) { return RB * T >= 5 ? 1 : RB * T >= 4 ? MXG_D4 : RB * T >= 2 ? MXG_D2 : MXG_D1; }
 constexpr int mxg_lds(int T) {
@@ -120,7 +120,6 @@ struct MxTile {
     SegInfo si;
     int b0, nblk;   // its blocks inside the segment
     int ft, part;
-    bool once;      // the expert's only row tile: its weights are read once
 };
 
 // Tile number L of the launch, order expert, then groups of at most 8 row tiles, part and feature
@@ -163,17 +162,7 @@ __device__ __forceinline__ bool mx_find_tile(const MxGemmArgs& a, int lane, MxTi
     const int per = blocks / tiles, more = blocks % tiles;
     ti.b0 = rt * per + (rt < more ? rt : more);
     ti.nblk = per + (rt < more ? 1 : 0);
-    ti.once = tiles == 1;
     return true;
-}
-
-// Buffer descriptor over the 2 GiB from a wave-uniform p on: a request's address is then one lane
-// offset and one scalar.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_rsrc(const void* p) {
-    const unsigned long long v = (unsigned long long)p;
-    const unsigned lo = __builtin_amdgcn_readfirstlane((int)(unsigned)v);
-    const unsigned hi = __builtin_amdgcn_readfirstlane((int)(unsigned)(v >> 32));
-    return __builtin_amdgcn_make_buffer_rsrc((void*)(((unsigned long long)hi << 32) | lo), 0, (int)0x80000000u, 0x00027000);
 }
 
 // At most n vector-memory requests and no LDS read in flight, then the other waves.
@@ -185,7 +174,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_rsrc(const void* p) {
         asm volatile("" ::: "memory");                                             \
     } while (0)
 
-template <int NMAT, int T, int RB>
+// ONCE: most weights of the launch are read by one tile only, and go past L2.
+template <int NMAT, int T, bool ONCE, int RB>
 __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& ti, int lane, int wave, unsigned char* smem) {
     constexpr int NF = MXG_NF, D = mxg_depth(T, RB), NS = D + 1;
     constexpr int STAGE = RB * T * 4096;
@@ -206,8 +196,7 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& 
 #pragma unroll
         for (int r = 0; r < NF; r++) {
             const int at = ((r / NMAT * a.KS + ks) * NMAT + r % NMAT) * 1024;
-            if (ti.once) q[slot][r] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, at, 2));
-            else q[slot][r] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, at, 0));
+            q[slot][r] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, at, ONCE ? 2 : 0));
             sc[slot][r] = __builtin_amdgcn_raw_buffer_load_b32(rs, lane * 4, (r * a.KW + (ks >> 2)) * 256, 0);
         }
 #pragma unroll
@@ -305,7 +294,7 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& 
     }
 }
 
-template <int NMAT, int T>
+template <int NMAT, int T, bool ONCE>
 __global__ __launch_bounds__(64 * MXG_WAVES, 2) void mx_gemm_kernel(MxGemmArgs a) {
     constexpr int RBM = mxg_blocks_max(T);
     extern __shared__ __align__(16) unsigned char smem[];
@@ -314,17 +303,17 @@ __global__ __launch_bounds__(64 * MXG_WAVES, 2) void mx_gemm_kernel(MxGemmArgs a
     MxTile ti;
     if (!mx_find_tile<RBM>(a, lane, ti)) return;
     switch (ti.nblk) {
-        case 1: mx_gemm_tile<NMAT, T, 1>(a, ti, lane, wave, smem); break;
-        case 2: mx_gemm_tile<NMAT, T, 2>(a, ti, lane, wave, smem); break;
+        case 1: mx_gemm_tile<NMAT, T, ONCE, 1>(a, ti, lane, wave, smem); break;
+        case 2: mx_gemm_tile<NMAT, T, ONCE, 2>(a, ti, lane, wave, smem); break;
         default:
             if constexpr (RBM > 2) {
                 switch (ti.nblk) {
-                    case 3: mx_gemm_tile<NMAT, T, 3>(a, ti, lane, wave, smem); break;
-                    case 4: mx_gemm_tile<NMAT, T, 4>(a, ti, lane, wave, smem); break;
-                    case 5: mx_gemm_tile<NMAT, T, 5>(a, ti, lane, wave, smem); break;
-                    case 6: mx_gemm_tile<NMAT, T, 6>(a, ti, lane, wave, smem); break;
-                    case 7: mx_gemm_tile<NMAT, T, 7>(a, ti, lane, wave, smem); break;
-                    default: mx_gemm_tile<NMAT, T, 8>(a, ti, lane, wave, smem); break;
+                    case 3: mx_gemm_tile<NMAT, T, ONCE, 3>(a, ti, lane, wave, smem); break;
+                    case 4: mx_gemm_tile<NMAT, T, ONCE, 4>(a, ti, lane, wave, smem); break;
+                    case 5: mx_gemm_tile<NMAT, T, ONCE, 5>(a, ti, lane, wave, smem); break;
+                    case 6: mx_gemm_tile<NMAT, T, ONCE, 6>(a, ti, lane, wave, smem); break;
+                    case 7: mx_gemm_tile<NMAT, T, ONCE, 7>(a, ti, lane, wave, smem); break;
+                    default: mx_gemm_tile<NMAT, T, ONCE, 8>(a, ti, lane, wave, smem); break;
                 }
             }
     }
@@ -391,7 +380,8 @@ template <int NMAT, int T>
 static void mxg_go(const MxGemmArgs& a, hipStream_t s) {
     const unsigned rtiles = (unsigned)(a.N / (16 * mxg_blocks_max(T)) + a.E);
     const unsigned grid = (rtiles * (unsigned)(a.FT * a.S) + 7) / 8 * 8;
-    hipLaunchKernelGGL((mx_gemm_kernel<NMAT, T>), dim3(grid), dim3(64 * MXG_WAVES), mxg_lds(T), s, a);
+    auto* kernel = a.N <= 16 * mxg_blocks_max(T) * a.E ? mx_gemm_kernel<NMAT, T, true> : mx_gemm_kernel<NMAT, T, false>;
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * MXG_WAVES), mxg_lds(T), s, a);
 }
 
 // The result in n_parts slabs of [N,d] floats from *slabs on, where the caller asks for them; else yg.

@@ -32,6 +32,18 @@
 #define MXS_MAX_SLOTS 64
 #define MXS_DOWN_COLS 32  // features of a unit of the second projection
 
+// Division of wave-uniform numbers below 2^31 by one that the launch fixes: two multiplications (the
+// general one takes some thirty vector instructions, and a kernel's first microseconds are its
+// prologue's instructions times the four waves of a SIMD).
+struct MxDiv {
+    unsigned d, m;  // m = floor(2^32 / d), 2^32 - 1 for 1
+};
+static inline MxDiv mx_divisor(unsigned d) { return MxDiv{d, d > 1 ? (unsigned)(0x100000000ull / d) : 0xFFFFFFFFu}; }
+__device__ __forceinline__ unsigned mx_div(unsigned n, const MxDiv& v) {
+    const unsigned q = __umulhi(n, v.m);  // the quotient or one less
+    return (q + 1) * v.d <= n ? q + 1 : q;
+}
+
 struct MxArgs {
     const u32x4_t* wfrag;
     const unsigned* wscale;
@@ -44,7 +56,7 @@ struct MxArgs {
     int E, N, K, C;
     int NB, KS, KW;           // 16-feature blocks, fragments and scale words of a reduction
     int P;                    // reduction parts
-    int lds_operands;         // bytes of LDS for the rows' operands; the shared units' sums lie behind
+    MxDiv by_groups, by_P, by_k, by_N, by_T, by_grid;
     unsigned* counters;       // [n_counters], one per feature group of the second projection:
     int n_counters;           // cleared by up, counted by down
     int finish;
@@ -64,44 +76,54 @@ constexpr int parts_of(int R) { return R == ROWS_BF16 ? 1 : 3; }
 
 // Stages the rows [row0, row0 + rows) of reduction words [w0, w1) as operands, 16-byte chunks
 // [(word, fragment, j, lane / 16)][column]: indices word*512 + fragment*128 + 32*(lane/16) + 8j .. +7.
-// First the requests (up to four chunks a thread), then the operands; chunks beyond are done in turn.
-template <int R>
-struct MxStage {
-    u32x4_t raw[4][R == ROWS_F32 ? 2 : 1];
-    float sc[4];
-};
+// A wave takes one word of one row (or of one part of it) at a time: block b of (row, word).
 template <int R>
 struct MxStager {
+    static constexpr int REGS = R == ROWS_F32 ? 2 : 1;
     const MxArgs& a;
     const int* rowmap;
     const float* row_scale;
-    int row0, rows, w0, chunks;  // chunks: 16-byte chunks of one row (fp32: of one part of it)
+    int row0, rows, w0, words, blocks;
     __device__ __forceinline__ MxStager(const MxArgs& args, const int* rm, const float* rs, int r0, int nr, int wa, int wb)
-        : a(args), rowmap(rm), row_scale(rs), row0(r0), rows(nr), w0(wa), chunks((wb - wa) * 64) {}
-    // item -> (row or part row, chunk of it); consecutive threads take consecutive chunks of a row
-    __device__ __forceinline__ int items() const { return chunks * rows * (R == ROWS_PARTS ? 3 : 1); }
-    __device__ __forceinline__ void request(int item, u32x4_t (&raw)[R == ROWS_F32 ? 2 : 1], float& sc) const {
-        const int rr = item / chunks, c = item % chunks;
-        const int t = rr % rows, part = rr / rows;
+        : a(args), rowmap(rm), row_scale(rs), row0(r0), rows(nr), w0(wa), words(wb - wa),
+          blocks((wb - wa) * nr * (R == ROWS_PARTS ? 3 : 1)) {}
+    __device__ __forceinline__ void split(int b, int& rr, int& w) const {
+        rr = 0;
+        w = b;
+        while (w >= words) {
+            w -= words;
+            rr++;
+        }
+    }
+    __device__ __forceinline__ void request(int b, int lane, u32x4_t (&raw)[REGS], float& sc) const {
+        int t, w;
+        split(b, t, w);
+        int part = 0;
+        if (R == ROWS_PARTS)
+            while (t >= rows) {
+                t -= rows;
+                part++;
+            }
         int src = row0 + t;
-        if (rowmap) src = rowmap[src];
-        else if (a.row_perm) src = a.row_perm[src] / a.row_k;
+        if (rowmap) src = __builtin_amdgcn_readfirstlane(rowmap[src]);
+        else if (a.row_perm) src = (int)mx_div((unsigned)__builtin_amdgcn_readfirstlane(a.row_perm[src]), a.by_k);
         sc = R == ROWS_F32 && row_scale ? row_scale[src] : 1.0f;
         if (R == ROWS_PARTS) src += part * a.N;
-        const int k0 = w0 * 512 + c * 8;
-        raw[0] = u32x4_t{0u, 0u, 0u, 0u};
-        if (R == ROWS_F32) raw[R == ROWS_F32 ? 1 : 0] = u32x4_t{0u, 0u, 0u, 0u};
+        const int k0 = (w0 + w) * 512 + lane * 8;
+#pragma unroll
+        for (int i = 0; i < REGS; i++) raw[i] = u32x4_t{0u, 0u, 0u, 0u};
         if (k0 >= a.K) return;
-        const char* p = (const char*)a.act + ((size_t)src * a.K + k0) * (R == ROWS_F32 ? 4 : 2);
-        raw[0] = *(const u32x4_t*)p;
-        if (R == ROWS_F32) raw[R == ROWS_F32 ? 1 : 0] = *(const u32x4_t*)(p + 16);
+        const char* p = (const char*)a.act + (size_t)src * a.K * (R == ROWS_F32 ? 4 : 2) + (size_t)k0 * (R == ROWS_F32 ? 4 : 2);
+#pragma unroll
+        for (int i = 0; i < REGS; i++) raw[i] = *(const u32x4_t*)(p + 16 * i);
     }
-    __device__ __forceinline__ void put(int item, const u32x4_t (&raw)[R == ROWS_F32 ? 2 : 1], float sc, u32x4_t* s_b) const {
+    __device__ __forceinline__ void put(int b, int lane, const u32x4_t (&raw)[REGS], float sc, u32x4_t* s_b) const {
 #pragma clang fp contract(off)
+        int rr, w;
+        split(b, rr, w);
         const int nc = rows * parts_of(R);
-        const int rr = item / chunks, c = item % chunks;
-        // c counts 8-index groups along the reduction: fragment c / 16, lane group c / 4 % 4, j c % 4
-        u32x4_t* dst = s_b + (size_t)((c & ~15) + (c & 3) * 4 + ((c >> 2) & 3)) * nc + rr;
+        // lane: 8-index group of the word; fragment lane / 16, lane group lane / 4 % 4, j lane % 4
+        u32x4_t* dst = s_b + (w * 64 + (lane & 48) + (lane & 3) * 4 + ((lane >> 2) & 3)) * nc + rr;
         if (R != ROWS_F32) {
             *dst = raw[0];
             return;
@@ -137,18 +159,12 @@ __device__ __forceinline__ f32x4_t mx_parts_sum(const f32x4_t& v, int rows, int 
 // whose L2 is another: both sides go past the caches that the other does not share, so that
 // neither has to write back or drop a whole cache (device fences by every wave made the second
 // projection of one token 72 us long instead of 28).
-__device__ __forceinline__ void mx_store_shared(float* p, const f32x4_t& v) {
-    typedef float f2 __attribute__((ext_vector_type(2)));
-    __hip_atomic_store((unsigned long long*)p, __builtin_bit_cast(unsigned long long, f2{v[0], v[1]}), __ATOMIC_RELAXED,
-                       __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store((unsigned long long*)p + 1, __builtin_bit_cast(unsigned long long, f2{v[2], v[3]}), __ATOMIC_RELAXED,
-                       __HIP_MEMORY_SCOPE_AGENT);
+#define MXS_SHARED 16  // cache policy of a buffer access: sc1, coherent for the device
+__device__ __forceinline__ void mx_store_shared(const __amdgpu_buffer_rsrc_t& r, unsigned at, const f32x4_t& v) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), r, at, 0, MXS_SHARED);
 }
-__device__ __forceinline__ f32x4_t mx_load_shared(const float* p) {
-    typedef float f2 __attribute__((ext_vector_type(2)));
-    const f2 a = __builtin_bit_cast(f2, __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-    const f2 b = __builtin_bit_cast(f2, __hip_atomic_load((const unsigned long long*)p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-    return f32x4_t{a[0], a[1], b[0], b[1]};
+__device__ __forceinline__ f32x4_t mx_load_shared(const __amdgpu_buffer_rsrc_t& r, unsigned at) {
+    return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, MXS_SHARED));
 }
 
 // Per-expert batching of N <= 64 slots by one wave, E <= 64: lane p owns slot p and finds the slots
@@ -196,35 +212,37 @@ __device__ __forceinline__ void mx_batch_wave(const int* s_idx, int N, int E, in
     }
 }
 
-// The workgroup's waves route the tokens, one at a time each: lane e holds expert e's logit, and its
-// rank is the number of logits before it (larger, or equal and of a lower expert).  k rounds of a
-// contest by exchanges between lanes, as in moe_route, take 2.5 us for 64 experts and k = 6; this
-// a fifth.  The weights, which only the writing workgroup needs, are moe_route's to the bit.
+// The workgroup's waves route the tokens, one at a time each, lane e holding expert e's logit: k
+// rounds of the wave's maximum and, of the lanes that have it, the lowest.  The weights, which only
+// the writing workgroup needs, are moe_route's to the bit.
 __device__ __forceinline__ void mx_route(const float* logits, const MxStep& st, int E, int wave, int W, int lane, int* s_idx,
-                                         float* s_top, bool write) {
+                                         bool write) {
     for (int t = wave; t < st.T; t += W) {
-        const float v = lane < E ? logits[(size_t)t * E + lane] : -INFINITY;
-        int rank = 0;
-        for (int e = 0; e < E; e++) {
-            const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), e));
-            rank += (lane > e ? o >= v : o > v) ? 1 : 0;
+        float v = lane < E ? logits[(size_t)t * E + lane] : -INFINITY;
+        float my_v = 0.f, top = 0.f;
+        int my_e = 0;
+        unsigned long long open = E < 64 ? (1ull << E) - 1 : ~0ull;  // experts not taken yet
+        for (int j = 0; j < st.k; j++) {
+            const float m = wave_max(v);
+            unsigned long long have = __ballot(v == m) & open;
+            if (have == 0ull) have = open;  // (logits that are NaN, or all that is left is -infinity's end)
+            const int e = (int)__builtin_ctzll(have);
+            open &= ~(1ull << e);
+            if (j == 0) top = m;
+            if (lane == j) {
+                my_v = m;
+                my_e = e;
+            }
+            if (lane == e) v = -INFINITY;
         }
-        if (lane < st.k) s_idx[t * st.k + lane] = 0;  // (logits that are NaN leave ranks out)
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        if (lane < E && rank < st.k) {
-            s_idx[t * st.k + rank] = lane;
-            s_top[t * st.k + rank] = v;
-        }
+        if (lane < st.k) s_idx[t * st.k + lane] = my_e;
         if (!write) continue;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        const float u = lane < st.k ? expf(s_top[t * st.k + lane] - s_top[t * st.k]) : 0.f;
+        const float u = lane < st.k ? expf(my_v - top) : 0.f;
         float sum = u;
 #pragma unroll
         for (int m = 1; m < MOE_MAX_K; m <<= 1) sum += __shfl_xor(sum, m, 64);
         if (lane < st.k) {
-            st.idx[(size_t)t * st.k + lane] = s_idx[t * st.k + lane];
+            st.idx[(size_t)t * st.k + lane] = my_e;
             st.weights[(size_t)t * st.k + lane] = u / sum;
         }
     }
@@ -233,14 +251,14 @@ __device__ __forceinline__ void mx_route(const float* logits, const MxStep& st, 
 // The groups of `mask` (bit i: group (g0 + i) % groups) are complete: add the parts, and what the
 // step asks for beyond them.  All of them at once: one after the other, each waiting for its own
 // slabs, the last workgroup of an 8-expert step took 12 us.
-__device__ __forceinline__ f32x4_t mx_row_sum(const MxArgs& a, int row, size_t col) {
-    const float* p = a.out + (size_t)row * a.C + col;
-    f32x4_t v = mx_load_shared(p);
+__device__ __forceinline__ f32x4_t mx_row_sum(const MxArgs& a, const __amdgpu_buffer_rsrc_t& slabs, int row, size_t col) {
+    const unsigned at = (unsigned)(((size_t)row * a.C + col) * 4), stride = (unsigned)(a.part_stride * 4);
+    f32x4_t v = mx_load_shared(slabs, at);
     for (int q = 1; q < a.P; q += 4) {  // four requests at a time, added in order
         f32x4_t u[4];
 #pragma unroll
         for (int i = 0; i < 4; i++)
-            if (q + i < a.P) u[i] = mx_load_shared(p + (size_t)(q + i) * a.part_stride);
+            if (q + i < a.P) u[i] = mx_load_shared(slabs, at + (q + i) * stride);
 #pragma unroll
         for (int i = 0; i < 4; i++)
             if (q + i < a.P) v += u[i];
@@ -250,27 +268,28 @@ __device__ __forceinline__ f32x4_t mx_row_sum(const MxArgs& a, int row, size_t c
 
 __device__ __forceinline__ void mx_finish(const MxArgs& a, const int* s_group, int n, int tid, float* s_x) {
     constexpr int C4 = MXS_DOWN_COLS / 4;  // 16-byte columns of a group
+    const __amdgpu_buffer_rsrc_t slabs = mx_rsrc(a.out);
     if (a.finish == FIN_ROWS) {
         for (int i = tid; i < n * a.N * C4; i += 64 * MXS_WAVES) {
-            const int c4 = i % C4, row = i / C4 % a.N;
-            const size_t col = (size_t)s_group[i / C4 / a.N] * MXS_DOWN_COLS + 4 * c4;
-            const f32x4_t v = mx_row_sum(a, row, col);
+            const int c4 = i % C4, gi = (int)mx_div(i / C4, a.by_N), row = i / C4 - gi * a.N;
+            const size_t col = (size_t)s_group[gi] * MXS_DOWN_COLS + 4 * c4;
+            const f32x4_t v = mx_row_sum(a, slabs, row, col);
             *(f32x4_t*)(a.yg + (size_t)row * a.C + col) = v;
         }
         return;
     }
     const MxStep& st = a.st;
-    const int T = a.N / st.k;
+    const int T = (int)a.by_T.d;
     for (int i = tid; i < n * T * C4; i += 64 * MXS_WAVES) {
-        const int c4 = i % C4, t = i / C4 % T;
-        const size_t col = (size_t)s_group[i / C4 / T] * MXS_DOWN_COLS + 4 * c4;
+        const int c4 = i % C4, gi = (int)mx_div(i / C4, a.by_T), t = i / C4 - gi * T;
+        const size_t col = (size_t)s_group[gi] * MXS_DOWN_COLS + 4 * c4;
         const size_t at = (size_t)t * a.C + col;
         f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
         for (int j = 0; j < st.k; j++) {
             const float w = st.weights[t * st.k + j];
             int row = st.inv_perm[t * st.k + j];
             row = row < 0 ? 0 : (row >= a.N ? a.N - 1 : row);
-            const f32x4_t v = mx_row_sum(a, row, col);
+            const f32x4_t v = mx_row_sum(a, slabs, row, col);
             if (st.yg) *(f32x4_t*)(st.yg + (size_t)row * a.C + col) = v;
             acc += w * v;
         }
@@ -310,7 +329,6 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
     __shared__ u32x4_t s_zero;       // ... of the columns that no row has
     __shared__ int s_tiles[3][MXS_MAX_TILES], s_ntiles;
     __shared__ int s_idx[GATE ? MXS_MAX_SLOTS : 1];
-    __shared__ float s_top[GATE ? MXS_MAX_SLOTS : 1];
     __shared__ int s_batch[GATE ? 3 : 1][MXS_MAX_SLOTS];
     __shared__ float s_gate[GATE ? 3 : 1][64];  // the summed shares, 1/rms per token, the logits
     __shared__ float s_gpart[GATE ? MXS_WAVES : 1][GS_MAX_ITEMS];
@@ -361,7 +379,7 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
             lg = s_gate[2];
             row_scale = s_gate[1];
         }
-        mx_route(lg, st, a.E, wave, MXS_WAVES, lane, s_idx, s_top, blockIdx.x == 0);
+        mx_route(lg, st, a.E, wave, MXS_WAVES, lane, s_idx, blockIdx.x == 0);
         __syncthreads();
         rowmap = s_batch[1];
     }
@@ -393,26 +411,19 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
     const unsigned n_tiles = (unsigned)__builtin_amdgcn_readfirstlane(s_ntiles);
     const unsigned groups = (unsigned)(DOWN ? a.NB / 2 : a.NB);
     const unsigned total = n_tiles * (unsigned)a.P * groups;  // < 2^31 (host check)
-    const unsigned per = total / gridDim.x, rem = total % gridDim.x;
-    const unsigned u_begin = per * blockIdx.x + rem * blockIdx.x / gridDim.x;
-    const unsigned u_end = per * (blockIdx.x + 1) + rem * (blockIdx.x + 1) / gridDim.x;
+    const unsigned per = mx_div(total, a.by_grid), rem = total - per * gridDim.x;
+    const unsigned u_begin = per * blockIdx.x + mx_div(rem * blockIdx.x, a.by_grid);
+    const unsigned u_end = per * (blockIdx.x + 1) + mx_div(rem * (blockIdx.x + 1), a.by_grid);
     if (u_begin >= u_end) {  // uniform over the workgroup
         write_xg();
         return;
     }
 
-    // With so few units that each can have `share` waves, these share its words (behind one another
-    // they would be as many trips to memory): units u_begin + wave / share.
-    const unsigned most = (total + gridDim.x - 1) / gridDim.x;
-    const int share = most * 4 <= MXS_WAVES && a.KW / a.P >= 4 ? 4 : most * 2 <= MXS_WAVES && a.KW / a.P >= 2 ? 2 : 1;
-    const int sub = wave % share;
-    const unsigned u_wave = u_begin + wave / share, u_step = MXS_WAVES / share;
-
-    // A wave's work is one sequence of words: those of its first unit, of the unit u_step further, ...
+    // A wave's work is one sequence of words: those of unit u_begin + wave, of the unit 16 further, ...
     // Word i is in register slot i % 2, and word i + 2 is requested when it has been used.
     struct Item {
         unsigned u, seg;  // unit (>= u_end: none), and its tile and part
-        int g, row0, rows, word, w0, wend, part;  // w0: the part's first word, wend: past this wave's last
+        int g, row0, rows, word, w0, w1, part;  // words [w0, w1) of the reduction
         const u32x4_t* p;   // the word's first fragment
         const unsigned* q;  // its scales
     };
@@ -420,16 +431,14 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
     auto first_word = [&](unsigned u) __attribute__((always_inline)) -> Item {
         Item n;
         n.u = u;
-        n.seg = u / groups;
-        const unsigned tile = n.seg / (unsigned)a.P;
+        n.seg = mx_div(u, a.by_groups);
+        const unsigned tile = mx_div(n.seg, a.by_P);
         n.g = (int)(u - n.seg * groups);
         n.part = (int)(n.seg - tile * (unsigned)a.P);
         n.row0 = __builtin_amdgcn_readfirstlane(s_tiles[1][tile]);
         n.rows = __builtin_amdgcn_readfirstlane(s_tiles[2][tile]);
-        n.w0 = n.part * a.KW / a.P;
-        const int words = (n.part + 1) * a.KW / a.P - n.w0;
-        n.word = n.w0 + sub * words / share;
-        n.wend = n.w0 + (sub + 1) * words / share;
+        n.word = n.w0 = (int)mx_div(n.part * a.KW, a.by_P);
+        n.w1 = (int)mx_div((n.part + 1) * a.KW, a.by_P);
         const size_t frow = ((size_t)__builtin_amdgcn_readfirstlane(s_tiles[0][tile]) * groups + (size_t)n.g) * 2;
         n.p = a.wfrag + frow * a.KS * 64 + (size_t)n.word * (4 * FSTEP);
         n.q = a.wscale + (frow * a.KW + n.word) * 64;
@@ -437,12 +446,12 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
     };
     auto next_word = [&](const Item& c) __attribute__((always_inline)) -> Item {
         Item n = c;
-        if (c.word + 1 < c.wend) {
+        if (c.word + 1 < c.w1) {
             n.word++;
             n.p += 4 * FSTEP;
             n.q += 64;
-        } else if (c.u + u_step < u_end) {
-            return first_word(c.u + u_step);
+        } else if (c.u + MXS_WAVES < u_end) {
+            return first_word(c.u + MXS_WAVES);
         } else {
             n.u = u_end;
         }
@@ -468,47 +477,49 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
 
     // Rows first, weights behind them (requests are answered in order, and the first burst of weights
     // takes microseconds), then the rows' operands into LDS.
-    unsigned seg = u_begin / groups;
+    unsigned seg = mx_div(u_begin, a.by_groups);
     auto rows_at = [&](unsigned sg) __attribute__((always_inline)) -> MxStager<R> {
-        const unsigned tile = sg / (unsigned)a.P;
+        const unsigned tile = mx_div(sg, a.by_P);
         const int part = (int)(sg - tile * (unsigned)a.P);
         return MxStager<R>(a, rowmap, row_scale, __builtin_amdgcn_readfirstlane(s_tiles[1][tile]),
-                           __builtin_amdgcn_readfirstlane(s_tiles[2][tile]), part * a.KW / a.P, (part + 1) * a.KW / a.P);
+                           __builtin_amdgcn_readfirstlane(s_tiles[2][tile]), (int)mx_div(part * a.KW, a.by_P),
+                           (int)mx_div((part + 1) * a.KW, a.by_P));
     };
     Item item[2];
     {
         const MxStager<R> stager = rows_at(seg);
-        MxStage<R> m;
+        u32x4_t raw[2][MxStager<R>::REGS];
+        float sc1[2];
 #pragma unroll
-        for (int i = 0; i < 4; i++)
-            if (tid + i * THREADS < stager.items()) stager.request(tid + i * THREADS, m.raw[i], m.sc[i]);
+        for (int i = 0; i < 2; i++)
+            if (wave + i * MXS_WAVES < stager.blocks) stager.request(wave + i * MXS_WAVES, lane, raw[i], sc1[i]);
         __builtin_amdgcn_sched_barrier(0);
         item[0].u = u_end;
-        if (u_wave < u_end) {
-            item[0] = first_word(u_wave);
+        if (u_begin + wave < u_end) {
+            item[0] = first_word(u_begin + wave);
             request(item[0], 0);
             item[1] = next_word(item[0]);
             request(item[1], 1);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 4; i++)
-            if (tid + i * THREADS < stager.items()) stager.put(tid + i * THREADS, m.raw[i], m.sc[i], s_b);
-        for (int it = tid + 4 * THREADS; it < stager.items(); it += THREADS) {
-            stager.request(it, m.raw[0], m.sc[0]);
-            stager.put(it, m.raw[0], m.sc[0], s_b);
+        for (int i = 0; i < 2; i++)
+            if (wave + i * MXS_WAVES < stager.blocks) stager.put(wave + i * MXS_WAVES, lane, raw[i], sc1[i], s_b);
+        for (int b = wave + 2 * MXS_WAVES; b < stager.blocks; b += MXS_WAVES) {
+            stager.request(b, lane, raw[0], sc1[0]);
+            stager.put(b, lane, raw[0], sc1[0], s_b);
         }
     }
     __syncthreads();
-    const unsigned seg_end = (u_end - 1) / groups;
+    const unsigned seg_end = mx_div(u_end - 1, a.by_groups);
     auto next_rows = [&]() __attribute__((always_inline)) {  // by all waves alike
         const MxStager<R> stager = rows_at(++seg);
         __syncthreads();
-        for (int it = tid; it < stager.items(); it += THREADS) {
-            u32x4_t raw[R == ROWS_F32 ? 2 : 1];
+        for (int b = wave; b < stager.blocks; b += MXS_WAVES) {
+            u32x4_t raw[MxStager<R>::REGS];
             float s1;
-            stager.request(it, raw, s1);
-            stager.put(it, raw, s1, s_b);
+            stager.request(b, lane, raw, s1);
+            stager.put(b, lane, raw, s1, s_b);
         }
         __syncthreads();
     };
@@ -534,8 +545,10 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
             *(f32x4_t*)(a.out + at) = sa;
             *(f32x4_t*)(a.out + at + 16) = sb;
         } else {
-            mx_store_shared(a.out + (size_t)cur.part * a.part_stride + at, sa);
-            mx_store_shared(a.out + (size_t)cur.part * a.part_stride + at + 16, sb);
+            const __amdgpu_buffer_rsrc_t slabs = mx_rsrc(a.out);
+            const unsigned to = (unsigned)(((size_t)cur.part * a.part_stride + at) * 4);
+            mx_store_shared(slabs, to, sa);
+            mx_store_shared(slabs, to + 64, sb);
         }
     };
     auto process = [&](auto slot_) __attribute__((always_inline)) {
@@ -565,31 +578,15 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
             }
         }
         request(item[slot], slot);
-        if (share > 1 || !live || cur.word + 1 < cur.wend) return;
+        if (!live || cur.word + 1 < cur.w1) return;
         store(cur);
         acc[0] = acc[1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     };
-    const Item first = item[0];
     while (item[0].u < u_end) {  // (without a way out between the slots, which the waits would have to cover)
         process(std::integral_constant<int, 0>{});
         process(std::integral_constant<int, 1>{});
     }
     while (seg < seg_end) next_rows();
-    if (share > 1) {  // a unit a wave at most: the first of its waves adds the others' sums, in order
-        f32x4_t* s_part = (f32x4_t*)(s_raw + a.lds_operands);
-        if (sub > 0) {
-            s_part[((wave - wave / share - 1) * 2 + 0) * 64 + lane] = acc[0];
-            s_part[((wave - wave / share - 1) * 2 + 1) * 64 + lane] = acc[1];
-        }
-        __syncthreads();
-        if (sub == 0 && first.u < u_end) {
-            for (int w = 0; w < share - 1; w++) {
-                acc[0] += s_part[((wave - wave / share + w) * 2 + 0) * 64 + lane];
-                acc[1] += s_part[((wave - wave / share + w) * 2 + 1) * 64 + lane];
-            }
-            store(first);
-        }
-    }
     write_xg();
     if (!DOWN || a.finish == FIN_NONE) return;
 
@@ -600,7 +597,7 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
     for (unsigned base = u_begin; base < u_end; base += 64) {
         if (wave == 0) {
             bool last = false;
-            const unsigned g = (base + lane) % groups;
+            const unsigned g = base + lane - mx_div(base + lane, a.by_groups) * groups;
             if (base + lane < u_end)
                 last = __hip_atomic_fetch_add(a.counters + g, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u == need;
             const unsigned long long m = __ballot(last);
@@ -618,16 +615,17 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
 static inline size_t mx_align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 // Parts of the second projection: the operands of a part fit in LDS, and few rows (on at most as many
-// experts) give every CU two units, of two words at least.
+// experts) give every CU four units, of two words at least.
 static int mx_parts(int N, int d, int f) {
     const int KW = mx_words(f);
     int P = (KW + MXS_MAX_WORDS - 1) / MXS_MAX_WORDS;
-    while (P * 2 <= KW && (long long)N * (d / MXS_DOWN_COLS) * P < 2 * 256) P++;
+    while (P * 2 <= KW && (long long)N * (d / MXS_DOWN_COLS) * P < 4 * 256) P++;
     return P;
 }
 
 bool moe_mx_stream_serves(int N, int E, int d, int f) {
     if (mx_words(d) > MXS_MAX_WORDS || N / rows_of(ROWS_F32) + E > MXS_MAX_TILES) return false;
+    if ((long long)mx_parts(N, d, f) * N * d * 4 >= (1ll << 31)) return false;  // (the slabs' offsets)
     return (long long)MXS_MAX_TILES * mx_parts(1, d, f) * ((d > f ? d : f) / 16) < (1ll << 31);
 }
 
@@ -662,16 +660,20 @@ static int mx_stream_go(const MxArgs& a, int rows_max, hipStream_t s) {
     if (GATE && a.st.gate_sums && lds < (size_t)MXS_WAVES * GS_WAVE_ROWS * GS_MAX_ITEMS * 4)
         lds = (size_t)MXS_WAVES * GS_WAVE_ROWS * GS_MAX_ITEMS * 4;
     if (DOWN && a.st.w_gate_next && lds < (size_t)64 * 4 * MXS_DOWN_COLS * 4) lds = (size_t)64 * 4 * MXS_DOWN_COLS * 4;
-    MxArgs args = a;
-    args.lds_operands = (int)lds;
-    lds += 12 * 2 * 64 * sizeof(f32x4_t);  // of at most 4 units, 3 waves each
     static std::atomic<bool> attr_set[MOE_MAX_DEVICES];
     const int dev = moe_current_device();
     if (dev < 0) return MOE_ERR_HIP;
     if (!attr_set[dev].load(std::memory_order_relaxed)) {
-        MOE_HIP_TRY(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 152 * 1024));
+        MOE_HIP_TRY(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 136 * 1024));
         attr_set[dev].store(true, std::memory_order_relaxed);
     }
+    MxArgs args = a;
+    args.by_groups = mx_divisor((unsigned)(DOWN ? a.NB / 2 : a.NB));
+    args.by_P = mx_divisor((unsigned)a.P);
+    args.by_k = mx_divisor((unsigned)a.row_k);
+    args.by_N = mx_divisor((unsigned)a.N);
+    args.by_T = mx_divisor((unsigned)(a.finish == FIN_LAYER ? a.N / a.st.k : a.N));
+    args.by_grid = mx_divisor((unsigned)moe_num_cus());
     void* params[1] = {(void*)&args};
     MOE_HIP_TRY(hipLaunchKernel(fn, dim3((unsigned)moe_num_cus()), dim3(64 * MXS_WAVES), params, lds, s));
     return moe_launch_status();

@@ -354,7 +354,7 @@ int moe_decode_layer(const moe_weights_t* W, const float* x, const float* logits
  *   x_out [T,d] fp32 out; may be x_in itself (in place), no other overlap between arguments
  *   w_gate_next [d,E] fp32 or NULL (then gate_sums_next is not written);
  *   gate_sums_next [d/16][stride] fp32 out: pass it, with n_shares = d/16, to the next call
- * MOE_ERR_UNSUPPORTED for fp32 weights, T*k > 4, E > 16, T*(E+1) > 32, d/16 above the number
+ * MOE_ERR_UNSUPPORTED for fp32 weights, T*k > 4, E > 16, with bf16 weights T*(E+1) > 32, d/16 above the number
  * of compute units (or above 32 per wavefront of the first kernel), or a shape the STREAM
  * family does not serve: use the
  * separate calls then.
@@ -373,7 +373,7 @@ int moe_decode_block_supported(int T, int E, int k, int d, int f, moe_dtype_t w_
  */
 int moe_gate_sums(const float* x, const float* w_gate, int T, int d, int E, float* sums,
                   void* stream);
-/* HOST: floats per share: 32, one 128-byte line (0 for invalid sizes). */
+/* HOST: floats per share: T*(E+1) in whole 128-byte lines (0 for invalid sizes). */
 size_t moe_gate_sums_stride(int T, int E);
 
 /*

@@ -849,12 +849,10 @@ bool moe_ffn_stream_block_supported(int T, int E, int k, int d, int f) {
            d / 16 <= GS_WAVE_ROWS * pl.Wu && small_down_ok(T * k, d, f);
 }
 
-// A share is one 128-byte line: the workgroups that write neighbouring shares sit on different
+// A share is whole 128-byte lines: the workgroups that write neighbouring shares sit on different
 // XCDs, and a line written from two L2s is written back in pieces.
 int moe_ffn_stream_gate_stride(int T, int E) {
-    (void)T;
-    (void)E;
-    return GS_MAX_ITEMS;
+    return (T * (E + 1) + GS_MAX_ITEMS - 1) / GS_MAX_ITEMS * GS_MAX_ITEMS;
 }
 
 // One transformer block's expert layer on the residual stream in two launches: the first

@@ -7,9 +7,9 @@
 // come as operand chunks (mx_rows_kernel, and the first projection's epilogue for the second) through
 // a ring of LDS stages that the workgroup's four waves fill with direct-to-LDS loads, one fragment's
 // 128 reduction indices a stage.
-//   * tile: up to RBM blocks of 16 rows of one expert x 256 features; an expert's blocks are dealt
+//   * tile: up to RBM (2 or 8) blocks of 16 rows of one expert x 256 features; an expert's blocks are dealt
 //     evenly to its tiles, and the loop exists once per number of blocks.
-//   * two workgroups per CU: one's prologue and epilogue run under the other's loop.
+//   * two workgroups per CU, or four: one's prologue and epilogue run under the other's loop.
 //   * a step waits for its stage, meets the other waves at a barrier (which also frees the stage of
 //     the step before), requests the operands D steps ahead, and multiplies.
 //   * few tiles (second projection): the reduction is cut in S parts, every part a slab of partial
@@ -26,17 +26,13 @@
 #define MXG_EXACT_ROWS 72
 #define MXG_WAVES 4
 #define MXG_NF 4   // fragment rows of a wave
-constexpr int mxg_blocks_max(int T) { return T == 3 ? 2 : 8; }  // RBM
-// steps requested ahead, in stages of LDS: 8 KiB .. 64 KiB a workgroup
-#ifndef MXG_D1
-#define MXG_D1 3
-#define MXG_D2 2
-#define MXG_D4 2
-#endif
-constexpr int mxg_depth(int T, int RB) { return RB * T >= 5 ? 1 : RB * T >= 4 ? MXG_D4 : RB * T >= 2 ? MXG_D2 : MXG_D1; }
-constexpr int mxg_lds(int T) {
+// Steps requested ahead, in stages of LDS (8 .. 64 KiB a workgroup).  More rows are more matrix work under
+// which a request may travel: 8 experts of 64 rows take 135 + 90 us with one step (both projections), 126 +
+// 69 with two; with one row, three or six steps are the same within 3 %.
+constexpr int mxg_depth(int T, int RB) { return RB * T > 4 ? 1 : RB * T > 1 ? 2 : 3; }
+constexpr int mxg_lds(int T, int RBM) {
     int most = 0;
-    for (int rb = 1; rb <= mxg_blocks_max(T); rb++) {
+    for (int rb = 1; rb <= RBM; rb++) {
         const int b = (mxg_depth(T, rb) + 1) * rb * T * 4096;
         most = b > most ? b : most;
     }
@@ -228,6 +224,8 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& 
         const u32x4_t* st = (const u32x4_t*)(smem + u * STAGE) + lane;
 #pragma unroll
         for (int j = 0; j < 4; j++) {
+            // (the largest tile has no registers for two quarters' rows: without this the compiler spills)
+            if (RB == 8 && j > 0) __builtin_amdgcn_sched_barrier(0);
             bf16x8_t x[RB][T];
 #pragma unroll
             for (int b = 0; b < RB; b++)
@@ -294,28 +292,22 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& 
     }
 }
 
-template <int NMAT, int T, bool ONCE>
-__global__ __launch_bounds__(64 * MXG_WAVES, 2) void mx_gemm_kernel(MxGemmArgs a) {
-    constexpr int RBM = mxg_blocks_max(T);
+template <int NMAT, int T, int RBM, bool ONCE>
+__global__ __launch_bounds__(64 * MXG_WAVES, RBM > 2 ? 2 : 4) void mx_gemm_kernel(MxGemmArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     MxTile ti;
     if (!mx_find_tile<RBM>(a, lane, ti)) return;
-    switch (ti.nblk) {
-        case 1: mx_gemm_tile<NMAT, T, ONCE, 1>(a, ti, lane, wave, smem); break;
-        case 2: mx_gemm_tile<NMAT, T, ONCE, 2>(a, ti, lane, wave, smem); break;
-        default:
-            if constexpr (RBM > 2) {
-                switch (ti.nblk) {
-                    case 3: mx_gemm_tile<NMAT, T, ONCE, 3>(a, ti, lane, wave, smem); break;
-                    case 4: mx_gemm_tile<NMAT, T, ONCE, 4>(a, ti, lane, wave, smem); break;
-                    case 5: mx_gemm_tile<NMAT, T, ONCE, 5>(a, ti, lane, wave, smem); break;
-                    case 6: mx_gemm_tile<NMAT, T, ONCE, 6>(a, ti, lane, wave, smem); break;
-                    case 7: mx_gemm_tile<NMAT, T, ONCE, 7>(a, ti, lane, wave, smem); break;
-                    default: mx_gemm_tile<NMAT, T, ONCE, 8>(a, ti, lane, wave, smem); break;
-                }
-            }
+    if (ti.nblk == 1) mx_gemm_tile<NMAT, T, ONCE, 1>(a, ti, lane, wave, smem);
+    else if (ti.nblk == 2) mx_gemm_tile<NMAT, T, ONCE, 2>(a, ti, lane, wave, smem);
+    if constexpr (RBM == 8) {
+        if (ti.nblk == 3) mx_gemm_tile<NMAT, T, ONCE, 3>(a, ti, lane, wave, smem);
+        else if (ti.nblk == 4) mx_gemm_tile<NMAT, T, ONCE, 4>(a, ti, lane, wave, smem);
+        else if (ti.nblk == 5) mx_gemm_tile<NMAT, T, ONCE, 5>(a, ti, lane, wave, smem);
+        else if (ti.nblk == 6) mx_gemm_tile<NMAT, T, ONCE, 6>(a, ti, lane, wave, smem);
+        else if (ti.nblk == 7) mx_gemm_tile<NMAT, T, ONCE, 7>(a, ti, lane, wave, smem);
+        else if (ti.nblk == 8) mx_gemm_tile<NMAT, T, ONCE, 8>(a, ti, lane, wave, smem);
     }
 }
 
@@ -335,17 +327,25 @@ __global__ __launch_bounds__(256) void mx_sum_kernel(const float4* __restrict__ 
 static inline size_t mxg_align256(size_t v) { return (v + 255) & ~(size_t)255; }
 static inline size_t mxg_blocks(int N, int E) { return (size_t)N / 16 + E; }
 
+// Blocks of a tile, at most, by the mean rows of an expert in use.  Tiles of 32 rows let four workgroups
+// run on a CU instead of two, and experts above share their weights in L2 or not at all: 8 experts, 77
+// tokens, Zipf 1.2 (19 rows) 129 + 79 us with tiles of 128 rows, 116 + 59 with 32; 64 experts of 28 rows,
+// uneven, 45 + 26 and 52 + 32.
+#define MXG_SMALL_ROWS 20
+static int mxg_rbm(int N, int E, int T) {
+    return T == 3 || N <= MXG_SMALL_ROWS * (N < E ? N : E) ? 2 : 8;
+}
+
 struct MxGemmShape {
     int tu, td;  // parts of the rows and of h
     int S;       // reduction parts of the second projection
-    int upper;   // row tiles, at most (of the fewest blocks a tile may have)
 };
 static MxGemmShape mxg_shape(int N, int E, int d, int f, bool x_f32, bool y_f32) {
     MxGemmShape sh;
     sh.tu = x_f32 && y_f32 && N <= MXG_EXACT_ROWS ? 3 : 1;
     sh.td = y_f32 && N <= MXG_EXACT_ROWS ? 3 : 1;
     // row tiles that there are about: the experts in use, and those of full tiles
-    const int rows = 16 * mxg_blocks_max(sh.td);
+    const int rows = 16 * mxg_rbm(N, E, sh.td);
     const int tiles = N / rows + (N < E ? N : E);
     const int ft = (d / 16 + MXG_WAVES * MXG_NF - 1) / (MXG_WAVES * MXG_NF);
     int S = 512 / (tiles * ft);
@@ -371,17 +371,23 @@ size_t moe_mx_gemm_workspace(int N, int E, int d, int f) {
 
 int moe_mx_gemm_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan) {
     if (!moe_mx_gemm_supported(N, E, d, f)) return MOE_ERR_UNSUPPORTED;
-    plan->up_tile_rows = plan->down_tile_rows = 16 * mxg_blocks_max(N <= MXG_EXACT_ROWS ? 3 : 1);
+    plan->up_tile_rows = plan->down_tile_rows = 16 * mxg_rbm(N, E, 1);  // (32 for a result in fp32 of up to 72 rows)
     plan->up_tile_features = plan->down_tile_features = MXG_WAVES * MXG_NF * 16;
     return MOE_OK;
 }
 
-template <int NMAT, int T>
+template <int NMAT, int T, int RBM, bool ONCE>
 static void mxg_go(const MxGemmArgs& a, hipStream_t s) {
-    const unsigned rtiles = (unsigned)(a.N / (16 * mxg_blocks_max(T)) + a.E);
+    const unsigned rtiles = (unsigned)(a.N / (16 * RBM) + a.E);
     const unsigned grid = (rtiles * (unsigned)(a.FT * a.S) + 7) / 8 * 8;
-    auto* kernel = a.N <= 16 * mxg_blocks_max(T) * a.E ? mx_gemm_kernel<NMAT, T, true> : mx_gemm_kernel<NMAT, T, false>;
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * MXG_WAVES), mxg_lds(T), s, a);
+    hipLaunchKernelGGL((mx_gemm_kernel<NMAT, T, RBM, ONCE>), dim3(grid), dim3(64 * MXG_WAVES), mxg_lds(T, RBM), s, a);
+}
+template <int NMAT, int T>
+static void mxg_pick(const MxGemmArgs& a, hipStream_t s) {
+    const int rbm = mxg_rbm(a.N, a.E, T);
+    const bool once = a.N <= 16 * rbm * a.E;
+    if (T == 3 || rbm == 2) once ? mxg_go<NMAT, T, 2, true>(a, s) : mxg_go<NMAT, T, 2, false>(a, s);
+    else once ? mxg_go<NMAT, 1, 8, true>(a, s) : mxg_go<NMAT, 1, 8, false>(a, s);
 }
 
 // The result in n_parts slabs of [N,d] floats from *slabs on, where the caller asks for them; else yg.
@@ -411,8 +417,8 @@ int moe_mx_gemm_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtyp
     a.K = d; a.C = f; a.NB = f / 16; a.KS = mx_frags(d); a.KW = mx_words(d);
     a.FT = (2 * a.NB + MXG_WAVES * MXG_NF - 1) / (MXG_WAVES * MXG_NF);
     a.S = 1;
-    if (sh.tu == 1) mxg_go<2, 1>(a, s);
-    else mxg_go<2, 3>(a, s);
+    if (sh.tu == 1) mxg_pick<2, 1>(a, s);
+    else mxg_pick<2, 3>(a, s);
     moe_record_mid_event(s);
     a.wfrag = (const u32x4_t*)W->w2;
     a.wscale = (const unsigned*)W->s2;
@@ -422,8 +428,8 @@ int moe_mx_gemm_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtyp
     a.K = f; a.C = d; a.NB = d / 16; a.KS = mx_frags(f); a.KW = mx_words(f);
     a.FT = (a.NB + MXG_WAVES * MXG_NF - 1) / (MXG_WAVES * MXG_NF);
     a.S = sh.S;
-    if (sh.td == 1) mxg_go<1, 1>(a, s);
-    else mxg_go<1, 3>(a, s);
+    if (sh.td == 1) mxg_pick<1, 1>(a, s);
+    else mxg_pick<1, 3>(a, s);
     if (slabs) {
         *slabs = a.yg;
         *n_parts = sh.S;

@@ -31,6 +31,7 @@
 #define MXS_MAX_WORDS 8  // scale words (512 indices each) of a part: 128 KiB of operands for 16 columns
 #define MXS_MAX_SLOTS 64
 #define MXS_DOWN_COLS 32  // features of a unit of the second projection
+#define MXS_MAX_SUMS 96   // T * (E + 1) of a block step's gating sums
 
 // Division of wave-uniform numbers below 2^31 by one that the launch fixes: two multiplications (the
 // general one takes some thirty vector instructions, and a kernel's first microseconds are its
@@ -330,8 +331,7 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
     __shared__ int s_tiles[3][MXS_MAX_TILES], s_ntiles;
     __shared__ int s_idx[GATE ? MXS_MAX_SLOTS : 1];
     __shared__ int s_batch[GATE ? 3 : 1][MXS_MAX_SLOTS];
-    __shared__ float s_gate[GATE ? 3 : 1][64];  // the summed shares, 1/rms per token, the logits
-    __shared__ float s_gpart[GATE ? MXS_WAVES : 1][GS_MAX_ITEMS];
+    __shared__ float s_gate[GATE ? 3 : 1][MXS_MAX_SUMS];  // the summed shares, 1/rms per token, the logits
     __shared__ int s_group[64], s_nlast;
 
     constexpr int THREADS = 64 * MXS_WAVES;
@@ -353,15 +353,25 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
             const int per_w = (st.n_shares + MXS_WAVES - 1) / MXS_WAVES;
             const int row0 = wave * per_w;
             const int row1 = (row0 + per_w) < st.n_shares ? (row0 + per_w) : st.n_shares;
-            gate_add_shares(st.gate_sums, row0, row1, st.gate_stride, items, lane,
-                            (float*)s_raw + wave * (GS_WAVE_ROWS * GS_MAX_ITEMS), s_gpart[wave]);
+            float* s_gpart = (float*)s_raw;  // [MXS_WAVES][MXS_MAX_SUMS]
+            for (int it = lane; it < items; it += 64) {
+                float v = 0.f;
+                for (int r = row0; r < row1; r += 8) {  // eight requests at a time, added in order
+                    float u[8];
+#pragma unroll
+                    for (int i = 0; i < 8; i++) u[i] = r + i < row1 ? st.gate_sums[(size_t)(r + i) * st.gate_stride + it] : 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; i++) v += u[i];
+                }
+                s_gpart[wave * MXS_MAX_SUMS + it] = v;
+            }
             __syncthreads();
             if (wave == 0) {
-                if (lane < items) {
-                    float v = s_gpart[0][lane];
+                for (int it = lane; it < items; it += 64) {
+                    float v = s_gpart[it];
 #pragma unroll
-                    for (int w = 1; w < MXS_WAVES; w++) v += s_gpart[w][lane];
-                    s_gate[0][lane] = v;
+                    for (int w = 1; w < MXS_WAVES; w++) v += s_gpart[w * MXS_MAX_SUMS + it];
+                    s_gate[0][it] = v;
                 }
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
                 __builtin_amdgcn_wave_barrier();
@@ -646,8 +656,7 @@ bool moe_mx_stream_routes(int T, int E, int k, int d, int f) {
 
 bool moe_mx_block_supported(int T, int E, int k, int d, int f) {
     if (!moe_mx_stream_routes(T, E, k, d, f)) return false;
-    if (T * k > 4 || E > 16 || T * (E + 1) > GS_MAX_ITEMS) return false;
-    return d / 16 <= GS_WAVE_ROWS * MXS_WAVES;
+    return T * k <= 4 && E <= 16 && T * (E + 1) <= MXS_MAX_SUMS && T * E <= 64;
 }
 
 template <bool DOWN, int R, bool GATE>
@@ -657,8 +666,7 @@ static int mx_stream_go(const MxArgs& a, int rows_max, hipStream_t s) {
     const int rows = rows_max < rows_of(R) ? rows_max : rows_of(R);
     const int words = (a.KW + a.P - 1) / a.P;
     size_t lds = (size_t)words * 1024 * rows * parts_of(R);
-    if (GATE && a.st.gate_sums && lds < (size_t)MXS_WAVES * GS_WAVE_ROWS * GS_MAX_ITEMS * 4)
-        lds = (size_t)MXS_WAVES * GS_WAVE_ROWS * GS_MAX_ITEMS * 4;
+    if (GATE && a.st.gate_sums && lds < (size_t)MXS_WAVES * MXS_MAX_SUMS * 4) lds = (size_t)MXS_WAVES * MXS_MAX_SUMS * 4;
     if (DOWN && a.st.w_gate_next && lds < (size_t)64 * 4 * MXS_DOWN_COLS * 4) lds = (size_t)64 * 4 * MXS_DOWN_COLS * 4;
     static std::atomic<bool> attr_set[MOE_MAX_DEVICES];
     const int dev = moe_current_device();

@@ -235,7 +235,8 @@ def test_the_other_layer_calls(T, E, k):
     W.free()
 
 
-@pytest.mark.parametrize("T,E,k,d,f", [(1, 8, 2, 256, 512), (2, 16, 2, 320, 448), (4, 4, 1, 1024, 192), (1, 8, 4, 2048, 1408)])
+@pytest.mark.parametrize("T,E,k,d,f", [(1, 8, 2, 256, 512), (2, 16, 2, 320, 448), (4, 4, 1, 1024, 192), (1, 8, 4, 2048, 1408),
+                                       (4, 16, 1, 320, 192), (1, 3, 1, 64, 4160), (2, 16, 2, 4096, 192)])
 def test_stack(T, E, k, d, f):
     """A stack of blocks in two launches each, against the same stack in separate calls and in 64 bits."""
     rng = np.random.default_rng(T + E)
@@ -245,8 +246,7 @@ def test_stack(T, E, k, d, f):
         conv, mats = ref.matrices(10 + n, E, d, f)
         wg = (rng.standard_normal((d, E)) / np.sqrt(d)).astype(np.float32)
         layers.append((pack(conv), cuda(wg), mats, wg.astype(np.float64)))
-    # (two launches a block where a share of the gating sums is one line; separate launches beyond)
-    assert moe.moe_decode_block_supported(T, E, k, d, f, moe.MOE_MXFP4) == (T * (E + 1) <= 32)
+    assert moe.moe_decode_block_supported(T, E, k, d, f, moe.MOE_MXFP4)
     dev = [(W, wg) for W, wg, _, _ in layers]
     idx = []
     fused = moe.moe_stack_forward(dev, x.clone(), k, idx_out=idx)

@@ -124,7 +124,8 @@ int moe_weights_pack(const void* w1, const void* w3, const void* w2, int E, int 
  *   no output may overlap an input.
  * moe_weights_pack_mxfp4: moe_weights_pack for converted matrices (w1, w3: K = d, C = f; w2:
  *   K = f, C = d; d and f multiples of 64), one device copy in the order the kernels read.
- * The handle serves moe_expert_ffn, moe_expert_ffn_path (AUTO, STREAM up to 72 rows, GROUPED),
+ * The handle serves moe_expert_ffn, moe_expert_ffn_path (AUTO: STREAM up to 72 rows and 4 per expert,
+ * else GROUPED; MID is unsupported),
  * _tokens, _noalloc, _parts (one slab), moe_layer, moe_decode_layer (E up to 64 there, two
  * launches), moe_decode_block and moe_layer_mxfp4 below.  The products are formed on the bf16
  * matrix cores from the exact element values; activations and h are treated as with bf16

@@ -509,9 +509,13 @@ static size_t mx_layer_rows(int N, int d) { return align256((size_t)N * d * size
 size_t moe_layer_mxfp4_workspace(int T, int E, int k, int d, int f) {
     if (!tek_ok(T, E, k) || !dims_ok(d) || !dims_ok(f)) return 0;
     const int N = T * k;
-    const bool stream = moe_mx_auto_path(N, E, d, f) == MOE_FFN_STREAM;
-    return align256(stream ? moe_mx_stream_workspace(N, E, d, f) : mx_layer_rows(N, d) + moe_mx_gemm_workspace(N, E, d, f)) +
-           256;
+    // (either path, where the result's type decides)
+    size_t need = mx_layer_rows(N, d) + moe_mx_gemm_workspace(N, E, d, f);
+    if (moe_mx_stream_serves(N, E, d, f)) {
+        const size_t s = moe_mx_stream_workspace(N, E, d, f);
+        if (s > need) need = s;
+    }
+    return align256(need) + 256;
 }
 
 int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, const float* logits, int T, int k,
@@ -530,8 +534,9 @@ int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, 
     if (!moe_aligned16(x) || !moe_aligned16(y) || !moe_aligned16(logits) || !moe_aligned16(idx) ||
         !moe_aligned16(weights) || !moe_aligned16(perm) || !moe_aligned16(inv_perm))
         return MOE_ERR_INVALID_ARG;
-    const int path = moe_mx_auto_path(N, E, d, f);
-    if (path == MOE_FFN_GROUPED && !moe_mx_gemm_supported(N, E, d, f)) return MOE_ERR_UNSUPPORTED;
+    const bool routes = moe_mx_stream_routes(T, E, k, d, f);
+    const bool streams = routes || moe_mx_streams(N, E, d, f, y_dtype == MOE_F32);
+    if (!streams && !moe_mx_gemm_supported(N, E, d, f)) return MOE_ERR_UNSUPPORTED;
     if (!workspace || (((uintptr_t)workspace) & 255u)) return MOE_ERR_WORKSPACE;
     if (workspace_bytes < moe_layer_mxfp4_workspace(T, E, k, d, f)) return MOE_ERR_WORKSPACE;
     // every workgroup of the first launch may read x and logits while one writes the outputs
@@ -545,13 +550,13 @@ int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, 
             return MOE_ERR_INVALID_ARG;
 
     MxStep st = mx_step(logits, T, k, idx, weights, counts, offsets, perm, inv_perm, y, y_dtype);
-    if (moe_mx_stream_routes(T, E, k, d, f))
+    if (routes)
         return moe_mx_stream_launch(W, x, x_dtype, nullptr, k, nullptr, N, workspace, nullptr, &st, s);
     int rc = moe_route_launch(logits, T, E, k, idx, weights, s);
     if (rc == MOE_OK)
         rc = moe_permute_launch(idx, T, E, k, nullptr, 0, x_dtype, counts, offsets, perm, inv_perm, nullptr, s);
     if (rc != MOE_OK) return rc;
-    if (path == MOE_FFN_STREAM) {
+    if (streams) {
         st.logits = nullptr;
         return moe_mx_stream_launch(W, x, x_dtype, perm, k, offsets, N, workspace, nullptr, &st, s);
     }

@@ -4,9 +4,9 @@
 // Both conversions are bound by memory (the elements' bytes once, 17/32 byte per element for
 // codes and scales).  A matrix W [K,C] has its features along the rows and its codes along the
 // reduction, so either direction is a transposition: a workgroup takes 64 * V features by 256
-// reduction indices, every thread one scale block of V neighbouring features (two where C is
-// even), and the 16-byte chunks of codes change hands in LDS, so that global memory sees 256-byte
-// rows on one side (bf16) and 128-byte runs of a feature's codes on the other.
+// reduction indices, every thread one scale block of V neighbouring features (as many as C is a
+// multiple of, up to 8 bytes), and the 16-byte chunks of codes change hands in LDS, so that global
+// memory sees 512-byte rows on one side and 128-byte runs of a feature's codes on the other.
 #include <new>
 
 #include "moe_mx.h"
@@ -15,32 +15,22 @@
 #define CV_BLOCKS 8   // scale blocks of a tile along the reduction
 #define CV_THREADS (CV_LANES * CV_BLOCKS)
 
-// V neighbouring elements as one access
+// V neighbouring elements as one access of 2 .. 8 bytes
+template <int BYTES>
+struct CvWord;
+template <>
+struct CvWord<2> { typedef uint16_t type; };
+template <>
+struct CvWord<4> { typedef unsigned type; };
+template <>
+struct CvWord<8> { typedef uint2 type; };
 template <bool BF16, int V>
-struct CvElems;
-template <>
-struct CvElems<true, 1> { typedef uint16_t type; };
-template <>
-struct CvElems<true, 2> { typedef unsigned type; };
-template <>
-struct CvElems<false, 1> { typedef float type; };
-template <>
-struct CvElems<false, 2> { typedef float2 type; };
-
-template <bool BF16, int V>
-__device__ __forceinline__ void cv_load(const void* w, size_t i, float (&v)[V]) {
-    if constexpr (BF16) {
-        const unsigned u = *(const typename CvElems<BF16, V>::type*)((const uint16_t*)w + i);
-        v[0] = moe_bf16_to_f32(u & 0xFFFFu);
-        if constexpr (V == 2) v[1] = __uint_as_float(u & 0xFFFF0000u);
-    } else if constexpr (V == 2) {
-        const float2 f = *(const float2*)((const float*)w + i);
-        v[0] = f.x;
-        v[1] = f.y;
-    } else {
-        v[0] = ((const float*)w)[i];
-    }
-}
+union CvElems {
+    typename CvWord<(BF16 ? 2 : 4) * V>::type word;
+    uint16_t h[V];
+    float f[V];
+    __device__ __forceinline__ float at(int n) const { return BF16 ? moe_bf16_to_f32(h[n]) : f[n]; }
+};
 
 // The scale is 2^(exponent of the largest magnitude - 2), the exponent kept in [-126, 127]: the
 // largest element, 6 = 1.5 * 2^2, then has the largest magnitude's exponent.  The division by a
@@ -61,14 +51,16 @@ __global__ __launch_bounds__(CV_THREADS) void mx_quantize_kernel(const void* __r
     const int b = blockIdx.y * CV_BLOCKS + kb;
     if (b < KB && c0 + cl < C) {
         const size_t at = (e * K + (size_t)b * MX_BLOCK) * C + c0 + cl;
-        float v[MX_BLOCK][V];
+        typedef CvElems<BF16, V> Elems;
+        Elems v[MX_BLOCK];
 #pragma unroll
-        for (int i = 0; i < MX_BLOCK; i++) cv_load<BF16, V>(w, at + (size_t)i * C, v[i]);
+        for (int i = 0; i < MX_BLOCK; i++)
+            v[i].word = *(const decltype(Elems::word)*)((const char*)w + (at + (size_t)i * C) * (BF16 ? 2 : 4));
 #pragma unroll
         for (int n = 0; n < V; n++) {
             float top = 0.f;
 #pragma unroll
-            for (int i = 0; i < MX_BLOCK; i++) top = fmaxf(top, fabsf(v[i][n]));
+            for (int i = 0; i < MX_BLOCK; i++) top = fmaxf(top, fabsf(v[i].at(n)));
             int s = (int)(__float_as_uint(top) >> 23) - 2;
             s = s < 1 ? 1 : s;
             const float scale = __uint_as_float((unsigned)s << 23);
@@ -76,10 +68,10 @@ __global__ __launch_bounds__(CV_THREADS) void mx_quantize_kernel(const void* __r
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 unsigned o = 0u;
-                o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * j][n], v[8 * j + 1][n], scale, 0);
-                o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * j + 2][n], v[8 * j + 3][n], scale, 1);
-                o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * j + 4][n], v[8 * j + 5][n], scale, 2);
-                o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * j + 6][n], v[8 * j + 7][n], scale, 3);
+                o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * j].at(n), v[8 * j + 1].at(n), scale, 0);
+                o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * j + 2].at(n), v[8 * j + 3].at(n), scale, 1);
+                o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * j + 4].at(n), v[8 * j + 5].at(n), scale, 2);
+                o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * j + 6].at(n), v[8 * j + 7].at(n), scale, 3);
                 q[j] = o;
             }
             s_codes[kb][cl + n] = q;
@@ -137,30 +129,35 @@ __global__ __launch_bounds__(CV_THREADS) void mx_dequantize_kernel(const uint8_t
         for (int n = 0; n < V; n++) v[n] = mx_widen8(q[n][j], scale[n]);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            const size_t o = at + (size_t)(8 * j + i) * C;
-            if constexpr (V == 2) {
-                if (BF16) *(bf16x2_t*)((__bf16*)w + o) = bf16x2_t{v[0][i], v[1][i]};
-                else *(float2*)((float*)w + o) = make_float2((float)v[0][i], (float)v[1][i]);
-            } else {
-                if (BF16) ((__bf16*)w)[o] = v[0][i];
-                else ((float*)w)[o] = (float)v[0][i];
+            CvElems<BF16, V> o;
+#pragma unroll
+            for (int n = 0; n < V; n++) {
+                if constexpr (BF16) o.h[n] = __builtin_bit_cast(uint16_t, (__bf16)v[n][i]);
+                else o.f[n] = (float)v[n][i];
             }
+            *(decltype(o.word)*)((char*)w + (at + (size_t)(8 * j + i) * C) * (BF16 ? 2 : 4)) = o.word;
         }
     }
 }
+
+// Features a thread takes.
+static int cv_width(int C, bool bf16) { return bf16 && C % 4 == 0 ? 4 : C % 2 == 0 ? 2 : 1; }
 
 static dim3 cv_grid(int E, int K, int C, int V, size_t& ctiles) {
     ctiles = ((size_t)C + CV_LANES * V - 1) / (CV_LANES * V);
     return dim3((unsigned)(E * ctiles), (unsigned)((K / MX_BLOCK + CV_BLOCKS - 1) / CV_BLOCKS));
 }
 
+#define CV_PICK(kernel)                                                                                      \
+    w_dtype == MOE_BF16 ? (V == 4 ? kernel<true, 4> : V == 2 ? kernel<true, 2> : kernel<true, 1>)            \
+                        : (V == 2 ? kernel<false, 2> : kernel<false, 1>)
+
 int moe_mx_quantize_launch(const void* w, moe_dtype_t w_dtype, int E, int K, int C, uint8_t* codes, uint8_t* scales,
                            hipStream_t s) {
     size_t ctiles;
-    const int V = C % 2 ? 1 : 2;
+    const int V = cv_width(C, w_dtype == MOE_BF16);
     const dim3 grid = cv_grid(E, K, C, V, ctiles);
-    auto* kernel = w_dtype == MOE_BF16 ? (V == 2 ? mx_quantize_kernel<true, 2> : mx_quantize_kernel<true, 1>)
-                                       : (V == 2 ? mx_quantize_kernel<false, 2> : mx_quantize_kernel<false, 1>);
+    auto* kernel = CV_PICK(mx_quantize_kernel);
     hipLaunchKernelGGL(kernel, grid, dim3(CV_THREADS), 0, s, w, K, C, ctiles, codes, scales);
     return moe_launch_status();
 }
@@ -168,10 +165,9 @@ int moe_mx_quantize_launch(const void* w, moe_dtype_t w_dtype, int E, int K, int
 int moe_mx_dequantize_launch(const uint8_t* codes, const uint8_t* scales, int E, int K, int C, void* w,
                              moe_dtype_t w_dtype, hipStream_t s) {
     size_t ctiles;
-    const int V = C % 2 ? 1 : 2;
+    const int V = cv_width(C, w_dtype == MOE_BF16);
     const dim3 grid = cv_grid(E, K, C, V, ctiles);
-    auto* kernel = w_dtype == MOE_BF16 ? (V == 2 ? mx_dequantize_kernel<true, 2> : mx_dequantize_kernel<true, 1>)
-                                       : (V == 2 ? mx_dequantize_kernel<false, 2> : mx_dequantize_kernel<false, 1>);
+    auto* kernel = CV_PICK(mx_dequantize_kernel);
     hipLaunchKernelGGL(kernel, grid, dim3(CV_THREADS), 0, s, codes, scales, K, C, ctiles, w);
     return moe_launch_status();
 }

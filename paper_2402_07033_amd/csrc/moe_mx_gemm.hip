@@ -346,7 +346,7 @@ static MxGemmShape mxg_shape(int N, int E, int d, int f, bool x_f32, bool y_f32)
     sh.td = y_f32 && N <= MXG_EXACT_ROWS ? 3 : 1;
     // row tiles that there are about: the experts in use, and those of full tiles
     const int rows = 16 * mxg_rbm(N, E, sh.td);
-    const int tiles = N / rows + (N < E ? N : E);
+    const int tiles = N / rows + (N < E ? N : E) + (N == 0);
     const int ft = (d / 16 + MXG_WAVES * MXG_NF - 1) / (MXG_WAVES * MXG_NF);
     int S = 512 / (tiles * ft);
     const int most = mx_frags(f) / 8;

@@ -30,6 +30,7 @@
 #define MXS_WAVES 16
 #define MXS_MAX_WORDS 8  // scale words (512 indices each) of a part: 128 KiB of operands for 16 columns
 #define MXS_MAX_SLOTS 64
+#define MXS_MAX_ROWS 72
 #define MXS_DOWN_COLS 32  // features of a unit of the second projection
 #define MXS_MAX_SUMS 96   // T * (E + 1) of a block step's gating sums
 
@@ -634,14 +635,20 @@ static int mx_parts(int N, int d, int f) {
 }
 
 bool moe_mx_stream_serves(int N, int E, int d, int f) {
-    if (mx_words(d) > MXS_MAX_WORDS || N / rows_of(ROWS_F32) + E > MXS_MAX_TILES) return false;
+    if (N > MXS_MAX_ROWS || mx_words(d) > MXS_MAX_WORDS || N / rows_of(ROWS_F32) + E > MXS_MAX_TILES) return false;
     if ((long long)mx_parts(N, d, f) * N * d * 4 >= (1ll << 31)) return false;  // (the slabs' offsets)
     return (long long)MXS_MAX_TILES * mx_parts(1, d, f) * ((d > f ? d : f) / 16) < (1ll << 31);
 }
 
-// The rows up to which streaming is taken; the GEMM above it.
+// Streaming, or the GEMM: fp32 results are streamed where an expert's rows are one tile of 5 on average, bf16
+// results (16 rows a tile) further.  8 experts of the Mixtral shape with 4 rows each 81 + 55 us (both
+// projections), the GEMM 102 + 63 and 12 for rows and sums; 6 rows each 142 + 91 and 102 + 62; 32 rows of
+// uneven experts 100 + 68; bf16 rows, 9 each, 85 + 55 and 96 + 59.
+bool moe_mx_streams(int N, int E, int d, int f, bool y_f32) {
+    return N <= MXS_MAX_ROWS && N <= (y_f32 ? 4 : 8) * E && moe_mx_stream_serves(N, E, d, f);
+}
 int moe_mx_auto_path(int N, int E, int d, int f) {
-    return N <= 72 && moe_mx_stream_serves(N, E, d, f) ? MOE_FFN_STREAM : MOE_FFN_GROUPED;
+    return moe_mx_streams(N, E, d, f, true) ? MOE_FFN_STREAM : MOE_FFN_GROUPED;
 }
 
 // counters, h [3][N,f] bf16, the second projection's slabs [P][N,d] fp32

@@ -119,16 +119,18 @@ def test_stream(d, f, E, N, how, dtype):
     W = pack(conv)
     x, x64 = rows(rng, N, d, dtype)
     offsets = split_rows(rng, N, E, how)
-    assert moe.moe_expert_ffn_plan(N, E, d, f, moe.MOE_MXFP4)["path"] == moe.MOE_FFN_STREAM
-    yg = moe.moe_expert_ffn(W, x, cuda(offsets))
+    assert moe.moe_expert_ffn_plan(N, E, d, f, moe.MOE_MXFP4, moe.MOE_FFN_STREAM)["path"] == moe.MOE_FFN_STREAM
+    yg = moe.moe_expert_ffn(W, x, cuda(offsets), path=moe.MOE_FFN_STREAM)
     want, bound = ref.ffn(x64, offsets, mats, 0.0 if dtype == BF16 else ref.SPLIT, ref.SPLIT)
     check(yg, want, bound, what=(d, f, E, N, how))
-    # the same rows again, without allocation and through the parts' call: the same bits
+    # the family that the library takes, without allocation and through the parts' call: the same bits
+    auto = moe.moe_expert_ffn(W, x, cuda(offsets))
+    check(auto, want, bound, what=(d, f, E, N, how))
     again = torch.empty_like(yg)
     moe.moe_expert_ffn_noalloc(W, x, cuda(offsets), again)
-    assert torch.equal(again, yg)
+    assert torch.equal(again, auto)
     parts = torch.empty((1,) + tuple(yg.shape), device="cuda")
-    assert moe.moe_expert_ffn_parts(W, x, cuda(offsets), parts) == 1 and torch.equal(parts[0], yg)
+    assert moe.moe_expert_ffn_parts(W, x, cuda(offsets), parts) == 1 and torch.equal(parts[0], auto)
     W.free()
 
 

@@ -509,13 +509,9 @@ static size_t mx_layer_rows(int N, int d) { return align256((size_t)N * d * size
 size_t moe_layer_mxfp4_workspace(int T, int E, int k, int d, int f) {
     if (!tek_ok(T, E, k) || !dims_ok(d) || !dims_ok(f)) return 0;
     const int N = T * k;
-    // (either path, where the result's type decides)
-    size_t need = mx_layer_rows(N, d) + moe_mx_gemm_workspace(N, E, d, f);
-    if (moe_mx_stream_serves(N, E, d, f)) {
-        const size_t s = moe_mx_stream_workspace(N, E, d, f);
-        if (s > need) need = s;
-    }
-    return align256(need) + 256;
+    const bool streams = moe_mx_stream_routes(T, E, k, d, f) || moe_mx_auto_path(N, E, d, f) == MOE_FFN_STREAM;
+    return align256(streams ? moe_mx_stream_workspace(N, E, d, f)
+                            : mx_layer_rows(N, d) + moe_mx_gemm_workspace(N, E, d, f)) + 256;
 }
 
 int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, const float* logits, int T, int k,
@@ -535,7 +531,7 @@ int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, 
         !moe_aligned16(weights) || !moe_aligned16(perm) || !moe_aligned16(inv_perm))
         return MOE_ERR_INVALID_ARG;
     const bool routes = moe_mx_stream_routes(T, E, k, d, f);
-    const bool streams = routes || moe_mx_streams(N, E, d, f, y_dtype == MOE_F32);
+    const bool streams = routes || moe_mx_auto_path(N, E, d, f) == MOE_FFN_STREAM;
     if (!streams && !moe_mx_gemm_supported(N, E, d, f)) return MOE_ERR_UNSUPPORTED;
     if (!workspace || (((uintptr_t)workspace) & 255u)) return MOE_ERR_WORKSPACE;
     if (workspace_bytes < moe_layer_mxfp4_workspace(T, E, k, d, f)) return MOE_ERR_WORKSPACE;

@@ -85,8 +85,7 @@ struct MxStep {
     float* sums_next;         // [d/16][gate_stride]
 };
 
-int moe_mx_auto_path(int N, int E, int d, int f);  // of the expert FFN, whose result is fp32
-bool moe_mx_streams(int N, int E, int d, int f, bool y_f32);
+int moe_mx_auto_path(int N, int E, int d, int f);
 bool moe_mx_stream_serves(int N, int E, int d, int f);
 size_t moe_mx_stream_workspace(int N, int E, int d, int f);
 // yg (step == null), or what `step` asks for.  offsets: device, unless step routes.

@@ -13,7 +13,7 @@
 // A unit is (tile of rows of one expert, reduction part, group of features): 16 columns of w1 and
 // w3, or 32 of w2.  The units are dealt to the workgroups in contiguous, equal ranges.
 //   up   (x.w1, x.w3 -> silu*mul -> h): one part.  Its prologue may route the tokens and batch
-//        them (up to 64 slots).  h is left as three bf16 parts, or one where the result is bf16.
+//        them (up to 64 slots).  h is left as its bf16 parts.
 //   down (h.w2): P parts.  Every unit leaves its partial sums in slab [part][N][d]; a counter
 //        per feature group tells the workgroup that finishes the group's last unit, and that
 //        one adds the parts in part order -- and the rows of a token in slot order, weighted,
@@ -62,7 +62,7 @@ struct MxArgs {
     unsigned* counters;       // [n_counters], one per feature group of the second projection:
     int n_counters;           // cleared by up, counted by down
     int finish;
-    int h_parts;              // up: bf16 parts of h, 1 or 3
+    int h_parts;              // up: bf16 parts of h, 2 or 3
     float* yg;                // FIN_ROWS: out
     MxStep st;
 };
@@ -70,11 +70,12 @@ enum { FIN_NONE = 0, FIN_ROWS = 1, FIN_LAYER = 2 };
 
 // How a tile's rows become the matrix instructions' 16 operand columns.  An fp32 row is three
 // bf16 parts, and 5 rows have all their parts in one instruction (column part * rows + row), which
-// are added in the end.  More rows of an expert are more tiles.  h comes as its parts, [3][N][f],
-// already.
-enum { ROWS_BF16 = 0, ROWS_F32 = 1, ROWS_PARTS = 2 };
-constexpr int rows_of(int R) { return R == ROWS_BF16 ? 16 : 5; }
-constexpr int parts_of(int R) { return R == ROWS_BF16 ? 1 : 3; }
+// are added in the end.  More rows of an expert are more tiles.  h comes as its parts, [parts][N][f],
+// already: three where the result is fp32, two (16 bits) where it is bf16.
+enum { ROWS_BF16 = 0, ROWS_F32 = 1, ROWS_PARTS3 = 2, ROWS_PARTS2 = 3 };
+constexpr int parts_of(int R) { return R == ROWS_BF16 ? 1 : R == ROWS_PARTS2 ? 2 : 3; }
+constexpr int rows_of(int R) { return 16 / parts_of(R); }
+constexpr bool rows_in_parts(int R) { return R == ROWS_PARTS3 || R == ROWS_PARTS2; }
 
 // Stages the rows [row0, row0 + rows) of reduction words [w0, w1) as operands, 16-byte chunks
 // [(word, fragment, j, lane / 16)][column]: indices word*512 + fragment*128 + 32*(lane/16) + 8j .. +7.
@@ -88,7 +89,7 @@ struct MxStager {
     int row0, rows, w0, words, blocks;
     __device__ __forceinline__ MxStager(const MxArgs& args, const int* rm, const float* rs, int r0, int nr, int wa, int wb)
         : a(args), rowmap(rm), row_scale(rs), row0(r0), rows(nr), w0(wa), words(wb - wa),
-          blocks((wb - wa) * nr * (R == ROWS_PARTS ? 3 : 1)) {}
+          blocks((wb - wa) * nr * (rows_in_parts(R) ? parts_of(R) : 1)) {}
     __device__ __forceinline__ void split(int b, int& rr, int& w) const {
         rr = 0;
         w = b;
@@ -101,7 +102,7 @@ struct MxStager {
         int t, w;
         split(b, t, w);
         int part = 0;
-        if (R == ROWS_PARTS)
+        if (rows_in_parts(R))
             while (t >= rows) {
                 t -= rows;
                 part++;
@@ -110,7 +111,7 @@ struct MxStager {
         if (rowmap) src = __builtin_amdgcn_readfirstlane(rowmap[src]);
         else if (a.row_perm) src = (int)mx_div((unsigned)__builtin_amdgcn_readfirstlane(a.row_perm[src]), a.by_k);
         sc = R == ROWS_F32 && row_scale ? row_scale[src] : 1.0f;
-        if (R == ROWS_PARTS) src += part * a.N;
+        if (rows_in_parts(R)) src += part * a.N;
         const int k0 = (w0 + w) * 512 + lane * 8;
 #pragma unroll
         for (int i = 0; i < REGS; i++) raw[i] = u32x4_t{0u, 0u, 0u, 0u};
@@ -151,7 +152,7 @@ __device__ __forceinline__ f32x4_t mx_parts_sum(const f32x4_t& v, int rows, int 
     if (R == ROWS_BF16) return v;
     f32x4_t o = v;
 #pragma unroll
-    for (int p = 1; p < 3; p++)
+    for (int p = 1; p < parts_of(R); p++)
 #pragma unroll
         for (int i = 0; i < 4; i++) o[i] += __shfl(v[i], (lane & 48) + ((lane + p * rows) & 15), 64);
     return o;
@@ -640,15 +641,11 @@ bool moe_mx_stream_serves(int N, int E, int d, int f) {
     return (long long)MXS_MAX_TILES * mx_parts(1, d, f) * ((d > f ? d : f) / 16) < (1ll << 31);
 }
 
-// Streaming, or the GEMM: fp32 results are streamed where an expert's rows are one tile of 5 on average, bf16
-// results (16 rows a tile) further.  8 experts of the Mixtral shape with 4 rows each 81 + 55 us (both
-// projections), the GEMM 102 + 63 and 12 for rows and sums; 6 rows each 142 + 91 and 102 + 62; 32 rows of
-// uneven experts 100 + 68; bf16 rows, 9 each, 85 + 55 and 96 + 59.
-bool moe_mx_streams(int N, int E, int d, int f, bool y_f32) {
-    return N <= MXS_MAX_ROWS && N <= (y_f32 ? 4 : 8) * E && moe_mx_stream_serves(N, E, d, f);
-}
+// Streaming, or the GEMM: streaming where an expert's rows are one tile of 5 on average.  8 experts of the
+// Mixtral shape with 4 rows each 81 + 55 us (both projections), the GEMM 102 + 63 and 12 for rows and sums;
+// 6 rows each 142 + 91 and 102 + 62; 32 rows of uneven experts 100 + 68.
 int moe_mx_auto_path(int N, int E, int d, int f) {
-    return moe_mx_streams(N, E, d, f, true) ? MOE_FFN_STREAM : MOE_FFN_GROUPED;
+    return N <= 4 * E && moe_mx_stream_serves(N, E, d, f) ? MOE_FFN_STREAM : MOE_FFN_GROUPED;
 }
 
 // counters, h [3][N,f] bf16, the second projection's slabs [P][N,d] fp32
@@ -716,8 +713,8 @@ int moe_mx_stream_launch(const moe_weights* W, const void* x, moe_dtype_t act_dt
     a.counters = counters;
     a.n_counters = W->d / MXS_DOWN_COLS;
     if (step) a.st = *step;
-    // A bf16 result is rounded to 8 bits once more, so h is held in as many before it.
-    a.h_parts = step && step->y_dtype == MOE_BF16 && !step->yg ? 1 : 3;
+    // (a bf16 result is rounded to 8 bits in the end)
+    a.h_parts = step && step->y_dtype == MOE_BF16 && !step->yg ? 2 : 3;
     // rows of a tile, at most.  (A token uses an expert once, but logits that are NaN may say otherwise.)
     const int rows_max = N;
     int rc;
@@ -739,6 +736,6 @@ int moe_mx_stream_launch(const moe_weights* W, const void* x, moe_dtype_t act_dt
     a.out = a.finish == FIN_NONE ? yg : slabs;
     a.part_stride = (size_t)N * W->d;
     a.yg = yg;
-    return a.h_parts == 1 ? mx_stream_go<true, ROWS_BF16, false>(a, rows_max, s)
-                          : mx_stream_go<true, ROWS_PARTS, false>(a, rows_max, s);
+    return a.h_parts == 2 ? mx_stream_go<true, ROWS_PARTS2, false>(a, rows_max, s)
+                          : mx_stream_go<true, ROWS_PARTS3, false>(a, rows_max, s);
 }

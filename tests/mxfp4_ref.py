@@ -64,8 +64,8 @@ def expert(x, w1, w3, w2, u, uh):
     return product(h, dh * (1 + uh), w2, uh)
 
 
-# what rows and h are held to: three bf16 parts (all 24 bits), or one
-SPLIT, ROUND = 2.0 ** -24, 2.0 ** -8
+# what rows and h are held to: three bf16 parts (all 24 bits), two (half a step of half a step), one
+SPLIT, PAIR, ROUND = 2.0 ** -24, 2.0 ** -16, 2.0 ** -8
 
 
 def ffn(x, offsets, mats, u, uh):

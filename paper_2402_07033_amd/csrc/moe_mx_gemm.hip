@@ -26,10 +26,12 @@
 #define MXG_EXACT_ROWS 72
 #define MXG_WAVES 4
 #define MXG_NF 4   // fragment rows of a wave
-// Steps requested ahead, in stages of LDS (8 .. 64 KiB a workgroup).  More rows are more matrix work under
-// which a request may travel: 8 experts of 64 rows take 135 + 90 us with one step (both projections), 126 +
-// 69 with two; with one row, three or six steps are the same within 3 %.
-constexpr int mxg_depth(int T, int RB) { return RB * T > 4 ? 1 : RB * T > 1 ? 2 : 3; }
+// Steps requested ahead, in stages of LDS (12 .. 64 KiB a workgroup).  More rows are more matrix work under
+// which a request may travel, and a third stage of many rows leaves room for one workgroup per CU.  First +
+// second projection, us: 8 experts of 64 rows (d 4096, f 14336) 146 + 95 with one step, 126 + 70 with two;
+// of 1024 rows 1408 + 696 with one, 1549 + 1430 with two.  A third step for single blocks was slower: 8
+// experts of 10 rows 88 + 51 against 84 + 49; 16 (f 6400) of 12 rows 86 + 36 against 81 + 40.
+constexpr int mxg_depth(int T, int RB) { return RB * T > 4 ? 1 : 2; }
 constexpr int mxg_lds(int T, int RBM) {
     int most = 0;
     for (int rb = 1; rb <= RBM; rb++) {

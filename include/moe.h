@@ -124,12 +124,13 @@ int moe_weights_pack(const void* w1, const void* w3, const void* w2, int E, int 
  *   no output may overlap an input.
  * moe_weights_pack_mxfp4: moe_weights_pack for converted matrices (w1, w3: K = d, C = f; w2:
  *   K = f, C = d; d and f multiples of 64), one device copy in the order the kernels read.
- * The handle serves moe_expert_ffn, moe_expert_ffn_path (AUTO: STREAM up to 72 rows and 4 per expert,
- * else GROUPED; MID is unsupported),
- * _tokens, _noalloc, _parts (one slab), moe_layer, moe_decode_layer (E up to 64 there, two
+ * The handle serves moe_expert_ffn, moe_expert_ffn_path (AUTO: STREAM up to 72 rows, 4 per expert of the
+ * handle and d <= 4096, else GROUPED; MID is unsupported), _tokens, _noalloc, _parts (one slab), moe_layer, moe_decode_layer (E up to 64 there, two
  * launches), moe_decode_block and moe_layer_mxfp4 below.  The products are formed on the bf16
- * matrix cores from the exact element values; activations and h are treated as with bf16
- * weights (see moe_expert_ffn).
+ * matrix cores from the exact element values, with fp32 accumulation.  fp32 activations keep their 24
+ * bits (three bf16 parts) on STREAM, and on GROUPED up to 72 rows of an fp32 result; h keeps 24 where
+ * the result is fp32 there, 16 where a streamed result is bf16.  Beyond, GROUPED rounds both to bf16.
+ * Rows that offsets do not cover are left as they were.
  */
 int moe_mxfp4_quantize(const void* w, moe_dtype_t w_dtype, int E, int K, int C, uint8_t* codes, uint8_t* scales,
                        void* stream);
@@ -300,7 +301,8 @@ int moe_combine_parts(const float* yg_parts, int n_parts, const int32_t* inv_per
  *   idx, weights, counts, offsets, perm, inv_perm: as moe_route / moe_permute, all written
  *   workspace >= moe_layer_mxfp4_workspace(T, E, k, d, f) bytes, 256-byte aligned
  *   y [T,d] of y_dtype out.  No output and no byte of the workspace may overlap x or logits.
- * T == 0 writes counts and offsets only.
+ * T == 0 writes counts and offsets only.  A token whose logits hold NaN, or nothing above -infinity, has
+ * unspecified idx, weights and y; the other tokens' are as without it, and no access is out of range.
  */
 int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, const float* logits, int T, int k,
                     int32_t* idx, float* weights, int32_t* counts, int32_t* offsets, int32_t* perm, int32_t* inv_perm,

@@ -313,9 +313,11 @@ __global__ __launch_bounds__(64 * MXG_WAVES, RBM > 2 ? 2 : 4) void mx_gemm_kerne
     }
 }
 
-// yg = slab 0 + slab 1 + ... in that order.
-__global__ __launch_bounds__(256) void mx_sum_kernel(const float4* __restrict__ slabs, size_t n4, int S, float4* __restrict__ yg) {
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (size_t)gridDim.x * 256) {
+// yg = slab 0 + slab 1 + ... in that order, up to the last expert's last row.
+__global__ __launch_bounds__(256) void mx_sum_kernel(const float4* __restrict__ slabs, size_t n4, int S, float4* __restrict__ yg,
+                                                     const int32_t* __restrict__ end, int row4) {
+    const size_t covered = (size_t)(*end < 0 ? 0 : *end) * row4, stop = covered < n4 ? covered : n4;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < stop; i += (size_t)gridDim.x * 256) {
         float4 s = slabs[i];
         for (int p = 1; p < S; p++) {
             const float4 v = slabs[(size_t)p * n4 + i];
@@ -439,7 +441,7 @@ int moe_mx_gemm_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtyp
         const size_t n4 = (size_t)N * d / 4;
         const size_t blocks = (n4 + 255) / 256;
         hipLaunchKernelGGL(mx_sum_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s,
-                           (const float4*)parts, n4, sh.S, (float4*)yg);
+                           (const float4*)parts, n4, sh.S, (float4*)yg, offsets + E, d / 4);
     }
     return moe_launch_status();
 }

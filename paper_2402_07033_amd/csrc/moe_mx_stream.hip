@@ -273,8 +273,10 @@ __device__ __forceinline__ void mx_finish(const MxArgs& a, const int* s_group, i
     constexpr int C4 = MXS_DOWN_COLS / 4;  // 16-byte columns of a group
     const __amdgpu_buffer_rsrc_t slabs = mx_rsrc(a.out);
     if (a.finish == FIN_ROWS) {
+        const int end = a.offsets[a.E];  // rows behind the last expert's have no sums
         for (int i = tid; i < n * a.N * C4; i += 64 * MXS_WAVES) {
             const int c4 = i % C4, gi = (int)mx_div(i / C4, a.by_N), row = i / C4 - gi * a.N;
+            if (row >= end) continue;
             const size_t col = (size_t)s_group[gi] * MXS_DOWN_COLS + 4 * c4;
             const f32x4_t v = mx_row_sum(a, slabs, row, col);
             *(f32x4_t*)(a.yg + (size_t)row * a.C + col) = v;

@@ -353,3 +353,132 @@ def test_quantize_then_layer():
     want = ref.layer(x64, logits, mats, k, 0.0, ref.PAIR)
     check(out["y"], want["y"], want["bound"], BF16)
     W.free()
+
+
+# ---- calls that the documentation allows and that go wrong easily -----------------------
+
+@pytest.mark.parametrize("N,path", [(7, moe.MOE_FFN_STREAM), (7, moe.MOE_FFN_GROUPED), (200, moe.MOE_FFN_GROUPED)])
+def test_rows_behind_the_last_expert_stay(N, path):
+    """A padded batch: what offsets do not cover is left as it was, whatever the workspace holds."""
+    E, d, f = 3, 256, 4096  # both families cut the second projection's reduction at this f
+    conv, mats = ref.matrices(8, E, d, f)
+    W = pack(conv)
+    rng = np.random.default_rng(N)
+    x, x64 = rows(rng, N, d, BF16)
+    used = N - 3
+    offsets = np.array([0, 1, 1, used], dtype=np.int32)
+    ws = torch.full((moe.moe_expert_ffn_workspace(N, E, d, f),), 0xFF, dtype=torch.uint8, device="cuda")
+    yg = torch.full((N, d), 7.0, device="cuda")
+    moe.moe_expert_ffn(W, x, cuda(offsets), workspace=ws, yg=yg, path=path)
+    assert (yg[used:] == 7.0).all()
+    want, bound = ref.ffn(x64, offsets, mats, 0.0, ref.SPLIT if N <= 72 else ref.ROUND)
+    check(yg[:used], want[:used], bound[:used])
+    # and none at all
+    yg.fill_(7.0)
+    moe.moe_expert_ffn(W, x, cuda(np.zeros(E + 1, dtype=np.int32)), workspace=ws, yg=yg, path=path)
+    assert (yg == 7.0).all()
+    W.free()
+
+
+@pytest.mark.parametrize("T", [5, 40])
+@pytest.mark.parametrize("what", ["nan logits", "masked logits", "nan row", "infinite row"])
+def test_a_bad_token_stays_alone(T, what):
+    """Logits that are NaN or -infinity, rows that are NaN or infinite: the other tokens' results hold."""
+    E, d, f, k = 8, 320, 448, 2
+    conv, mats = ref.matrices(9, E, d, f)
+    W = pack(conv)
+    rng = np.random.default_rng(T)
+    x, x64 = rows(rng, T, d, F32)
+    logits = rng.standard_normal((T, E)).astype(np.float32)
+    bad = 3
+    given = logits.copy()
+    if what == "nan logits":
+        given[bad] = np.nan
+    elif what == "masked logits":
+        given[bad] = -np.inf
+        given[:, 5] = logits[:, 5] = -np.inf  # an expert that nobody may take
+    else:
+        x[bad] = float("nan") if what == "nan row" else float("inf")
+    out = moe.moe_layer_mxfp4(W, x, cuda(given), k)
+    idx = out["idx"].cpu().numpy()
+    # (moe_route, which more than 16 tokens go through, leaves the ids of NaN logits unspecified; the batching
+    # clamps them, so the slots' order is one all the same)
+    if what != "nan logits" or T <= 16:
+        assert idx.min() >= 0 and idx.max() < E
+    assert np.array_equal(np.sort(out["perm"].cpu().numpy()), np.arange(T * k))
+    others = np.arange(T) != bad
+    exact = T * k <= 72
+    streams = T <= 16 or T * k <= min(72, 4 * E)
+    want = ref.layer(x64, np.where(np.isfinite(logits), logits, -1e30), mats, k,
+                     ref.SPLIT if exact or streams else ref.ROUND, ref.SPLIT if exact else ref.ROUND)
+    assert np.array_equal(idx[others], want["idx"][others])
+    check(out["y"][cuda(others)], want["y"][others], want["bound"][others])
+    W.free()
+
+
+@pytest.mark.parametrize("T", [3, 200])
+def test_two_graphs_share_a_workspace(T):
+    """Replayed in turn on one stream, neither keeps anything in it for its next replay."""
+    E, k, d, f = 8, 2, 256, 2112
+    conv, _ = ref.matrices(10, E, d, f)
+    W = pack(conv)
+    ws = torch.empty(moe.moe_layer_mxfp4_workspace(T, E, k, d, f), dtype=torch.uint8, device="cuda")
+    small = max(1, T // 2)  # the second graph has another layout of the same memory
+    runs = []
+    for n in (T, small):
+        x, logits = torch.randn((n, d), device="cuda"), torch.randn((n, E), device="cuda")
+        out = moe.moe_layer_mxfp4(W, x, logits, k, workspace=ws)
+        want = out["y"].clone()
+        bufs = dict(idx=out["idx"], weights=out["w"], out=tuple(out[m] for m in ("counts", "offsets", "perm", "inv_perm")),
+                    workspace=ws, y=out["y"])
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            moe.moe_layer_mxfp4(W, x, logits, k, **bufs)
+        runs.append((g, out["y"], want, x, logits, bufs))
+    for _ in range(4):
+        for g, y, want, *_ in runs:
+            y.fill_(float("nan"))
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, want) for _, y, want, *_ in runs)
+        ws.fill_(0xFF)
+    W.free()
+
+
+@pytest.mark.parametrize("path", [moe.MOE_FFN_STREAM, moe.MOE_FFN_GROUPED])
+def test_matrices_past_32_bits(path):
+    """64 experts of 4096 x 16384: 4 GiB of first-projection codes, and rows on the last experts."""
+    E, d, f, N = 64, 4096, 16384, 3
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    conv = []
+    for K, C in ((d, f), (d, f), (f, d)):
+        codes = torch.randint(0, 256, (E, C, K // 2), dtype=torch.uint8, device="cuda", generator=gen)
+        scales = torch.randint(119, 121, (E, C, K // 32), dtype=torch.uint8, device="cuda", generator=gen)
+        conv.append((codes, scales))
+    W = moe.moe_weights_pack_mxfp4(*conv)
+    rng = np.random.default_rng(0)
+    x, x64 = rows(rng, N, d, BF16)
+    offsets = np.zeros(E + 1, dtype=np.int32)
+    offsets[E - 1], offsets[E] = 1, N  # expert 62: row 0, expert 63: rows 1 and 2
+    yg = moe.moe_expert_ffn(W, x, cuda(offsets), path=path)
+    for e, lo, hi in ((62, 0, 1), (63, 1, 3)):
+        mats = [ref.dequantize(c[e:e + 1].cpu().numpy(), s[e:e + 1].cpu().numpy())[0] for c, s in conv]
+        want, bound = ref.expert(x64[lo:hi], *mats, 0.0, ref.SPLIT)
+        check(yg[lo:hi], want, bound, what=e)
+    W.free()
+
+
+def test_tensors_that_are_refused():
+    conv, _ = ref.matrices(11, 4, 64, 64)
+    W = pack(conv)
+    x, logits = torch.randn((6, 64), device="cuda"), torch.randn((6, 4), device="cuda")
+    for bad in (dict(x=torch.randn((64, 6), device="cuda").t()), dict(logits=torch.randn((4, 6), device="cuda").t()),
+                dict(x=x.cpu()), dict(logits=logits.double()), dict(x=x[:, :32].contiguous()), dict(logits=logits[:, :3].contiguous()),
+                dict(x=x.half())):
+        with pytest.raises((ValueError, TypeError)):
+            moe.moe_layer_mxfp4(W, **{**dict(x=x, logits=logits), **bad}, k=2)
+    # the layer may not write where it reads
+    with pytest.raises(moe.MoeError):
+        moe.moe_layer_mxfp4(W, x, logits, 2, y=x)
+    W.free()

@@ -311,7 +311,7 @@ int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, 
 size_t moe_layer_mxfp4_workspace(int T, int E, int k, int d, int f);
 
 /*
- * One decode step of the layer in three launches (Sec. 3.3 "Execution" for a handful of
+ * One decode step of the layer in three launches, two on an MXFP4 handle (Sec. 3.3 "Execution" for a handful of
  * tokens, where every launch is a few percent of the step): the first-projection kernel runs
  * the gating function and the per-expert batching in its prologue and reads the token rows
  * directly, the second projection leaves its reduction parts, and the combine adds them.

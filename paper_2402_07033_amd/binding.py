@@ -476,7 +476,7 @@ def moe_combine_parts(yg_parts: torch.Tensor, n_parts: int, inv_perm: torch.Tens
 def moe_decode_layer(W: "PackedWeights", x: torch.Tensor, logits: torch.Tensor, k: int, idx=None,
                      weights=None, out=None, workspace=None, yg=None, y=None, want_xg=False,
                      stream=None) -> dict:
-    """One decode step (T <= 16) in three launches: gate + first projection, second
+    """One decode step (T <= 16) in three launches (two on an MXFP4 handle): gate + first projection, second
     projection, combine.  `out` = (counts, offsets, perm, inv_perm, xg-or-None)."""
     _dev(x, torch.float32, "x")
     _dev(logits, torch.float32, "logits")

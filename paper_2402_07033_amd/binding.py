@@ -810,7 +810,8 @@ class StackBuffers:
     """Preallocated device buffers for moe_stack_forward (one layer's worth, reused).  The
     routing outputs exist twice (sets 0 and 1, used by even and odd layers) because the
     one-launch seam between two blocks reads the previous block's while writing the next
-    block's; x_alt is the second residual-stream buffer of that seam."""
+    block's; x_alt is the second residual-stream buffer of that seam.  w_dtype: the handles' type,
+    where it is MOE_MXFP4."""
 
     def __init__(self, T: int, E: int, k: int, d: int, f: int, device="cuda", w_dtype: int = MOE_BF16):
         N = T * k

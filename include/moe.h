@@ -127,9 +127,10 @@ int moe_weights_pack(const void* w1, const void* w3, const void* w2, int E, int 
  * The handle serves moe_expert_ffn, moe_expert_ffn_path (AUTO: STREAM up to 72 rows, 4 per expert of the
  * handle and d <= 4096, else GROUPED; MID is unsupported), _tokens, _noalloc, _parts (one slab), moe_layer, moe_decode_layer (E up to 64 there, two
  * launches), moe_decode_block and moe_layer_mxfp4 below.  The products are formed on the bf16
- * matrix cores from the exact element values, with fp32 accumulation.  fp32 activations keep their 24
- * bits (three bf16 parts) on STREAM, and on GROUPED up to 72 rows of an fp32 result; h keeps 24 where
- * the result is fp32 there, 16 where a streamed result is bf16.  Beyond, GROUPED rounds both to bf16.
+ * matrix cores from the exact element values, with fp32 accumulation.  Where the result is fp32, as every
+ * call's but moe_layer_mxfp4's may be, fp32 activations and h = silu(a)*b keep their 24 bits (three bf16
+ * parts), whatever the number of rows.  Where it is bf16, STREAM keeps 24 bits of activations and 16 of h,
+ * GROUPED rounds both to bf16.
  * Rows that offsets do not cover are left as they were.
  */
 int moe_mxfp4_quantize(const void* w, moe_dtype_t w_dtype, int E, int K, int C, uint8_t* codes, uint8_t* scales,

@@ -14,16 +14,15 @@
 //     the step before), requests the operands D steps ahead, and multiplies.
 //   * few tiles (second projection): the reduction is cut in S parts, every part a slab of partial
 //     sums, which the combine (or mx_sum_kernel) adds in part order.
-//   * T parts per row: a row of fp32 is three bf16 parts (all 24 bits) where fp32 results are held to
-//     that, else one.
+//   * T bf16 parts per row, by the caller's types alone: a result in fp32 takes fp32 rows and h in three
+//     (all 24 bits), at any number of rows; bf16 rows are one, and where the result is bf16 so are fp32 rows
+//     and h.  Three parts are three times the matrix work: 1024 rows of 8 experts (d 4096, f 14336) in fp32
+//     took 322 us rounded to bf16, and take 792.
 #include <type_traits>
 
 #include "moe_mx.h"
 #include "moe_frag_pack.h"
 
-// Rows up to which fp32 operands keep 24 bits.  (Above, as with bf16 weights, rows and h are rounded
-// to bf16: three times the matrix work would bound the call.)
-#define MXG_EXACT_ROWS 72
 #define MXG_WAVES 4
 #define MXG_NF 4   // fragment rows of a wave
 // Steps requested ahead, in stages of LDS (12 .. 64 KiB a workgroup).  More rows are more matrix work under
@@ -295,7 +294,7 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& 
 }
 
 template <int NMAT, int T, int RBM, bool ONCE>
-__global__ __launch_bounds__(64 * MXG_WAVES, RBM > 2 ? 2 : 4) void mx_gemm_kernel(MxGemmArgs a) {
+__global__ __launch_bounds__(64 * MXG_WAVES, RBM > 2 ? 2 : T > 1 ? 3 : 4) void mx_gemm_kernel(MxGemmArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -346,8 +345,8 @@ struct MxGemmShape {
 };
 static MxGemmShape mxg_shape(int N, int E, int d, int f, bool x_f32, bool y_f32) {
     MxGemmShape sh;
-    sh.tu = x_f32 && y_f32 && N <= MXG_EXACT_ROWS ? 3 : 1;
-    sh.td = y_f32 && N <= MXG_EXACT_ROWS ? 3 : 1;
+    sh.td = y_f32 ? 3 : 1;
+    sh.tu = x_f32 ? sh.td : 1;
     // row tiles that there are about: the experts in use, and those of full tiles
     const int rows = 16 * mxg_rbm(N, E, sh.td);
     const int tiles = N / rows + (N < E ? N : E) + (N == 0);
@@ -375,7 +374,8 @@ size_t moe_mx_gemm_workspace(int N, int E, int d, int f) {
 
 int moe_mx_gemm_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan) {
     if (!moe_mx_gemm_supported(N, E, d, f)) return MOE_ERR_UNSUPPORTED;
-    plan->up_tile_rows = plan->down_tile_rows = 16 * mxg_rbm(N, E, 1);  // (32 for a result in fp32 of up to 72 rows)
+    plan->up_tile_rows = 16 * mxg_rbm(N, E, 1);  // (of bf16 rows; fp32 rows: as the second projection's)
+    plan->down_tile_rows = 16 * mxg_rbm(N, E, 3);
     plan->up_tile_features = plan->down_tile_features = MXG_WAVES * MXG_NF * 16;
     return MOE_OK;
 }

@@ -1,0 +1,128 @@
+"""What the kernels over 4-bit expert matrices keep of rows and of h = silu(a)*b: 24 bits where the result is
+fp32, at any number of rows.
+
+Two kinds of inputs.  `Picked`: every row has one value and every column of w2 one element, so that no sum
+hides what an operand lost, and the result is held to a few fp32 roundings.  Dense ones: against the bounds
+of mxfp4_ref, after a look (in the reference, on the CPU) that the bounds would show a result of zeros and
+one that leaves out a scale block of the rows."""
+import numpy as np
+import pytest
+import torch
+
+import mxfp4_ref as ref
+import paper_2402_07033_amd as moe
+from test_gpu_mxfp4 import check, cuda, pack, rows, split_rows
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def keep(v, parts):
+    """fp64 values with what `parts` bf16 parts hold of them."""
+    out = np.zeros_like(v)
+    for _ in range(parts):
+        out = out + ref.bf16((v - out).astype(np.float32)).astype(np.float64)
+    return out
+
+
+class Picked:
+    """Row n is x[n] in column at[n], else zero; column c of an expert's w2 has one element, in row src[c].
+    w1 is positive, so a > 0 and silu is no worse conditioned than 1.3."""
+
+    def __init__(self, seed, E, d, f, N):
+        rng = np.random.default_rng(seed)
+
+        def codes(shape, low):
+            c = rng.integers(1, 8, size=shape, dtype=np.uint8) | (rng.integers(0, 2, size=shape, dtype=np.uint8) << 3) * low
+            return c[..., 0::2] | (c[..., 1::2] << 4)
+
+        def scales(shape):
+            return rng.integers(125, 129, size=shape).astype(np.uint8)
+        w1 = codes((E, f, d), 0), scales((E, f, d // 32))
+        w3 = codes((E, f, d), 1), scales((E, f, d // 32))
+        self.src = rng.integers(0, f, size=(E, d))
+        c2 = np.zeros((E, d, f), dtype=np.uint8)
+        np.put_along_axis(c2, self.src[..., None], rng.integers(1, 8, size=(E, d, 1), dtype=np.uint8), axis=2)
+        w2 = c2[..., 0::2] | (c2[..., 1::2] << 4), scales((E, d, f // 32))
+        self.conv = [w1, w3, w2]
+        self.vals = [ref.dequantize(*m) for m in self.conv]
+        self.at = rng.integers(0, d, size=N)
+        # 24 bits each, the lowest set
+        self.x = np.zeros((N, d), dtype=np.float32)
+        top = np.ldexp((rng.integers(1 << 23, 1 << 24, size=N) | 1).astype(np.float64), -23 - rng.integers(0, 3, size=N))
+        self.x[np.arange(N), self.at] = top
+
+    def result(self, expert, x_parts=3, h_parts=3, bf16_rows=False):
+        """yg in 64 bits, rows and h as so many bf16 parts (3: all of an fp32 value)."""
+        n = np.arange(len(expert))
+        v = self.x[n, self.at].astype(np.float64)
+        v = keep(v, 1 if bf16_rows else x_parts)
+        a = v[:, None] * self.vals[0][expert, self.at]
+        b = v[:, None] * self.vals[1][expert, self.at]
+        h = keep((ref.silu(a) * b).astype(np.float32).astype(np.float64), h_parts)
+        src = self.src[expert]
+        return np.take_along_axis(h, src, axis=1) * np.take_along_axis(self.vals[2][expert], src[:, None], axis=1)[:, 0]
+
+
+# Roundings of a result over `Picked`, in steps of 2^-22 relative: the exact parts of x are added in two steps of
+# 2^-23 for each of a and b; silu carries 1.3 times that on, its exp counts at most half a step of 2^-23 (|a e^-a| is
+# below 0.3, so the argument's rounding counts less) and its sum and division 2^-24 each, the product 2^-24 and the
+# parts of h two more steps of 2^-23: 1.3 + 1 + 0.5 + 0.75 + 1 = 4.55, so 2^-19.8.  Without the third part of x or h
+# some elements are off by close to 2^-16.
+PICKED_BOUND = 2.0 ** -19
+
+
+def off(got, want):
+    return float(np.max(np.abs(got - want) / np.abs(want)))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,path", [(7, moe.MOE_FFN_STREAM), (72, moe.MOE_FFN_STREAM), (7, moe.MOE_FFN_GROUPED),
+                                    (72, moe.MOE_FFN_GROUPED), (73, moe.MOE_FFN_GROUPED), (200, moe.MOE_FFN_GROUPED),
+                                    (1100, moe.MOE_FFN_GROUPED)])
+@pytest.mark.parametrize("d,f,E", [(256, 512, 5), (320, 192, 3), (64, 4160, 2)])
+def test_fp32_results_keep_24_bits(d, f, E, N, path, dtype):
+    p = Picked(d + f + N, E, d, f, N)
+    offsets = split_rows(np.random.default_rng(N), N, E, "some")
+    expert = np.searchsorted(offsets[1:], np.arange(N), side="right")
+    want = p.result(expert, bf16_rows=dtype == BF16)
+    if dtype == F32:
+        assert off(p.result(expert, x_parts=2), want) > 2 * PICKED_BOUND
+    assert off(p.result(expert, h_parts=2, bf16_rows=dtype == BF16), want) > 2 * PICKED_BOUND
+    W = pack(p.conv)
+    yg = moe.moe_expert_ffn(W, cuda(p.x).to(dtype), cuda(offsets), path=path)
+    assert off(yg.cpu().numpy().astype(np.float64), want) <= PICKED_BOUND
+    W.free()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d,f,E,N,how", [(2048, 1408, 6, 73, "some"), (2048, 1408, 6, 200, "some"), (512, 6400, 2, 200, "some"),
+                                         (4096, 448, 2, 330, "some"), (192, 4160, 3, 530, "one"), (256, 512, 8, 517, "some")])
+def test_dense_rows_of_prompts(d, f, E, N, how, dtype):
+    rng = np.random.default_rng(d + f + N)
+    conv, mats = ref.matrices(d + f, E, d, f)
+    x, x64 = rows(rng, N, d, dtype)
+    offsets = split_rows(rng, N, E, how)
+    want, bound = ref.ffn(x64, offsets, mats, 0.0 if dtype == BF16 else ref.SPLIT, ref.SPLIT)
+    assert np.max(np.abs(want) / bound) > 2.0  # zeros
+    cut = x64.copy()
+    cut[:, -32:] = 0.0
+    assert np.max(np.abs(ref.ffn(cut, offsets, mats, 0.0, 0.0)[0] - want) / bound) > 2.0
+    W = pack(conv)
+    check(moe.moe_expert_ffn(W, x, cuda(offsets), path=moe.MOE_FFN_GROUPED), want, bound, what=(d, f, E, N, how))
+    W.free()
+
+
+@pytest.mark.parametrize("xd", [F32, BF16])
+@pytest.mark.parametrize("T,d,f,E,k", [(40, 256, 512, 8, 2), (130, 320, 192, 16, 3), (90, 64, 4160, 4, 1)])
+def test_the_layer_in_fp32(T, d, f, E, k, xd):
+    rng = np.random.default_rng(T)
+    conv, mats = ref.matrices(T, E, d, f)
+    x, x64 = rows(rng, T, d, xd)
+    logits = rng.standard_normal((T, E)).astype(np.float32)
+    want = ref.layer(x64, logits, mats, k, 0.0 if xd == BF16 else ref.SPLIT, ref.SPLIT)
+    W = pack(conv)
+    out = moe.moe_layer_mxfp4(W, x, cuda(logits), k, y=torch.empty((T, d), device="cuda"))
+    check(out["y"], want["y"], want["bound"], what=(T, d, f, E, k))
+    W.free()

@@ -129,8 +129,8 @@ int moe_weights_pack(const void* w1, const void* w3, const void* w2, int E, int 
  * launches), moe_decode_block and moe_layer_mxfp4 below.  The products are formed on the bf16
  * matrix cores from the exact element values, with fp32 accumulation.  Where the result is fp32, as every
  * call's but moe_layer_mxfp4's may be, fp32 activations and h = silu(a)*b keep their 24 bits (three bf16
- * parts), whatever the number of rows.  Where it is bf16, STREAM keeps 24 bits of activations and 16 of h,
- * GROUPED rounds both to bf16.
+ * parts), whatever the number of rows.  Where it is bf16, GROUPED keeps 16 bits of both, STREAM 24 of
+ * activations and 16 of h.
  * Rows that offsets do not cover are left as they were.
  */
 int moe_mxfp4_quantize(const void* w, moe_dtype_t w_dtype, int E, int K, int C, uint8_t* codes, uint8_t* scales,

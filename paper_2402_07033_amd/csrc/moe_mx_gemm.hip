@@ -15,9 +15,10 @@
 //   * few tiles (second projection): the reduction is cut in S parts, every part a slab of partial
 //     sums, which the combine (or mx_sum_kernel) adds in part order.
 //   * T bf16 parts per row, by the caller's types alone: a result in fp32 takes fp32 rows and h in three
-//     (all 24 bits), at any number of rows; bf16 rows are one, and where the result is bf16 so are fp32 rows
-//     and h.  Three parts are three times the matrix work: 1024 rows of 8 experts (d 4096, f 14336) in fp32
-//     took 322 us rounded to bf16, and take 792.
+//     (all 24 bits), one in bf16, which is rounded to 8 bits in the end, in two (16 bits); bf16 rows are
+//     one.  Each part is as much matrix work again.  Rounded to one part, bf16 results were off by 2.4e-3
+//     against 64 bits instead of their own rounding's 1.7e-3, and 4096 tokens of 2 of 8 experts (d 4096,
+//     f 14336) took 2260 us instead of 2960; 1024 fp32 rows for an fp32 result 322 instead of 792.
 #include <type_traits>
 
 #include "moe_mx.h"
@@ -236,9 +237,9 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& 
             for (int r = 0; r < NF; r++) {
                 const bf16x8_t w = mx_widen8(q[u][r][j], mx_scale(sc[u][r] >> (8 * (k & 3)), 0));
 #pragma unroll
-                for (int b = 0; b < RB; b++)
+                for (int t = 0; t < T; t++)
 #pragma unroll
-                    for (int t = 0; t < T; t++)
+                    for (int b = 0; b < RB; b++)
                         acc[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[b][t], acc[r][b], 0, 0, 0);
             }
         }
@@ -302,10 +303,12 @@ __global__ __launch_bounds__(64 * MXG_WAVES, RBM > 2 ? 2 : T > 1 ? 3 : 4) void m
     if (!mx_find_tile<RBM>(a, lane, ti)) return;
     if (ti.nblk == 1) mx_gemm_tile<NMAT, T, ONCE, 1>(a, ti, lane, wave, smem);
     else if (ti.nblk == 2) mx_gemm_tile<NMAT, T, ONCE, 2>(a, ti, lane, wave, smem);
-    if constexpr (RBM == 8) {
+    if constexpr (RBM >= 4) {
         if (ti.nblk == 3) mx_gemm_tile<NMAT, T, ONCE, 3>(a, ti, lane, wave, smem);
         else if (ti.nblk == 4) mx_gemm_tile<NMAT, T, ONCE, 4>(a, ti, lane, wave, smem);
-        else if (ti.nblk == 5) mx_gemm_tile<NMAT, T, ONCE, 5>(a, ti, lane, wave, smem);
+    }
+    if constexpr (RBM == 8) {
+        if (ti.nblk == 5) mx_gemm_tile<NMAT, T, ONCE, 5>(a, ti, lane, wave, smem);
         else if (ti.nblk == 6) mx_gemm_tile<NMAT, T, ONCE, 6>(a, ti, lane, wave, smem);
         else if (ti.nblk == 7) mx_gemm_tile<NMAT, T, ONCE, 7>(a, ti, lane, wave, smem);
         else if (ti.nblk == 8) mx_gemm_tile<NMAT, T, ONCE, 8>(a, ti, lane, wave, smem);
@@ -336,7 +339,8 @@ static inline size_t mxg_blocks(int N, int E) { return (size_t)N / 16 + E; }
 // uneven, 45 + 26 and 52 + 32.
 #define MXG_SMALL_ROWS 20
 static int mxg_rbm(int N, int E, int T) {
-    return T == 3 || N <= MXG_SMALL_ROWS * (N < E ? N : E) ? 2 : 8;
+    if (T == 3 || N <= MXG_SMALL_ROWS * (N < E ? N : E)) return 2;
+    return T == 2 ? 4 : 8;
 }
 
 struct MxGemmShape {
@@ -345,7 +349,7 @@ struct MxGemmShape {
 };
 static MxGemmShape mxg_shape(int N, int E, int d, int f, bool x_f32, bool y_f32) {
     MxGemmShape sh;
-    sh.td = y_f32 ? 3 : 1;
+    sh.td = y_f32 ? 3 : 2;
     sh.tu = x_f32 ? sh.td : 1;
     // row tiles that there are about: the experts in use, and those of full tiles
     const int rows = 16 * mxg_rbm(N, E, sh.td);
@@ -390,8 +394,11 @@ template <int NMAT, int T>
 static void mxg_pick(const MxGemmArgs& a, hipStream_t s) {
     const int rbm = mxg_rbm(a.N, a.E, T);
     const bool once = a.N <= 16 * rbm * a.E;
-    if (T == 3 || rbm == 2) once ? mxg_go<NMAT, T, 2, true>(a, s) : mxg_go<NMAT, T, 2, false>(a, s);
-    else once ? mxg_go<NMAT, 1, 8, true>(a, s) : mxg_go<NMAT, 1, 8, false>(a, s);
+    if constexpr (T < 3) {
+        constexpr int most = T == 1 ? 8 : 4;
+        if (rbm == most) return once ? mxg_go<NMAT, T, most, true>(a, s) : mxg_go<NMAT, T, most, false>(a, s);
+    }
+    once ? mxg_go<NMAT, T, 2, true>(a, s) : mxg_go<NMAT, T, 2, false>(a, s);
 }
 
 // The result in n_parts slabs of [N,d] floats from *slabs on, where the caller asks for them; else yg.
@@ -406,8 +413,8 @@ int moe_mx_gemm_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtyp
     const dim3 grid((unsigned)mxg_blocks(N, E), (unsigned)((mx_frags(d) + 7) / 8));
     if (act_dtype == MOE_BF16)
         hipLaunchKernelGGL((mx_rows_kernel<true, 1>), grid, dim3(256), 0, s, x, perm, k, offsets, E, N, d, xp, hp, f, sh.td);
-    else if (sh.tu == 1)
-        hipLaunchKernelGGL((mx_rows_kernel<false, 1>), grid, dim3(256), 0, s, x, perm, k, offsets, E, N, d, xp, hp, f, sh.td);
+    else if (sh.tu == 2)
+        hipLaunchKernelGGL((mx_rows_kernel<false, 2>), grid, dim3(256), 0, s, x, perm, k, offsets, E, N, d, xp, hp, f, sh.td);
     else
         hipLaunchKernelGGL((mx_rows_kernel<false, 3>), grid, dim3(256), 0, s, x, perm, k, offsets, E, N, d, xp, hp, f, sh.td);
     MxGemmArgs a = {};
@@ -422,6 +429,7 @@ int moe_mx_gemm_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtyp
     a.FT = (2 * a.NB + MXG_WAVES * MXG_NF - 1) / (MXG_WAVES * MXG_NF);
     a.S = 1;
     if (sh.tu == 1) mxg_pick<2, 1>(a, s);
+    else if (sh.tu == 2) mxg_pick<2, 2>(a, s);
     else mxg_pick<2, 3>(a, s);
     moe_record_mid_event(s);
     a.wfrag = (const u32x4_t*)W->w2;
@@ -432,7 +440,7 @@ int moe_mx_gemm_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtyp
     a.K = f; a.C = d; a.NB = d / 16; a.KS = mx_frags(f); a.KW = mx_words(f);
     a.FT = (a.NB + MXG_WAVES * MXG_NF - 1) / (MXG_WAVES * MXG_NF);
     a.S = sh.S;
-    if (sh.td == 1) mxg_pick<1, 1>(a, s);
+    if (sh.td == 2) mxg_pick<1, 2>(a, s);
     else mxg_pick<1, 3>(a, s);
     if (slabs) {
         *slabs = a.yg;

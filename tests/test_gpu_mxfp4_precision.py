@@ -1,5 +1,5 @@
 """What the kernels over 4-bit expert matrices keep of rows and of h = silu(a)*b: 24 bits where the result is
-fp32, at any number of rows.
+fp32, 16 where it is bf16, at any number of rows.
 
 Two kinds of inputs.  `Picked`: every row has one value and every column of w2 one element, so that no sum
 hides what an operand lost, and the result is held to a few fp32 roundings.  Dense ones: against the bounds
@@ -125,4 +125,28 @@ def test_the_layer_in_fp32(T, d, f, E, k, xd):
     W = pack(conv)
     out = moe.moe_layer_mxfp4(W, x, cuda(logits), k, y=torch.empty((T, d), device="cuda"))
     check(out["y"], want["y"], want["bound"], what=(T, d, f, E, k))
+    W.free()
+
+
+# A bf16 result over `Picked`: h to 16 bits and fp32 rows to 16 at least (2^-16 each, times 1, and 1.3 + 1 for the
+# rows' part in h: 2^-14.3), with the steps above 2^-14, and y's own rounding, 2^-8.  Rows or h in one part are off by
+# up to 2^-8 before that rounding.
+Y_BOUND = 2.0 ** -8 + 2.0 ** -14
+
+
+@pytest.mark.parametrize("xd", [F32, BF16])
+@pytest.mark.parametrize("T", [5, 60, 90, 300, 1500])
+@pytest.mark.parametrize("d,f,E", [(256, 512, 6), (320, 192, 5), (64, 4160, 2)])
+def test_bf16_results_keep_16_bits(d, f, E, T, xd):
+    p = Picked(d + f + T, E, d, f, T)
+    logits = np.random.default_rng(T).standard_normal((T, E)).astype(np.float32)
+    expert = logits.argmax(axis=1)  # (k = 1: weight 1)
+    want = p.result(expert, bf16_rows=xd == BF16)
+    assert off(ref.bf16(p.result(expert, h_parts=1, bf16_rows=xd == BF16).astype(np.float32)), want) > 1.2 * Y_BOUND
+    if xd == F32:
+        assert off(ref.bf16(p.result(expert, x_parts=1).astype(np.float32)), want) > 1.2 * Y_BOUND
+    W = pack(p.conv)
+    out = moe.moe_layer_mxfp4(W, cuda(p.x).to(xd), cuda(logits), 1, y=torch.empty((T, d), dtype=BF16, device="cuda"))
+    assert np.array_equal(out["idx"].cpu().numpy()[:, 0], expert)
+    assert off(out["y"].float().cpu().numpy().astype(np.float64), want) <= Y_BOUND
     W.free()

@@ -295,9 +295,10 @@ int moe_combine_parts(const float* yg_parts, int n_parts, const int32_t* inv_per
 /*
  * The whole layer over MXFP4 experts, from tokens and router logits to tokens: moe_route,
  * moe_permute without rows, the expert FFN and the gate-weighted sum, y rounded once to its type.
- * Two launches for T <= 16 tokens with T*k <= 64 slots and d <= 4096: the first routes the tokens
- * in its prologue, the second's workgroups count their parts and the last one of a feature group
- * adds them (in a fixed order: the same bits on every run).
+ * Two launches for T <= 16 tokens with T*k <= 64 slots and d <= 4096 (fp32 tokens: up to 5 slots per
+ * expert, or matrices of at most 96 MiB): the first routes the tokens in its prologue, the second's
+ * workgroups count their parts and the last one of a feature group adds them (in a fixed order: the
+ * same bits on every run).
  *   W of moe_weights_pack_mxfp4; x [T,d] of x_dtype; logits [T,E] fp32, E the handle's
  *   idx, weights, counts, offsets, perm, inv_perm: as moe_route / moe_permute, all written
  *   workspace >= moe_layer_mxfp4_workspace(T, E, k, d, f) bytes, 256-byte aligned

@@ -717,7 +717,7 @@ def moe_layer_mxfp4_workspace(T: int, E: int, k: int, d: int, f: int) -> int:
 def moe_layer_mxfp4(W: PackedWeights, x: torch.Tensor, logits: torch.Tensor, k: int, idx=None, weights=None,
                     out=None, workspace=None, y=None, stream=None) -> dict:
     """The whole layer over 4-bit experts: x [T,d] (fp32 or bf16), logits fp32 [T,E] -> y [T,d] of
-    x's type unless a y is given.  Two launches for a few tokens (T <= 16, T*k <= 64).  `out` =
+    x's type unless a y is given.  Two launches for a few tokens (T <= 16, T*k <= 64, few of them per expert).  `out` =
     (counts, offsets, perm, inv_perm)."""
     _dev(logits, torch.float32, "logits")
     xdt = _act_dtype(x)

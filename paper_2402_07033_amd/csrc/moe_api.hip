@@ -506,12 +506,30 @@ int moe_layer(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, int d,
 // what moe_layer_mxfp4 keeps besides the expert FFN's scratch: the experts' rows, where the GEMM leaves them
 static size_t mx_layer_rows(int N, int d) { return align256((size_t)N * d * sizeof(float)); }
 
+// Does a call of these sizes route in the streaming kernels' prologue?  That saves four launches, some 12 us.  fp32
+// rows of an expert are read by passes of 5 over its matrices, so where there are more of them per expert the GEMM is
+// faster, unless the matrices are small (96 MiB: between the last two).  Streamed / GEMM, us, 16 tokens where not
+// said: fp32, 8 experts (d 4096, f 14336) 4 rows each 164 / 179, 6 each 238 / 180, 8 each 226 / 181; 4 experts
+// (f 6400, 167 MB) 5 each (10 tokens) 49 / 69, 6 each (12) 76 / 70, 16 each 96 / 75; one (f 14336, 94 MB) 16 59 / 64;
+// 8 experts (d 2048, f 1408, 37 MB) 8 each 29 / 45.  bf16 rows, 16 to a pass: 8 experts (f 14336) 6 each 141 / 157,
+// 8 each 168 / 158; 4 (f 6400) 16 each 61 / 63.
+static bool mx_layer_routes(int T, int E, int k, int d, int f, bool x_f32) {
+    if (!moe_mx_stream_routes(T, E, k, d, f)) return false;
+    const size_t experts = (size_t)(T * k < E ? T * k : E), bytes = experts * 3 * d * f / MX_BLOCK * 17;
+    return !x_f32 || T * k <= 5 * E || bytes <= (96u << 20);
+}
+
 size_t moe_layer_mxfp4_workspace(int T, int E, int k, int d, int f) {
     if (!tek_ok(T, E, k) || !dims_ok(d) || !dims_ok(f)) return 0;
     const int N = T * k;
-    const bool streams = moe_mx_stream_routes(T, E, k, d, f) || moe_mx_auto_path(N, E, d, f) == MOE_FFN_STREAM;
-    return align256(streams ? moe_mx_stream_workspace(N, E, d, f)
-                            : mx_layer_rows(N, d) + moe_mx_gemm_workspace(N, E, d, f)) + 256;
+    size_t need = 0;
+    if (moe_mx_stream_routes(T, E, k, d, f) || moe_mx_auto_path(N, E, d, f) == MOE_FFN_STREAM)
+        need = moe_mx_stream_workspace(N, E, d, f);
+    if (!mx_layer_routes(T, E, k, d, f, true) && moe_mx_auto_path(N, E, d, f) != MOE_FFN_STREAM) {
+        const size_t g = mx_layer_rows(N, d) + moe_mx_gemm_workspace(N, E, d, f);
+        need = g > need ? g : need;
+    }
+    return align256(need) + 256;
 }
 
 int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, const float* logits, int T, int k,
@@ -530,7 +548,7 @@ int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, 
     if (!moe_aligned16(x) || !moe_aligned16(y) || !moe_aligned16(logits) || !moe_aligned16(idx) ||
         !moe_aligned16(weights) || !moe_aligned16(perm) || !moe_aligned16(inv_perm))
         return MOE_ERR_INVALID_ARG;
-    const bool routes = moe_mx_stream_routes(T, E, k, d, f);
+    const bool routes = mx_layer_routes(T, E, k, d, f, x_dtype == MOE_F32);
     const bool streams = routes || moe_mx_auto_path(N, E, d, f) == MOE_FFN_STREAM;
     if (!streams && !moe_mx_gemm_supported(N, E, d, f)) return MOE_ERR_UNSUPPORTED;
     if (!workspace || (((uintptr_t)workspace) & 255u)) return MOE_ERR_WORKSPACE;

@@ -199,6 +199,9 @@ int moe_expert_ffn_tokens(const moe_weights_t* W, const void* x, moe_dtype_t act
  *   Returns MOE_ERR_WORKSPACE when the kernel family that would run needs more scratch
  *   than that (decode-sized calls fit: the Mixtral shape needs 120 KiB per routed row;
  *   prefill-sized calls do not -- they take moe_expert_ffn with a caller's workspace).
+ *   An MXFP4 handle's GROUPED calls keep rows and h in up to three parts, in blocks of 16 rows of
+ *   an expert: 96*(d+f) bytes per block, and up to 8 slabs of 4*N*d where the rows are few
+ *   (8 experts of the Mixtral shape: up to about 150 rows fit).
  *   All calls on one GPU share the array: calls that overlap in time on one GPU (different
  *   streams, different host threads) race; serialise them.  Nothing in the array has to
  *   survive between calls and nothing has to be zero at the start of one.

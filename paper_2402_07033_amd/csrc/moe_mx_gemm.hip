@@ -331,7 +331,10 @@ __global__ __launch_bounds__(256) void mx_sum_kernel(const float4* __restrict__ 
 
 // ------------------------------------------------------------------ host ----
 static inline size_t mxg_align256(size_t v) { return (v + 255) & ~(size_t)255; }
-static inline size_t mxg_blocks(int N, int E) { return (size_t)N / 16 + E; }
+// Blocks of `rows` rows of one expert, at most: min(N, E) experts have rows, and a last block of at least one.
+static inline size_t mxg_blocks(int N, int E, int rows = 16) {
+    return ((size_t)N + (size_t)(rows - 1) * (N < E ? N : E)) / rows;
+}
 
 // Blocks of a tile, at most, by the mean rows of an expert in use.  Tiles of 32 rows let four workgroups
 // run on a CU instead of two, and experts above share their weights in L2 or not at all: 8 experts, 77
@@ -386,8 +389,7 @@ int moe_mx_gemm_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan) {
 
 template <int NMAT, int T, int RBM, bool ONCE>
 static void mxg_go(const MxGemmArgs& a, hipStream_t s) {
-    const unsigned rtiles = (unsigned)(a.N / (16 * RBM) + a.E);
-    const unsigned grid = (rtiles * (unsigned)(a.FT * a.S) + 7) / 8 * 8;
+    const unsigned grid = ((unsigned)mxg_blocks(a.N, a.E, 16 * RBM) * (unsigned)(a.FT * a.S) + 7) / 8 * 8;
     hipLaunchKernelGGL((mx_gemm_kernel<NMAT, T, RBM, ONCE>), dim3(grid), dim3(64 * MXG_WAVES), mxg_lds(T, RBM), s, a);
 }
 template <int NMAT, int T>

@@ -162,3 +162,12 @@ def test_python_refusals():
         moe.moe_mxfp4_quantize(cpu.double())
     with pytest.raises(TypeError):
         moe.moe_mxfp4_dequantize(torch.zeros((1, 2, 16), dtype=torch.uint8), torch.zeros((1, 2, 1), dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("E,d,f,N", [(16, 8192, 28672, 1), (16, 8192, 28672, 8), (64, 5120, 14336, 2), (64, 8192, 8192, 4)])
+def test_a_few_rows_of_wide_layers_need_no_workspace(L, mem, E, d, f, N):
+    """Scratch is for the experts that N rows can be on: d > 4096 has no streaming kernels, and its single rows go
+    through the GEMM."""
+    p = mem[0]
+    W = _MxWeights(E=E, d=d, f=f, dtype=MXFP4)
+    assert L.moe_expert_ffn_noalloc(C.addressof(W), p, F32, p + 65536, N, p + 131072, None) == HIP

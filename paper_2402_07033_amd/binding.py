@@ -810,10 +810,10 @@ class StackBuffers:
     """Preallocated device buffers for moe_stack_forward (one layer's worth, reused).  The
     routing outputs exist twice (sets 0 and 1, used by even and odd layers) because the
     one-launch seam between two blocks reads the previous block's while writing the next
-    block's; x_alt is the second residual-stream buffer of that seam.  w_dtype: the handles' type,
-    where it is MOE_MXFP4."""
+    block's; x_alt is the second residual-stream buffer of that seam.  w_dtype: the handles' type, or
+    all of them where a stack holds several."""
 
-    def __init__(self, T: int, E: int, k: int, d: int, f: int, device="cuda", w_dtype: int = MOE_BF16):
+    def __init__(self, T: int, E: int, k: int, d: int, f: int, device="cuda", w_dtype=MOE_BF16):
         N = T * k
         i32 = dict(dtype=torch.int32, device=device)
         f32 = dict(dtype=torch.float32, device=device)
@@ -829,13 +829,15 @@ class StackBuffers:
         self.ws = torch.empty(max(moe_expert_ffn_workspace(N, E, d, f, MOE_F32), 256),
                               dtype=torch.uint8, device=device)
         # the second projection's reduction parts (decode kernels; slab 0 is yg otherwise)
-        try:
-            plan = moe_expert_ffn_plan(N, E, d, f, MOE_MXFP4 if w_dtype == MOE_MXFP4 else MOE_BF16)
-        except MoeError:   # a shape only the fp32 kernels serve
-            plan = dict(n_parts=1, path=MOE_FFN_STREAM)
-        self.max_parts = max(1, plan["n_parts"])
-        # prefill-sized passes read the normalised rows through perm: no gathered copy
-        self.rows_through_perm = plan["path"] != MOE_FFN_STREAM
+        self.max_parts, self.rows_through_perm = 1, True
+        for t in {w_dtype} if isinstance(w_dtype, int) else set(w_dtype):
+            try:
+                plan = moe_expert_ffn_plan(N, E, d, f, MOE_MXFP4 if t == MOE_MXFP4 else MOE_BF16)
+            except MoeError:   # a shape only the fp32 kernels serve
+                plan = dict(n_parts=1, path=MOE_FFN_STREAM)
+            self.max_parts = max(self.max_parts, plan["n_parts"])
+            # prefill-sized passes read the normalised rows through perm: no gathered copy
+            self.rows_through_perm &= plan["path"] != MOE_FFN_STREAM
         self.yg_parts = torch.empty((self.max_parts, N, d), **f32)
         self.yg = self.yg_parts[0]
         self.y = torch.empty((T, d), **f32)
@@ -861,11 +863,12 @@ def moe_stack_forward(layers, x: torch.Tensor, k: int, eps: float = 1e-5, bufs=N
     _dev(x, torch.float32, "x")
     T, d = x.shape
     W0 = layers[0][0]
+    kinds = {W.dtype for W, _ in layers}
     if bufs is None:
-        bufs = StackBuffers(T, W0.E, k, d, W0.f, x.device, W0.dtype)
+        bufs = StackBuffers(T, W0.E, k, d, W0.f, x.device, kinds)
     fused_gate = fused and T <= 4 and W0.E <= 16
     seam = seam and fused_gate
-    if seam and W0.dtype != MOE_F32 and moe_decode_block_supported(T, W0.E, k, d, W0.f, W0.dtype):
+    if seam and all(t != MOE_F32 and moe_decode_block_supported(T, W0.E, k, d, W0.f, t) for t in kinds):
         # at most four routed rows: two launches per block, nothing between two blocks
         moe_gate_sums(x, layers[0][1], bufs.gate_sums[0], stream=stream)
         n_shares = 1

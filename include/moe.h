@@ -117,9 +117,9 @@ int moe_weights_pack(const void* w1, const void* w3, const void* w2, int E, int 
  * moe_mxfp4_quantize: per block of 32 the scale's exponent is that of the largest magnitude less
  *   2, at least -126 (a block of zeros: that); elements are rounded to nearest, ties to the even
  *   code, and saturate at 6.  Finite elements (others: unspecified values).
- * moe_mxfp4_dequantize: the values the codes stand for.  Exact in bf16 and fp32 for scale bytes
- *   1 .. 252, which is what moe_mxfp4_quantize writes; others are for the caller to avoid here
- *   and in every call on a handle packed from them (unspecified values).
+ * moe_mxfp4_dequantize: the values the codes stand for, exact in bf16 and fp32 for scale bytes
+ *   0 .. 252 (moe_mxfp4_quantize writes 1 .. 252).  With 253 and 254 a value past 2^128 is infinite,
+ *   with 255 every value is NaN; calls on a handle packed from them compute with these values.
  *   w [E,K,C] fp32 or bf16; 1 <= E <= 64, K a multiple of 32 and C any number, up to 2^20;
  *   no output may overlap an input.
  * moe_weights_pack_mxfp4: moe_weights_pack for converted matrices (w1, w3: K = d, C = f; w2:
@@ -129,7 +129,7 @@ int moe_weights_pack(const void* w1, const void* w3, const void* w2, int E, int 
  * launches), moe_decode_block and moe_layer_mxfp4 below.  The products are formed on the bf16
  * matrix cores from the exact element values, with fp32 accumulation.  Where the result is fp32, as every
  * call's but moe_layer_mxfp4's may be, fp32 activations and h = silu(a)*b keep their 24 bits (three bf16
- * parts), whatever the number of rows.  Where it is bf16, GROUPED keeps 16 bits of both, STREAM 24 of
+ * parts, whose bits end at 2^-133), whatever the number of rows.  Where it is bf16, GROUPED keeps 16 bits of both, STREAM 24 of
  * activations and 16 of h.
  * Rows that offsets do not cover are left as they were.
  */

@@ -3,7 +3,8 @@
 // reduction.  Layout of the packed handle and the conversion to matrix-core operands, shared
 // by the kernels that read it.
 //
-// Every element value is exact in bf16, and so is its product with the scale (2^-126 .. 2^125),
+// Every element value is exact in bf16, and so is its product with the scale (bytes 0 .. 252: from 2^-127,
+// subnormal products included, up to 2^125; past them a product may be past the type and is infinite),
 // so v_cvt_scalef32_pk_bf16_fp4 turns two codes and the scale into two bf16 operands without a
 // rounding: one instruction per two weights is all the 4-bit format costs on the way to the
 // bf16 matrix cores.

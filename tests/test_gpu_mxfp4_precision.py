@@ -150,3 +150,56 @@ def test_bf16_results_keep_16_bits(d, f, E, T, xd):
     assert np.array_equal(out["idx"].cpu().numpy()[:, 0], expert)
     assert off(out["y"].float().cpu().numpy().astype(np.float64), want) <= Y_BOUND
     W.free()
+
+
+# ---- scales at the ends of the format: other converters write them, 0 for blocks of zeros among others ----
+
+def test_every_scale_byte():
+    scales = np.arange(256, dtype=np.uint8).reshape(1, 256, 1)
+    codes = np.tile(np.arange(16, dtype=np.uint8) * 0x11, (1, 256, 1))
+    want = ref.dequantize(codes, scales)
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)
+    want[..., 255] = np.nan
+    for dtype in (F32, BF16):
+        got = moe.moe_mxfp4_dequantize(cuda(codes), cuda(scales), dtype=dtype).float().cpu().numpy()
+        assert np.array_equal(got.astype(np.float64), want, equal_nan=True)
+
+
+@pytest.mark.parametrize("path", [moe.MOE_FFN_STREAM, moe.MOE_FFN_GROUPED])
+@pytest.mark.parametrize("byte,dtype", [(0, F32), (0, BF16), (1, F32), (230, F32), (252, BF16)])
+def test_scales_at_the_ends_in_products(byte, dtype, path):
+    """w1 and w3 of one scale, rows that undo it: subnormal weights are not lost on the matrix cores.  (fp32 rows end at
+    2^-104 here: what lies below 2^-133 of a row is none of its parts'.)"""
+    p = Picked(byte, 2, 64, 64, 9)
+    for n in (0, 1):
+        p.conv[n] = (p.conv[n][0], np.full_like(p.conv[n][1], byte))
+        p.vals[n] = ref.dequantize(*p.conv[n])
+    p.x *= np.float32(2.0) ** np.float32(min(127 - byte, 126))
+    assert np.isfinite(p.x).all()
+    # a block of zeros, as a converter may write it: scale 0, codes 0
+    p.conv[2][1][:, :, 1][(p.conv[2][0].reshape(2, 64, 2, 16)[:, :, 1] == 0).all(axis=2)] = 0
+    p.vals[2] = ref.dequantize(*p.conv[2])
+    offsets = np.array([0, 4, 9], dtype=np.int32)
+    want = p.result(np.repeat([0, 1], [4, 5]), bf16_rows=dtype == BF16)
+    W = pack(p.conv)
+    yg = moe.moe_expert_ffn(W, cuda(p.x).to(dtype), cuda(offsets), path=path)
+    assert off(yg.cpu().numpy().astype(np.float64), want) <= PICKED_BOUND
+    W.free()
+
+
+@pytest.mark.parametrize("path", [moe.MOE_FFN_STREAM, moe.MOE_FFN_GROUPED])
+@pytest.mark.parametrize("d,f", [(64, 192), (320, 64), (4096, 64)])
+def test_zero_padding_is_kept_from_infinite_weights(d, f, path):
+    """Infinite weights in the last block of a reduction that ends inside a fragment reach the rows that have them only."""
+    E, N = 2, 5
+    conv, mats = ref.matrices(1, E, d, f)
+    conv[0][1][1, :, -1] = 254   # expert 1's first projection
+    conv[0][0][1, :, -16:] = 0x77
+    W = pack(conv)
+    x, x64 = rows(np.random.default_rng(0), N, d, F32)
+    offsets = np.array([0, 3, 5], dtype=np.int32)
+    yg = moe.moe_expert_ffn(W, x, cuda(offsets), path=path).cpu().numpy().astype(np.float64)
+    want, bound = ref.ffn(x64[:3], offsets[[0, 1]], [m[:1] for m in mats], ref.SPLIT, ref.SPLIT)
+    assert (np.abs(yg[:3] - want) <= bound + 2.0 ** -24 * np.abs(want)).all()
+    assert not np.isfinite(yg[3:]).any()
+    W.free()

@@ -30,41 +30,6 @@ __device__ __forceinline__ float wave_max(float v) {
     return fmaxf(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
 }
 
-// The contest for the token whose logits the group's G lanes hold (lane gl: expert e = gl with logit v, or -inf and
-// INT_MAX): returns the weight of the group's gl-th winner, my_i, for lanes gl < k.
-template <int G>
-__device__ __forceinline__ float route_token(float v, int e, int gl, int k, int& my_i) {
-    float my_v = 0.f, top_v = 0.f;
-    my_i = 0;
-    for (int j = 0; j < k; j++) {
-        float bv = v;
-        int be = e;
-#pragma unroll
-        for (int m = 1; m < G; m <<= 1) {
-            float ov = __shfl_xor(bv, m, 64);
-            int oe = __shfl_xor(be, m, 64);
-            if (ov > bv || (ov == bv && oe < be)) {
-                bv = ov;
-                be = oe;
-            }
-        }
-        if (j == 0) top_v = bv;
-        if (gl == j) {
-            my_v = bv;
-            my_i = be;
-        }
-        if (e == be) {  // the winner leaves the contest
-            v = -INFINITY;
-            e = 0x7fffffff;
-        }
-    }
-    float u = (gl < k) ? expf(my_v - top_v) : 0.f;
-    float s = u;
-#pragma unroll
-    for (int m = 1; m < G; m <<= 1) s += __shfl_xor(s, m, 64);
-    return u / s;
-}
-
 // Top-k contest of the gating function (Sec. 2.1) for the token whose logits sit in a group
 // of 16 lanes (lane gl holds expert gl's logit, or -inf / INT_MAX beyond E): k rounds of a
 // butterfly arg-max, larger value first, lower expert index among equals.  On return lane

@@ -32,8 +32,8 @@ static inline __host__ __device__ int mx_words(int K) { return (mx_frags(K) + 3)
 #ifdef __HIPCC__
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
-// The scale of fragment s of a scale word: 2^(byte - 127), which is what a float whose exponent
-// field is the byte stands for.
+// The scale of fragment s of a scale word, 2^(byte - 127): the conversion takes the exponent field of a float
+// as it is (byte 0, a float of zero, is 2^-127 to it).
 __device__ __forceinline__ float mx_scale(unsigned word, int s) {
     return __uint_as_float(((word >> (8 * s)) & 0xFFu) << 23);
 }

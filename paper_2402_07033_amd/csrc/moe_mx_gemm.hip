@@ -109,7 +109,7 @@ struct MxGemmArgs {
     float* yg;      // down: out, slab 0
     size_t part_stride;
     const int32_t* offsets;
-    int E, N, K, C, NB, KS, KW;
+    int E, N, C, NB, KS, KW;
     int FT;         // feature tiles
     int S;          // reduction parts
 };
@@ -251,16 +251,12 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& 
     int k = k_lo;
     for (; k + NS <= k_hi; k += NS) {
         step(k, integral_constant<int, 0>{}, integral_constant<bool, true>{});
-        if constexpr (NS > 1) step(k + 1, integral_constant<int, 1>{}, integral_constant<bool, true>{});
+        step(k + 1, integral_constant<int, 1>{}, integral_constant<bool, true>{});
         if constexpr (NS > 2) step(k + 2, integral_constant<int, 2>{}, integral_constant<bool, true>{});
-        if constexpr (NS > 3) step(k + 3, integral_constant<int, 3>{}, integral_constant<bool, true>{});
-        if constexpr (NS > 4) step(k + 4, integral_constant<int, 4>{}, integral_constant<bool, true>{});
-        static_assert(NS <= 5, "steps of the ring");
+        static_assert(NS == 2 || NS == 3, "steps of the ring");
     }
     if (k < k_hi) step(k, integral_constant<int, 0>{}, integral_constant<bool, false>{});
     if constexpr (NS > 2) if (k + 1 < k_hi) step(k + 1, integral_constant<int, 1>{}, integral_constant<bool, false>{});
-    if constexpr (NS > 3) if (k + 2 < k_hi) step(k + 2, integral_constant<int, 2>{}, integral_constant<bool, false>{});
-    if constexpr (NS > 4) if (k + 3 < k_hi) step(k + 3, integral_constant<int, 3>{}, integral_constant<bool, false>{});
     // no request for LDS outlives the workgroup
     __builtin_amdgcn_s_waitcnt(0x0070);
     if (idle) return;
@@ -427,7 +423,7 @@ int moe_mx_gemm_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtyp
     a.xp = xp;
     a.hp = (uint16_t*)hp;
     a.TH = sh.td;
-    a.K = d; a.C = f; a.NB = f / 16; a.KS = mx_frags(d); a.KW = mx_words(d);
+    a.C = f; a.NB = f / 16; a.KS = mx_frags(d); a.KW = mx_words(d);
     a.FT = (2 * a.NB + MXG_WAVES * MXG_NF - 1) / (MXG_WAVES * MXG_NF);
     a.S = 1;
     if (sh.tu == 1) mxg_pick<2, 1>(a, s);
@@ -439,7 +435,7 @@ int moe_mx_gemm_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtyp
     a.xp = hp;
     a.yg = sh.S > 1 ? parts : yg;
     a.part_stride = (size_t)N * d;
-    a.K = f; a.C = d; a.NB = d / 16; a.KS = mx_frags(f); a.KW = mx_words(f);
+    a.C = d; a.NB = d / 16; a.KS = mx_frags(f); a.KW = mx_words(f);
     a.FT = (a.NB + MXG_WAVES * MXG_NF - 1) / (MXG_WAVES * MXG_NF);
     a.S = sh.S;
     if (sh.td == 2) mxg_pick<1, 2>(a, s);

@@ -15,6 +15,41 @@
 
 // ------------------------------------------------------------------ route ----
 
+// The contest for the token whose logits the group's G lanes hold (lane gl: expert e = gl with logit v, or -inf and
+// INT_MAX): returns the weight of the group's gl-th winner, my_i, for lanes gl < k.
+template <int G>
+__device__ __forceinline__ float route_token(float v, int e, int gl, int k, int& my_i) {
+    float my_v = 0.f, top_v = 0.f;
+    my_i = 0;
+    for (int j = 0; j < k; j++) {
+        float bv = v;
+        int be = e;
+#pragma unroll
+        for (int m = 1; m < G; m <<= 1) {
+            float ov = __shfl_xor(bv, m, 64);
+            int oe = __shfl_xor(be, m, 64);
+            if (ov > bv || (ov == bv && oe < be)) {
+                bv = ov;
+                be = oe;
+            }
+        }
+        if (j == 0) top_v = bv;
+        if (gl == j) {
+            my_v = bv;
+            my_i = be;
+        }
+        if (e == be) {  // the winner leaves the contest
+            v = -INFINITY;
+            e = 0x7fffffff;
+        }
+    }
+    float u = (gl < k) ? expf(my_v - top_v) : 0.f;
+    float s = u;
+#pragma unroll
+    for (int m = 1; m < G; m <<= 1) s += __shfl_xor(s, m, 64);
+    return u / s;
+}
+
 template <int G>
 __global__ __launch_bounds__(256) void route_kernel(const float* __restrict__ logits, int T, int E,
                                                     int k, int32_t* __restrict__ idx,

@@ -18,7 +18,7 @@
 //     (all 24 bits), one in bf16, which is rounded to 8 bits in the end, in two (16 bits); bf16 rows are
 //     one.  Each part is as much matrix work again.  Rounded to one part, bf16 results were off by 2.4e-3
 //     against 64 bits instead of their own rounding's 1.7e-3, and 4096 tokens of 2 of 8 experts (d 4096,
-//     f 14336) took 2260 us instead of 2960; 1024 fp32 rows for an fp32 result 322 instead of 792.
+//     f 14336) took 2260 us instead of 2840; 1024 fp32 rows for an fp32 result 322 instead of 792.
 #include <type_traits>
 
 #include "moe_mx.h"
@@ -27,10 +27,11 @@
 #define MXG_WAVES 4
 #define MXG_NF 4   // fragment rows of a wave
 // Steps requested ahead, in stages of LDS (12 .. 64 KiB a workgroup).  More rows are more matrix work under
-// which a request may travel, and a third stage of many rows leaves room for one workgroup per CU.  First +
-// second projection, us: 8 experts of 64 rows (d 4096, f 14336) 146 + 95 with one step, 126 + 70 with two;
-// of 1024 rows 1408 + 696 with one, 1549 + 1430 with two.  A third step for single blocks was slower: 8
-// experts of 10 rows 88 + 51 against 84 + 49; 16 (f 6400) of 12 rows 86 + 36 against 81 + 40.
+// which a request may travel, and a third stage of many rows leaves room for one workgroup per CU.  One part,
+// the first projection with one step / two, us: 8 experts of 64 rows (d 4096, f 14336) 146 / 126, of 1024 rows
+// 1408 / 1549; a third step for single blocks was slower, 8 experts of 10 rows 84 with two, 88 with three, 16
+// (f 6400) of 12 rows 81, 86.  Two parts in tiles of 32 rows, the layer: 8 experts of 12 rows 190 / 165, of 75
+// rows 356 / 344, of 1024 rows 2980 / 2990.
 constexpr int mxg_depth(int T, int RB) { return RB * T > 4 ? 1 : 2; }
 constexpr int mxg_lds(int T, int RBM) {
     int most = 0;
@@ -299,12 +300,10 @@ __global__ __launch_bounds__(64 * MXG_WAVES, RBM > 2 ? 2 : T > 1 ? 3 : 4) void m
     if (!mx_find_tile<RBM>(a, lane, ti)) return;
     if (ti.nblk == 1) mx_gemm_tile<NMAT, T, ONCE, 1>(a, ti, lane, wave, smem);
     else if (ti.nblk == 2) mx_gemm_tile<NMAT, T, ONCE, 2>(a, ti, lane, wave, smem);
-    if constexpr (RBM >= 4) {
+    if constexpr (RBM == 8) {
         if (ti.nblk == 3) mx_gemm_tile<NMAT, T, ONCE, 3>(a, ti, lane, wave, smem);
         else if (ti.nblk == 4) mx_gemm_tile<NMAT, T, ONCE, 4>(a, ti, lane, wave, smem);
-    }
-    if constexpr (RBM == 8) {
-        if (ti.nblk == 5) mx_gemm_tile<NMAT, T, ONCE, 5>(a, ti, lane, wave, smem);
+        else if (ti.nblk == 5) mx_gemm_tile<NMAT, T, ONCE, 5>(a, ti, lane, wave, smem);
         else if (ti.nblk == 6) mx_gemm_tile<NMAT, T, ONCE, 6>(a, ti, lane, wave, smem);
         else if (ti.nblk == 7) mx_gemm_tile<NMAT, T, ONCE, 7>(a, ti, lane, wave, smem);
         else if (ti.nblk == 8) mx_gemm_tile<NMAT, T, ONCE, 8>(a, ti, lane, wave, smem);
@@ -332,15 +331,16 @@ static inline size_t mxg_blocks(int N, int E, int rows = 16) {
     return ((size_t)N + (size_t)(rows - 1) * (N < E ? N : E)) / rows;
 }
 
-// Blocks of a tile, at most, by the mean rows of an expert in use.  Tiles of 32 rows let four workgroups
-// run on a CU instead of two, and experts above share their weights in L2 or not at all: 8 experts, 77
-// tokens, Zipf 1.2 (19 rows) 129 + 79 us with tiles of 128 rows, 116 + 59 with 32; 64 experts of 28 rows,
-// uneven, 45 + 26 and 52 + 32.
-#define MXG_SMALL_ROWS 20
-static int mxg_rbm(int N, int E, int T) {
-    if (T == 3 || N <= MXG_SMALL_ROWS * (N < E ? N : E)) return 2;
-    return T == 2 ? 4 : 8;
-}
+// Blocks of a tile, at most.  Rows of one part (the first projection of bf16 rows) by the mean rows of an expert in
+// use: tiles of 32 rows let four workgroups run on a CU instead of two, and experts of more rows share their weights in
+// L2.  The layer in bf16, tiles of 32 rows / of 128, us: 8 experts (d 4096, f 14336) 20 rows each 170 / 171, 25 each
+// 171 / 173, 32 each 224 / 212, 40 each 238 / 223, 100 each 409 / 376; 16 (f 6400) 20 each 163 / 163, 30 each 220 / 202;
+// 64 (d 2048, f 1408) 10 each 83 / 84, 19 each 89 / 92, 28 each 107 / 100, 39 each 121 / 114.  Rows of several parts are
+// the matrix work of a larger tile already.  The layer with two parts of h (and of x), 32 / 64 rows: 8 experts (f 14336)
+// 16 each 165 / 174, 25 each 171 / 172, 50 each 254 / 259, 256 each 808 / 896 (1111 / 1204), 1024 each 2840 / 2865
+// (4142 / 4121); 64 of 96 each 184 / 196 (230 / 251), of 384 each 545 / 550 (764 / 755).
+#define MXG_SMALL_ROWS 25
+static int mxg_rbm(int N, int E, int T) { return T > 1 || N <= MXG_SMALL_ROWS * (N < E ? N : E) ? 2 : 8; }
 
 struct MxGemmShape {
     int tu, td;  // parts of the rows and of h
@@ -392,10 +392,8 @@ template <int NMAT, int T>
 static void mxg_pick(const MxGemmArgs& a, hipStream_t s) {
     const int rbm = mxg_rbm(a.N, a.E, T);
     const bool once = a.N <= 16 * rbm * a.E;
-    if constexpr (T < 3) {
-        constexpr int most = T == 1 ? 8 : 4;
-        if (rbm == most) return once ? mxg_go<NMAT, T, most, true>(a, s) : mxg_go<NMAT, T, most, false>(a, s);
-    }
+    if constexpr (T == 1)
+        if (rbm == 8) return once ? mxg_go<NMAT, T, 8, true>(a, s) : mxg_go<NMAT, T, 8, false>(a, s);
     once ? mxg_go<NMAT, T, 2, true>(a, s) : mxg_go<NMAT, T, 2, false>(a, s);
 }
 

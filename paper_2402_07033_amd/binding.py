@@ -726,7 +726,6 @@ def moe_layer_mxfp4(W: PackedWeights, x: torch.Tensor, logits: torch.Tensor, k: 
     d, N, dev = W.d, T * k, x.device
     if E != W.E or tuple(x.shape) != (T, d):
         raise ValueError(f"expected x [T,{d}] and logits [T,{W.E}]")
-    _here(x, logits)
     if not 1 <= k <= min(E, _MAX_K) or N >= _MAX_N:
         raise MoeError(_INVALID_ARG, "moe_layer_mxfp4")  # before N rows are allocated
     i32 = dict(dtype=torch.int32, device=dev)
@@ -744,10 +743,11 @@ def moe_layer_mxfp4(W: PackedWeights, x: torch.Tensor, logits: torch.Tensor, k: 
     for t, n, dt, what in ((idx, N, torch.int32, "idx"), (weights, N, torch.float32, "weights"),
                            (counts, E, torch.int32, "counts"), (offsets, E + 1, torch.int32, "offsets"),
                            (perm, N, torch.int32, "perm"), (inv_perm, N, torch.int32, "inv_perm"),
-                           (y, T * d, y.dtype, "y")):
+                           (y, T * d, y.dtype, "y"), (workspace, 0, workspace.dtype, "workspace")):
         _dev(t, dt, what)
         if t.numel() < n:
             raise ValueError(f"{what}: {t.numel()} elements, {n} are written")
+    _here(x, logits, idx, weights, counts, offsets, perm, inv_perm, workspace, y)
     _check(lib().moe_layer_mxfp4(W.handle, x.data_ptr(), xdt, logits.data_ptr(), T, k, idx.data_ptr(),
                                  weights.data_ptr(), counts.data_ptr(), offsets.data_ptr(), perm.data_ptr(),
                                  inv_perm.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),

@@ -106,3 +106,16 @@ def test_rows_of_a_hot_expert(T, hot, xd, yd):
     assert np.array_equal(out["perm"].cpu().numpy(), want["perm"])
     check(out["y"], want["y"], want["bound"], yd, (T, hot))
     W.free()
+
+
+def test_workspace_and_outputs_in_host_memory_are_refused():
+    E, d, T, k = 4, 64, 6, 2
+    W = pack(ref.matrices(11, E, d, 64)[0])
+    x, logits = torch.randn((T, d), device="cuda"), torch.randn((T, E), device="cuda")
+    need = moe.moe_layer_mxfp4_workspace(T, E, k, d, 64)
+    for bad in (dict(workspace=torch.empty(need, dtype=torch.uint8)), dict(y=torch.empty((T, d))),
+                dict(workspace=torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2]),
+                dict(idx=torch.empty((T, k), dtype=torch.int32)), dict(weights=torch.empty((T, k)))):
+        with pytest.raises(TypeError):
+            moe.moe_layer_mxfp4(W, x, logits, k, **bad)
+    W.free()

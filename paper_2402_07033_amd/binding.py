@@ -203,6 +203,15 @@ def _dev(t: torch.Tensor, dtype, what: str):
     return t
 
 
+def _scratch(nbytes: int, device, stream) -> torch.Tensor:
+    """A call's own workspace, dropped when it returns: where it runs on another stream than the current one, the
+    memory goes back only when that stream has passed the call."""
+    t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
 def _act_dtype(t: torch.Tensor) -> int:
     if t.dtype == torch.float32:
         return MOE_F32
@@ -370,8 +379,7 @@ def moe_expert_ffn(W: PackedWeights, xg: torch.Tensor, offsets: torch.Tensor, wo
     N = xg.shape[0]
     adt = _act_dtype(xg)
     if workspace is None:
-        need = moe_expert_ffn_workspace(N, W.E, W.d, W.f, adt)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=xg.device)
+        workspace = _scratch(moe_expert_ffn_workspace(N, W.E, W.d, W.f, adt), xg.device, stream)
     if yg is None:
         yg = torch.empty((N, W.d), dtype=torch.float32, device=xg.device)
     _check(lib().moe_expert_ffn_path(W.handle, _ptr(xg), adt, _ptr(offsets), N,
@@ -407,8 +415,7 @@ def moe_expert_ffn_parts(W: "PackedWeights", xg: torch.Tensor, offsets: torch.Te
     N = xg.shape[0]
     adt = _act_dtype(xg)
     if workspace is None:
-        need = moe_expert_ffn_workspace(N, W.E, W.d, W.f, adt)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=xg.device)
+        workspace = _scratch(moe_expert_ffn_workspace(N, W.E, W.d, W.f, adt), xg.device, stream)
     n = C.c_int(0)
     _check(lib().moe_expert_ffn_parts(W.handle, _ptr(xg), adt, _ptr(offsets), N,
                                       _ptr(workspace), workspace.numel(), _ptr(yg_parts),
@@ -428,8 +435,7 @@ def moe_expert_ffn_tokens(W: "PackedWeights", x: torch.Tensor, k: int, perm: tor
     N = T * k
     adt = _act_dtype(x)
     if workspace is None:
-        need = moe_expert_ffn_workspace(N, W.E, W.d, W.f, adt)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=x.device)
+        workspace = _scratch(moe_expert_ffn_workspace(N, W.E, W.d, W.f, adt), x.device, stream)
     if yg is None:
         yg = torch.empty((N, W.d), dtype=torch.float32, device=x.device)
     _check(lib().moe_expert_ffn_tokens(W.handle, _ptr(x), adt, T, k, _ptr(perm),
@@ -495,8 +501,7 @@ def moe_decode_layer(W: "PackedWeights", x: torch.Tensor, logits: torch.Tensor, 
                torch.empty((N, d), dtype=torch.float32, device=dev) if want_xg else None)
     counts, offsets, perm, inv_perm, xg = out
     if workspace is None:
-        workspace = torch.empty(max(moe_expert_ffn_workspace(N, W.E, W.d, W.f, MOE_F32), 256),
-                                dtype=torch.uint8, device=dev)
+        workspace = _scratch(moe_expert_ffn_workspace(N, W.E, W.d, W.f, MOE_F32), dev, stream)
     if y is None:
         y = torch.empty((T, d), dtype=torch.float32, device=dev)
     _check(lib().moe_decode_layer(W.handle, _ptr(x), _ptr(logits), T, k, _ptr(idx),
@@ -525,7 +530,8 @@ def moe_gate_sums(x: torch.Tensor, w_gate: torch.Tensor, sums=None, stream=None)
     T, d = x.shape
     E = w_gate.shape[1]
     if sums is None:
-        sums = torch.zeros(moe_gate_sums_stride(T, E), dtype=torch.float32, device=x.device)
+        with torch.cuda.stream(stream):  # (no stream: the current one)
+            sums = torch.zeros(moe_gate_sums_stride(T, E), dtype=torch.float32, device=x.device)
     _check(lib().moe_gate_sums(_ptr(x), _ptr(w_gate), T, d, E, _ptr(sums), _stream(stream)),
            "moe_gate_sums")
     return sums
@@ -565,8 +571,7 @@ def moe_decode_block(W: "PackedWeights", x_in: torch.Tensor, k: int, gate_sums=N
                torch.empty(N, **i32))
     counts, offsets, perm, inv_perm = out[:4]
     if workspace is None:
-        workspace = torch.empty(max(moe_expert_ffn_workspace(N, W.E, W.d, W.f, MOE_F32), 256),
-                                dtype=torch.uint8, device=dev)
+        workspace = _scratch(moe_expert_ffn_workspace(N, W.E, W.d, W.f, MOE_F32), dev, stream)
     if x_out is None:
         x_out = torch.empty((T, d), **f32)
     if w_gate_next is not None:
@@ -694,8 +699,7 @@ def moe_layer(W: PackedWeights, x: torch.Tensor, logits: torch.Tensor, k: int,
     inv_perm = torch.empty(N, dtype=i32, device=dev)
     xg = torch.empty((N, d), dtype=x.dtype, device=dev)
     if workspace is None:
-        need = moe_expert_ffn_workspace(N, W.E, W.d, W.f, xdt)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        workspace = _scratch(moe_expert_ffn_workspace(N, W.E, W.d, W.f, xdt), dev, stream)
     yg = torch.empty((N, W.d), dtype=f32, device=dev)
     y = torch.empty((T, W.d), dtype=f32, device=dev)
     stage = C.c_int(0)
@@ -737,7 +741,7 @@ def moe_layer_mxfp4(W: PackedWeights, x: torch.Tensor, logits: torch.Tensor, k: 
         out = (torch.empty(E, **i32), torch.empty(E + 1, **i32), torch.empty(N, **i32), torch.empty(N, **i32))
     counts, offsets, perm, inv_perm = out[:4]
     if workspace is None:
-        workspace = torch.empty(max(moe_layer_mxfp4_workspace(T, E, k, d, W.f), 256), dtype=torch.uint8, device=dev)
+        workspace = _scratch(moe_layer_mxfp4_workspace(T, E, k, d, W.f), dev, stream)
     if y is None:
         y = torch.empty((T, d), dtype=x.dtype, device=dev)
     for t, n, dt, what in ((idx, N, torch.int32, "idx"), (weights, N, torch.float32, "weights"),
@@ -861,6 +865,9 @@ def moe_stack_forward(layers, x: torch.Tensor, k: int, eps: float = 1e-5, bufs=N
     the separate calls.  The fused variants leave the second projection's reduction parts
     unsummed and add them inside the combine (no separate launch)."""
     _dev(x, torch.float32, "x")
+    if stream is not None:  # the buffers and copies made here are the stream's, too
+        with torch.cuda.stream(stream):
+            return moe_stack_forward(layers, x, k, eps, bufs, logits_out, idx_out, on_layer, fused, None, seam)
     T, d = x.shape
     W0 = layers[0][0]
     kinds = {W.dtype for W, _ in layers}

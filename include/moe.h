@@ -156,13 +156,13 @@ size_t moe_expert_ffn_workspace(int N, int E, int d, int f, moe_dtype_t act_dtyp
  *     yg[i,:] = ( silu(xg[i,:] . w1_e) * (xg[i,:] . w3_e) ) . w2_e
  * with fp32 accumulation.  offsets is read on the device: the call never
  * learns the per-expert sizes on the host.
- *   W         packed handle (bf16 or fp32 weights)
+ *   W         packed handle (bf16, fp32 or MXFP4 weights)
  *   xg        [N,d] of act_dtype (fp32 weights need fp32 activations)
  *   offsets   [E+1] int32 DEVICE, offsets[0] = 0, non-decreasing, offsets[E] = N
  *   workspace >= moe_expert_ffn_workspace(...) bytes, 256-byte aligned; contents
  *             are scratch (may be reused by the next call on the same stream)
  *   yg        [N,d] fp32 out
- * bf16-weight kernels multiply on the bf16 matrix cores: fp32 activations are
+ * bf16-weight kernels multiply on the bf16 matrix cores (4-bit weights: above): fp32 activations are
  * split into bf16 high and low parts (STREAM path, ~2^-16 relative) or rounded
  * to bf16 (GROUPED, MID); the intermediate silu(a)*b is kept in fp32 (STREAM)
  * or bf16 (GROUPED, MID).  Every path adds its partial sums in a fixed order: the
@@ -324,7 +324,8 @@ size_t moe_layer_mxfp4_workspace(int T, int E, int k, int d, int f);
  * second projection finishes its reduction and the combine inside its workgroups: two
  * launches.
  * Same results as moe_route + moe_permute + moe_expert_ffn + moe_combine: index outputs bit
- * for bit, y and yg in the same fixed summation order.
+ * for bit, y and yg in the same fixed summation order (on an MXFP4 handle that of
+ * moe_expert_ffn_path with STREAM; AUTO takes GROUPED above 4 rows per expert).
  *   x [T,d] fp32, logits [T,E] fp32; bf16 or MXFP4 weights; 1 <= T <= 16, E <= 16 (MXFP4: 64), T*k <= 64 and a
  *   shape the STREAM family supports (MOE_ERR_UNSUPPORTED otherwise)
  *   idx, weights, counts, offsets, perm, inv_perm: as moe_route / moe_permute, all written

@@ -47,6 +47,10 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_rsrc(const void* p) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)(((unsigned long long)hi << 32) | lo), 0, (int)0x80000000u, 0x00027000);
 }
 
+// What a value's next bf16 part is taken from, behind its part p: nothing where p is infinite or NaN (inf - inf
+// would make an infinite value NaN).
+__device__ __forceinline__ float mx_rest(float v, float p) { return fabsf(p) < INFINITY ? v - p : 0.f; }
+
 // Eight codes and their scale -> eight bf16 operands, in the order of the codes.
 __device__ __forceinline__ bf16x8_t mx_widen8(unsigned codes, float scale) {
     const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);

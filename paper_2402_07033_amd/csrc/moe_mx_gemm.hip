@@ -54,7 +54,7 @@ __device__ __forceinline__ void mx_parts8(const float (&v)[8], u32x4_t (&o)[T]) 
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             p[i] = (__bf16)r[i];
-            r[i] -= (float)p[i];
+            r[i] = mx_rest(r[i], (float)p[i]);
         }
         o[t] = __builtin_bit_cast(u32x4_t, p);
     }
@@ -279,7 +279,7 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, const MxTile& 
                 for (int p = 0; p < a.TH; p++) {
                     *(uint2*)(dst + (size_t)p * 512) = make_uint2(moe_pack_bf16x2(h[0], h[1]), moe_pack_bf16x2(h[2], h[3]));
 #pragma unroll
-                    for (int i = 0; i < 4; i++) h[i] -= moe_bf16_to_f32(moe_bf16_rne(h[i]));
+                    for (int i = 0; i < 4; i++) h[i] = mx_rest(h[i], moe_bf16_to_f32(moe_bf16_rne(h[i])));
                 }
             } else {
                 const int rr = (ti.b0 + b) * 16 + t;

@@ -137,7 +137,7 @@ struct MxStager {
             // the scaled row is rounded to fp32 before the split, as if it had been stored
             const float v = __uint_as_float(raw[R == ROWS_F32 ? i / 4 : 0][i % 4]) * sc;
             o[0][i] = (__bf16)v;
-            const float r = v - (float)o[0][i];
+            const float r = mx_rest(v, (float)o[0][i]);
             o[1][i] = (__bf16)r;
             o[2][i] = (__bf16)(r - (float)o[1][i]);
         }
@@ -553,7 +553,7 @@ __global__ __launch_bounds__(64 * MXS_WAVES) void mx_stream_kernel(MxArgs a) {
                 *(uint2*)((uint16_t*)a.out + (size_t)p * a.N * a.C + at) =
                     make_uint2(moe_pack_bf16x2(h[0], h[1]), moe_pack_bf16x2(h[2], h[3]));
 #pragma unroll
-                for (int i = 0; i < 4; i++) h[i] -= moe_bf16_to_f32(moe_bf16_rne(h[i]));
+                for (int i = 0; i < 4; i++) h[i] = mx_rest(h[i], moe_bf16_to_f32(moe_bf16_rne(h[i])));
             }
         } else if (a.finish == FIN_NONE) {
             *(f32x4_t*)(a.out + at) = sa;

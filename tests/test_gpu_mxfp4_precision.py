@@ -203,3 +203,45 @@ def test_zero_padding_is_kept_from_infinite_weights(d, f, path):
     assert (np.abs(yg[:3] - want) <= bound + 2.0 ** -24 * np.abs(want)).all()
     assert not np.isfinite(yg[3:]).any()
     W.free()
+
+
+# ---- values past the types: what is infinite in 64-bit arithmetic rounded to the result's type is infinite ----
+
+def positive(seed, E, d, f):
+    """Matrices without a zero and without a sign: no sum is inf - inf or inf * 0."""
+    rng = np.random.default_rng(seed)
+    conv = []
+    for K, C in ((d, f), (d, f), (f, d)):
+        c = rng.integers(1, 8, size=(E, C, K), dtype=np.uint8)
+        conv.append((c[..., 0::2] | (c[..., 1::2] << 4), rng.integers(120, 123, size=(E, C, K // 32)).astype(np.uint8)))
+    return conv, [ref.dequantize(*m) for m in conv]
+
+
+@pytest.mark.parametrize("xd,yd", [(F32, F32), (BF16, BF16), (F32, BF16), (BF16, F32)])
+@pytest.mark.parametrize("T", [4, 60, 300])
+@pytest.mark.parametrize("d,f", [(192, 320), (256, 512)])
+def test_infinite_rows_and_products(d, f, T, xd, yd):
+    """Row 1 holds an infinity, row 2 overflows h, row 3 holds a NaN; the others are ordinary."""
+    E = 3
+    conv, mats = positive(d + T, E, d, f)
+    W = pack(conv)
+    rng = np.random.default_rng(T)
+    x = ref.bf16(rng.uniform(0.0, 1.0, size=(T, d)).astype(np.float32))
+    x[1, 7], x[2], x[3, d - 1] = np.inf, 2.0 ** 90, np.nan
+    logits = rng.standard_normal((T, E)).astype(np.float32)
+    ordinary = np.arange(T)
+    ordinary = ordinary[(ordinary < 1) | (ordinary > 3)]
+    safe = x.astype(np.float64)
+    safe[1:4] = 0.0
+    parts = ref.SPLIT if yd == F32 else ref.PAIR
+    want = ref.layer(safe, logits, mats, 1, 0.0, parts)
+    calls = [moe.moe_layer_mxfp4(W, cuda(x).to(xd), cuda(logits), 1, y=torch.empty((T, d), dtype=yd, device="cuda"))["y"]]
+    if yd == F32:  # either family, whatever the layer took
+        xg, offsets, inv = cuda(x).to(xd)[cuda(want["perm"]).long()], cuda(want["offsets"]), cuda(want["inv_perm"]).long()
+        for path in (moe.MOE_FFN_STREAM, moe.MOE_FFN_GROUPED)[T > 72:]:
+            calls.append(moe.moe_expert_ffn(W, xg, offsets, path=path)[inv])
+    for y in calls:
+        check(y[cuda(ordinary)], want["y"][ordinary], want["bound"][ordinary], yd)
+        got = y[1:4].float().cpu().numpy()
+        assert np.isposinf(got[:2]).all() and np.isnan(got[2]).all()
+    W.free()

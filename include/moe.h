@@ -220,7 +220,8 @@ size_t moe_expert_ffn_noalloc_max_bytes(void);
  *            of the first / second projection (0 otherwise).  The first projection's features
  *            count w1 and w3 columns together.  By the rows per expert, which only the device
  *            knows, the kernel may take tiles of 160 rows x 192..512 features instead:
- *            moe_expert_ffn_tiles says when.
+ *            moe_expert_ffn_tiles says when.  (MXFP4 handles: the tiles of bf16 rows; fp32 rows take
+ *            the second projection's for both.)
  * Returns MOE_ERR_UNSUPPORTED if a forced family cannot run the shape.
  */
 typedef struct {

@@ -9,7 +9,7 @@
 // 128 reduction indices a stage.
 //   * tile: up to RBM (2 or 8) blocks of 16 rows of one expert x 256 features; an expert's blocks are dealt
 //     evenly to its tiles, and the loop exists once per number of blocks.
-//   * two workgroups per CU, or four: one's prologue and epilogue run under the other's loop.
+//   * two to four workgroups per CU: one's prologue and epilogue run under the other's loop.
 //   * a step waits for its stage, meets the other waves at a barrier (which also frees the stage of
 //     the step before), requests the operands D steps ahead, and multiplies.
 //   * few tiles (second projection): the reduction is cut in S parts, every part a slab of partial

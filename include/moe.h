@@ -37,7 +37,8 @@ extern "C" {
 typedef enum {
     MOE_F32 = 0,
     MOE_BF16 = 1,
-    MOE_MXFP4 = 2 /* of a packed weight handle only: moe_weights_pack_mxfp4 */
+    MOE_MXFP4 = 2, /* of a packed weight handle only: moe_weights_pack_mxfp4 */
+    MOE_INT8 = 3   /* of a packed weight handle (moe_weights_pack_int8) and of moe_layer_int8's rows */
 } moe_dtype_t;
 
 typedef enum {
@@ -140,6 +141,52 @@ int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int E, int
 int moe_weights_pack_mxfp4(const uint8_t* w1_codes, const uint8_t* w1_scales, const uint8_t* w3_codes,
                            const uint8_t* w3_scales, const uint8_t* w2_codes, const uint8_t* w2_scales, int E, int d, int f,
                            moe_weights_t** out, void* stream);
+
+/*
+ * Matrices and rows in 8-bit integers, symmetric, with one scale per output channel of a matrix and one
+ * per row (token).  For the values v of a channel or a row:
+ *   scale = max|v| / 127, rounded to fp32;   code = v / scale to the nearest integer, ties to even
+ * so codes lie in [-127, 127].  All zeros: scale 0 and codes 0.  Values with a NaN or an infinity among
+ * them: scale NaN and codes 0, so every product with that row (or channel) is NaN and no other is touched.
+ * A stack of matrices W [E,K,C] (y = x.W) is held channel by channel,
+ *   codes [E,C,K] int8,  scales [E,C] fp32
+ * and rows x [T,K] are codes [T,K], scales [T].
+ * moe_int8_quantize, moe_int8_quantize_rows: from fp32 or bf16; moe_int8_dequantize, moe_int8_dequantize_rows:
+ *   code * scale, rounded to the output's type.
+ *   1 <= E <= 64, K a multiple of 16 up to 2^17, 1 <= C <= 2^20, T >= 0 (T*K < 2^40); no output may overlap an
+ *   input or another output.
+ */
+int moe_int8_quantize(const void* w, moe_dtype_t w_dtype, int E, int K, int C, int8_t* codes, float* scales, void* stream);
+int moe_int8_dequantize(const int8_t* codes, const float* scales, int E, int K, int C, void* w, moe_dtype_t w_dtype,
+                        void* stream);
+int moe_int8_quantize_rows(const void* x, moe_dtype_t x_dtype, int T, int K, int8_t* codes, float* scales, void* stream);
+int moe_int8_dequantize_rows(const int8_t* codes, const float* scales, int T, int K, void* x, moe_dtype_t x_dtype,
+                             void* stream);
+/*
+ * The product of 8-bit rows with an 8-bit matrix, or with one matrix per expert:
+ *   y[i,c] = x_scales[i] * w_scales[e,c] * sum_k x_codes[i,k] * w_codes[e,c,k],   i in [offsets[e], offsets[e+1])
+ * The sum is exact (32-bit integers), so results do not depend on its order; the scales are applied in fp32 and y is
+ * rounded once to its type.
+ *   x_codes [M,K], x_scales [M]; w_codes [E,C,K], w_scales [E,C]; codes in [-127, 127] (-128 may overflow a sum)
+ *   offsets [E+1] int32 DEVICE, offsets[0] = 0, non-decreasing, offsets[E] <= M: rows behind are left as they were;
+ *           NULL with E = 1: the matrix serves all M rows
+ *   y [M,C] of y_dtype (fp32 or bf16) out, no overlap with an input
+ *   0 <= M < 2^24, K a multiple of 16 up to 2^17, 1 <= C <= 2^20
+ */
+int moe_int8_matmul(const int8_t* x_codes, const float* x_scales, int M, const int8_t* w_codes, const float* w_scales, int E,
+                    int K, int C, const int32_t* offsets, void* y, moe_dtype_t y_dtype, void* stream);
+/*
+ * moe_weights_pack for matrices in 8 bits (w1, w3: K = d, C = f; w2: K = f, C = d; d and f multiples of 64 up to
+ * 2^17), one device copy in the order the kernels read.  The handle serves moe_expert_ffn, moe_expert_ffn_path
+ * (AUTO: STREAM where rows are few, else GROUPED; MID is unsupported), _tokens, _noalloc, _parts (one slab),
+ * moe_layer and moe_layer_int8 below; the decode calls (moe_decode_layer, moe_decode_block) are unsupported.
+ * Rows x and h = silu(a)*b are each brought to 8 bits with a scale per row; everything else is fp32.  A value of h
+ * within fp32 rounding of a border between two codes may take either.
+ * Rows that offsets do not cover are left as they were.
+ */
+int moe_weights_pack_int8(const int8_t* w1_codes, const float* w1_scales, const int8_t* w3_codes, const float* w3_scales,
+                          const int8_t* w2_codes, const float* w2_scales, int E, int d, int f, moe_weights_t** out,
+                          void* stream);
 
 int moe_weights_free(moe_weights_t* w);
 /* Device bytes held by a packed handle (0 for NULL). HOST query. */
@@ -315,6 +362,41 @@ int moe_layer_mxfp4(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, 
                     void* workspace, size_t workspace_bytes, void* y, moe_dtype_t y_dtype, void* stream);
 /* HOST query; 0 for arguments outside the domain. */
 size_t moe_layer_mxfp4_workspace(int T, int E, int k, int d, int f);
+
+/*
+ * The whole layer over 8-bit experts, from tokens and router logits to tokens: moe_route, moe_permute without rows,
+ * the expert FFN and the gate-weighted sum, y rounded once to its type.
+ *   W of moe_weights_pack_int8; logits [T,E] fp32, E the handle's
+ *   x [T,d] of x_dtype: fp32 or bf16 (brought to 8 bits here, x_scales NULL), or MOE_INT8: codes, with x_scales [T]
+ *     (as moe_int8_quantize_rows or moe_block_norm leave them)
+ *   idx, weights, counts, offsets, perm, inv_perm: as moe_route / moe_permute, all written
+ *   workspace >= moe_layer_int8_workspace(T, E, k, d, f) bytes, 256-byte aligned
+ *   y [T,d] of y_dtype (fp32 or bf16) out.  No output and no byte of the workspace may overlap x, x_scales or logits.
+ * T == 0 writes counts and offsets only.  Logits that hold NaN: as moe_layer_mxfp4.
+ */
+int moe_layer_int8(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, const float* x_scales, const float* logits,
+                   int T, int k, int32_t* idx, float* weights, int32_t* counts, int32_t* offsets, int32_t* perm,
+                   int32_t* inv_perm, void* workspace, size_t workspace_bytes, void* y, moe_dtype_t y_dtype, void* stream);
+/* HOST query; 0 for arguments outside the domain. */
+size_t moe_layer_int8_workspace(int T, int E, int k, int d, int f);
+
+/*
+ * The norms around a block in one launch: the one after it, the gated residual add, and the one before the next block.
+ *     u[t,:]  = norm_after ? y[t,:] / sqrt(mean(y[t,:]^2) + eps) * gain_after : y[t,:]
+ *     x'[t,:] = x[t,:] + residual_scale * row_gate[t] * gate * u[t,:]            (y NULL: x' = x)
+ *     h[t,:]  = x'[t,:] / sqrt(mean(x'[t,:]^2) + eps) * gain_before
+ * computed in 64 bits, every output rounded once from there (h from the x' before its rounding).
+ *   x [T,d] of x_dtype, y [T,d] of y_dtype (fp32 or bf16), y or NULL (then norm_after 0 and no gain_after, gates or x_out
+ *   needed); gain_after [d], gain_before [d], gate [d], row_gate [T]: fp32, each or NULL for ones
+ *   x_out [T,d] of x_dtype out or NULL; may be x itself
+ *   h [T,d] of h_dtype (fp32 or bf16) out or NULL
+ *   h_codes [T,d] int8, h_scales [T] fp32 out, both or neither: h in 8 bits (see moe_int8_quantize_rows)
+ *   eps > 0; d a multiple of 64 up to 2^20 (2^17 with h_codes).  At least one output; no other overlap between arguments.
+ */
+int moe_block_norm(const void* x, moe_dtype_t x_dtype, const void* y, moe_dtype_t y_dtype, int T, int d, int norm_after,
+                   const float* gain_after, const float* gate, const float* row_gate, float residual_scale,
+                   const float* gain_before, float eps, void* x_out, void* h, moe_dtype_t h_dtype, int8_t* h_codes,
+                   float* h_scales, void* stream);
 
 /*
  * One decode step of the layer in three launches, two on an MXFP4 handle (Sec. 3.3 "Execution" for a handful of

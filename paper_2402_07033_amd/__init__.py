@@ -19,7 +19,10 @@ from .binding import (ORCH_CPU, ORCH_GPU_RESIDENT, ORCH_GPU_TRANSFER, ORCH_SKIP,
                       moe_gate_sums, moe_gate_sums_stride, moe_rmsnorm_router_logits, moe_route, moe_route_permute,
                       moe_router_logits, moe_set_ffn_mid_event, moe_stack_forward,
                       moe_status_string, moe_weights_free, moe_weights_pack, moe_weights_pack_mxfp4,
-                      moe_layer_mxfp4, moe_layer_mxfp4_workspace, moe_mxfp4_dequantize, moe_mxfp4_quantize)
+                      moe_layer_mxfp4, moe_layer_mxfp4_workspace, moe_mxfp4_dequantize, moe_mxfp4_quantize,
+                      MOE_INT8, moe_block_norm, moe_int8_dequantize, moe_int8_dequantize_rows, moe_int8_matmul,
+                      moe_int8_quantize, moe_int8_quantize_rows, moe_layer_int8, moe_layer_int8_workspace,
+                      moe_weights_pack_int8)
 
 __all__ = [
     "ORCH_CPU", "ORCH_GPU_RESIDENT", "ORCH_GPU_TRANSFER", "ORCH_SKIP", "OrchLayer",
@@ -35,5 +38,7 @@ __all__ = [
     "moe_gate_sums", "moe_gate_sums_stride", "moe_rmsnorm_router_logits", "moe_route", "moe_route_permute", "moe_router_logits",
     "moe_set_ffn_mid_event", "moe_stack_forward", "moe_status_string", "moe_weights_free",
     "moe_weights_pack", "MOE_MXFP4", "moe_weights_pack_mxfp4", "moe_layer_mxfp4", "moe_layer_mxfp4_workspace",
-    "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
+    "moe_mxfp4_quantize", "moe_mxfp4_dequantize", "MOE_INT8", "moe_int8_quantize", "moe_int8_dequantize",
+    "moe_int8_quantize_rows", "moe_int8_dequantize_rows", "moe_int8_matmul", "moe_weights_pack_int8", "moe_layer_int8",
+    "moe_layer_int8_workspace", "moe_block_norm",
 ]

@@ -9,7 +9,7 @@ from typing import Optional
 
 import torch
 
-MOE_F32, MOE_BF16, MOE_MXFP4 = 0, 1, 2
+MOE_F32, MOE_BF16, MOE_MXFP4, MOE_INT8 = 0, 1, 2, 3
 MOE_FFN_AUTO, MOE_FFN_STREAM, MOE_FFN_GROUPED, MOE_FFN_MID = 0, 1, 2, 3
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -26,7 +26,9 @@ EXPORTS = ("moe_status_string", "moe_route", "moe_permute", "moe_layer", "moe_we
            "moe_norm_route_permute", "moe_combine_residual", "moe_combine_norm_route_permute",
            "moe_rmsnorm_router_logits", "moe_gate_sums", "moe_gate_sums_stride",
            "moe_decode_block_supported", "moe_mxfp4_quantize", "moe_mxfp4_dequantize", "moe_weights_pack_mxfp4",
-           "moe_layer_mxfp4", "moe_layer_mxfp4_workspace")
+           "moe_layer_mxfp4", "moe_layer_mxfp4_workspace", "moe_int8_quantize", "moe_int8_dequantize",
+           "moe_int8_quantize_rows", "moe_int8_dequantize_rows", "moe_int8_matmul", "moe_weights_pack_int8",
+           "moe_layer_int8", "moe_layer_int8_workspace", "moe_block_norm")
 PROBE_EXPORTS = ("moe_set_ffn_mid_event", "moe_mfma_rate_probe", "moe_hbm_read_probe")
 ORCH_EXPORTS = ("moe_orch_place", "moe_orch_hit_rate", "moe_orch_decide", "moe_orch_cpu_expert_ffn",
                 "moe_orch_layer_create", "moe_orch_layer_free", "moe_orch_calibrate",
@@ -144,6 +146,19 @@ def lib():
         L.moe_layer_mxfp4.restype = C.c_int
         L.moe_layer_mxfp4_workspace.argtypes = [i32] * 5
         L.moe_layer_mxfp4_workspace.restype = C.c_size_t
+        L.moe_int8_quantize.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp]
+        L.moe_int8_dequantize.argtypes = [vp, vp, i32, i32, i32, vp, i32, vp]
+        L.moe_int8_quantize_rows.argtypes = [vp, i32, i32, i32, vp, vp, vp]
+        L.moe_int8_dequantize_rows.argtypes = [vp, vp, i32, i32, vp, i32, vp]
+        L.moe_int8_matmul.argtypes = [vp, vp, i32, vp, vp, i32, i32, i32, vp, vp, i32, vp]
+        L.moe_weights_pack_int8.argtypes = [vp] * 6 + [i32] * 3 + [C.POINTER(vp), vp]
+        L.moe_layer_int8.argtypes = [vp, vp, i32, vp, vp, i32, i32] + [vp] * 7 + [C.c_size_t, vp, i32, vp]
+        L.moe_layer_int8_workspace.argtypes = [i32] * 5
+        L.moe_block_norm.argtypes = [vp, i32, vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, f32, vp, vp, i32, vp, vp, vp]
+        for n in ("moe_int8_quantize", "moe_int8_dequantize", "moe_int8_quantize_rows", "moe_int8_dequantize_rows",
+                  "moe_int8_matmul", "moe_weights_pack_int8", "moe_layer_int8", "moe_block_norm"):
+            getattr(L, n).restype = C.c_int
+        L.moe_layer_int8_workspace.restype = C.c_size_t
         dp = C.POINTER(C.c_double)
         L.moe_orch_place.argtypes = [vp, i32, i32, i32, vp]
         L.moe_orch_hit_rate.argtypes = [vp, vp, i32, i32]
@@ -360,6 +375,120 @@ def moe_weights_pack_mxfp4(w1, w3, w2, stream=None) -> PackedWeights:
     _check(lib().moe_weights_pack_mxfp4(_ptr(w1[0]), _ptr(w1[1]), _ptr(w3[0]), _ptr(w3[1]), _ptr(w2[0]), _ptr(w2[1]),
                                         E, d, f, C.byref(h), _stream(stream)), "moe_weights_pack_mxfp4")
     return PackedWeights(h.value, E, d, f, MOE_MXFP4)
+
+
+def _float_type(dtype) -> int:
+    if dtype == torch.float32:
+        return MOE_F32
+    if dtype == torch.bfloat16:
+        return MOE_BF16
+    raise TypeError(f"unsupported dtype {dtype}")
+
+
+def _out(t, shape, dtype, device, what: str):
+    """The caller's output tensor, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: expected {list(shape)}")
+    return _dev(t, dtype, what)
+
+
+def _int8_pair(pair, dims: int, what: str):
+    """(codes int8 [..., K], scales fp32 [...]) of a stack of matrices (dims 3) or of rows (dims 2)."""
+    codes, scales = pair
+    _dev(codes, torch.int8, what + " codes")
+    _dev(scales, torch.float32, what + " scales")
+    if codes.dim() != dims or tuple(scales.shape) != tuple(codes.shape[:-1]):
+        raise ValueError(f"{what}: expected codes [{'E,C' if dims == 3 else 'T'},K] and scales without the K")
+    _here(codes, scales)
+    return codes, scales
+
+
+def moe_int8_quantize(w: torch.Tensor, codes=None, scales=None, stream=None):
+    """w [E,K,C] (fp32 or bf16, K a multiple of 16 along the reduction) -> 8-bit (codes int8 [E,C,K],
+    scales fp32 [E,C], one per output channel)."""
+    dt = _act_dtype(w)
+    _dev(w, w.dtype, "w")
+    if w.dim() != 3:
+        raise ValueError("w: expected [E,K,C]")
+    E, K, c = w.shape
+    codes = _out(codes, (E, c, K), torch.int8, w.device, "codes")
+    scales = _out(scales, (E, c), torch.float32, w.device, "scales")
+    _here(w, codes, scales)
+    _check(lib().moe_int8_quantize(_ptr(w), dt, E, K, c, _ptr(codes), _ptr(scales), _stream(stream)),
+           "moe_int8_quantize")
+    return codes, scales
+
+
+def moe_int8_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.bfloat16, w=None, stream=None):
+    """codes [E,C,K], scales [E,C] -> code * scale, [E,K,C] of `dtype` (fp32 or bf16)."""
+    _int8_pair((codes, scales), 3, "matrix")
+    E, c, K = codes.shape
+    w = _out(w, (E, K, c), dtype if w is None else w.dtype, codes.device, "w")
+    _here(w)
+    _check(lib().moe_int8_dequantize(_ptr(codes), _ptr(scales), E, K, c, _ptr(w), _float_type(w.dtype), _stream(stream)),
+           "moe_int8_dequantize")
+    return w
+
+
+def moe_int8_quantize_rows(x: torch.Tensor, codes=None, scales=None, stream=None):
+    """x [T,K] (fp32 or bf16, K a multiple of 16) -> 8-bit rows (codes int8 [T,K], scales fp32 [T], one per row)."""
+    dt = _act_dtype(x)
+    _dev(x, x.dtype, "x")
+    if x.dim() != 2:
+        raise ValueError("x: expected [T,K]")
+    T, K = x.shape
+    codes = _out(codes, (T, K), torch.int8, x.device, "codes")
+    scales = _out(scales, (T,), torch.float32, x.device, "scales")
+    _here(x, codes, scales)
+    _check(lib().moe_int8_quantize_rows(_ptr(x), dt, T, K, _ptr(codes), _ptr(scales), _stream(stream)),
+           "moe_int8_quantize_rows")
+    return codes, scales
+
+
+def moe_int8_dequantize_rows(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.bfloat16, x=None, stream=None):
+    """codes [T,K], scales [T] -> code * scale, [T,K] of `dtype` (fp32 or bf16)."""
+    _int8_pair((codes, scales), 2, "rows")
+    x = _out(x, tuple(codes.shape), dtype if x is None else x.dtype, codes.device, "x")
+    _here(x)
+    _check(lib().moe_int8_dequantize_rows(_ptr(codes), _ptr(scales), codes.shape[0], codes.shape[1], _ptr(x),
+                                          _float_type(x.dtype), _stream(stream)), "moe_int8_dequantize_rows")
+    return x
+
+
+def moe_int8_matmul(x, w, offsets=None, dtype=torch.bfloat16, y=None, stream=None) -> torch.Tensor:
+    """8-bit rows x = (codes [M,K], scales [M]) times 8-bit matrices w = (codes [E,C,K], scales [E,C]) -> y [M,C]
+    of `dtype` (fp32 or bf16).  offsets int32 [E+1] on the device: expert e's rows are [offsets[e], offsets[e+1]);
+    without them E = 1."""
+    xq, xs = _int8_pair(x, 2, "x")
+    wq, ws = _int8_pair(w, 3, "w")
+    M, K = xq.shape
+    E, c = wq.shape[:2]
+    if wq.shape[2] != K:
+        raise ValueError("x and w have different reductions")
+    if offsets is not None:
+        _dev(offsets, torch.int32, "offsets")
+        if offsets.numel() != E + 1:
+            raise ValueError("offsets: expected [E+1]")
+    y = _out(y, (M, c), dtype if y is None else y.dtype, xq.device, "y")
+    _here(y, offsets)
+    _check(lib().moe_int8_matmul(_ptr(xq), _ptr(xs), M, _ptr(wq), _ptr(ws), E, K, c, _ptr(offsets), _ptr(y),
+                                 _float_type(y.dtype), _stream(stream)), "moe_int8_matmul")
+    return y
+
+
+def moe_weights_pack_int8(w1, w3, w2, stream=None) -> PackedWeights:
+    """A handle over 8-bit expert matrices: w1, w3 and w2 are pairs (codes, scales) as moe_int8_quantize
+    leaves them for w1, w3 [E,d,f] and w2 [E,f,d]."""
+    (c1, s1), (c3, s3), (c2, s2) = (_int8_pair(w, 3, n) for w, n in ((w1, "w1"), (w3, "w3"), (w2, "w2")))
+    E, f, d = c1.shape
+    if tuple(c3.shape) != (E, f, d) or tuple(c2.shape) != (E, d, f):
+        raise ValueError("the matrices must be w1,w3 [E,d,f] and w2 [E,f,d]")
+    h = C.c_void_p()
+    _check(lib().moe_weights_pack_int8(_ptr(c1), _ptr(s1), _ptr(c3), _ptr(s3), _ptr(c2), _ptr(s2), E, d, f, C.byref(h),
+                                       _stream(stream)), "moe_weights_pack_int8")
+    return PackedWeights(h.value, E, d, f, MOE_INT8)
 
 
 def moe_weights_free(w: PackedWeights):
@@ -759,6 +888,94 @@ def moe_layer_mxfp4(W: PackedWeights, x: torch.Tensor, logits: torch.Tensor, k: 
     return dict(idx=idx, w=weights, counts=counts, offsets=offsets, perm=perm, inv_perm=inv_perm, y=y)
 
 
+def moe_layer_int8_workspace(T: int, E: int, k: int, d: int, f: int) -> int:
+    """Bytes of scratch moe_layer_int8 needs (host query)."""
+    return int(lib().moe_layer_int8_workspace(T, E, k, d, f))
+
+
+def moe_layer_int8(W: PackedWeights, x, logits: torch.Tensor, k: int, idx=None, weights=None, out=None, workspace=None,
+                   y=None, dtype=None, stream=None) -> dict:
+    """The whole layer over 8-bit experts: x [T,d] (fp32 or bf16, or a pair (codes, scales) of 8-bit rows), logits
+    fp32 [T,E] -> y [T,d] of `dtype` (x's type if it is none; bf16 for 8-bit rows).  `out` = (counts, offsets, perm,
+    inv_perm)."""
+    _dev(logits, torch.float32, "logits")
+    scales = None
+    if isinstance(x, (tuple, list)):
+        x, scales = _int8_pair(x, 2, "x")
+        xdt = MOE_INT8
+    else:
+        xdt = _act_dtype(x)
+        _dev(x, x.dtype, "x")
+    T, E = logits.shape
+    d, N, dev = W.d, T * k, x.device
+    if E != W.E or tuple(x.shape) != (T, d):
+        raise ValueError(f"expected x [T,{d}] and logits [T,{W.E}]")
+    if not 1 <= k <= min(E, _MAX_K) or N >= _MAX_N:
+        raise MoeError(_INVALID_ARG, "moe_layer_int8")  # before N rows are allocated
+    i32 = torch.int32
+    idx = torch.empty((T, k), dtype=i32, device=dev) if idx is None else idx
+    weights = torch.empty((T, k), dtype=torch.float32, device=dev) if weights is None else weights
+    if out is None:
+        out = tuple(torch.empty(n, dtype=i32, device=dev) for n in (E, E + 1, N, N))
+    counts, offsets, perm, inv_perm = out[:4]
+    if workspace is None:
+        workspace = _scratch(moe_layer_int8_workspace(T, E, k, d, W.f), dev, stream)
+    if y is None:
+        if dtype is None:
+            dtype = torch.bfloat16 if scales is not None else x.dtype
+        y = torch.empty((T, d), dtype=dtype, device=dev)
+    for t, n, dt, what in ((idx, N, i32, "idx"), (weights, N, torch.float32, "weights"), (counts, E, i32, "counts"),
+                           (offsets, E + 1, i32, "offsets"), (perm, N, i32, "perm"), (inv_perm, N, i32, "inv_perm"),
+                           (y, T * d, y.dtype, "y"), (workspace, 0, workspace.dtype, "workspace")):
+        _dev(t, dt, what)
+        if t.numel() < n:
+            raise ValueError(f"{what}: {t.numel()} elements, {n} are written")
+    _here(x, logits, idx, weights, counts, offsets, perm, inv_perm, workspace, y)
+    _check(lib().moe_layer_int8(W.handle, x.data_ptr(), xdt, _ptr(scales), logits.data_ptr(), T, k, idx.data_ptr(),
+                                weights.data_ptr(), counts.data_ptr(), offsets.data_ptr(), perm.data_ptr(),
+                                inv_perm.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                y.data_ptr(), _float_type(y.dtype), _stream(stream)), "moe_layer_int8")
+    return dict(idx=idx, w=weights, counts=counts, offsets=offsets, perm=perm, inv_perm=inv_perm, y=y)
+
+
+def moe_block_norm(x: torch.Tensor, y=None, norm_after: bool = False, gain_after=None, gate=None, row_gate=None,
+                   residual_scale: float = 1.0, gain_before=None, eps: float = 1e-5, x_out=None, h=None,
+                   h_dtype=torch.float32, int8: bool = False, codes=None, scales=None, stream=None) -> dict:
+    """The norms around a block, one launch: u = y, or rmsnorm(y) * gain_after; x' = x + residual_scale * gate *
+    row_gate * u (gate [d], row_gate [T]); h = rmsnorm(x') * gain_before.  x, y [T,d] fp32 or bf16, gains and gates
+    fp32.  Returns x (x', of x's type; x_out may be x itself; x itself where there is no y), h of `h_dtype` (None: no
+    h) and with int8=True codes [T,d] and scales [T], h in 8 bits."""
+    xdt = _act_dtype(x)
+    _dev(x, x.dtype, "x")
+    if x.dim() != 2:
+        raise ValueError("x: expected [T,d]")
+    T, d = x.shape
+    if y is not None:
+        _dev(y, y.dtype, "y")
+        if tuple(y.shape) != (T, d):
+            raise ValueError("y: expected x's shape")
+        x_out = _out(x_out, (T, d), x.dtype, x.device, "x_out")
+    elif x_out is not None:
+        x_out = _out(x_out, (T, d), x.dtype, x.device, "x_out")
+    for t, n, what in ((gain_after, d, "gain_after"), (gate, d, "gate"), (row_gate, T, "row_gate"),
+                       (gain_before, d, "gain_before")):
+        if t is not None and _dev(t, torch.float32, what).numel() != n:
+            raise ValueError(f"{what}: expected [{n}]")
+    if h is not None or h_dtype is not None:
+        h = _out(h, (T, d), h_dtype if h is None else h.dtype, x.device, "h")
+    if int8:
+        codes = _out(codes, (T, d), torch.int8, x.device, "codes")
+        scales = _out(scales, (T,), torch.float32, x.device, "scales")
+    elif codes is not None or scales is not None:
+        raise ValueError("codes and scales are outputs of int8=True")
+    _here(x, y, gain_after, gate, row_gate, gain_before, x_out, h, codes, scales)
+    _check(lib().moe_block_norm(_ptr(x), xdt, _ptr(y), MOE_F32 if y is None else _act_dtype(y), T, d, int(norm_after),
+                                _ptr(gain_after), _ptr(gate), _ptr(row_gate), residual_scale, _ptr(gain_before), eps,
+                                _ptr(x_out), _ptr(h), MOE_F32 if h is None else _float_type(h.dtype), _ptr(codes),
+                                _ptr(scales), _stream(stream)), "moe_block_norm")
+    return dict(x=x if x_out is None else x_out, h=h, codes=codes, scales=scales)
+
+
 def moe_route_permute(logits: torch.Tensor, k: int, x: torch.Tensor, idx, weights, out,
                       stream=None):
     """Fused moe_route + moe_permute for T <= 16 (fp32 x); outputs as in the two calls."""
@@ -836,7 +1053,7 @@ class StackBuffers:
         self.max_parts, self.rows_through_perm = 1, True
         for t in {w_dtype} if isinstance(w_dtype, int) else set(w_dtype):
             try:
-                plan = moe_expert_ffn_plan(N, E, d, f, MOE_MXFP4 if t == MOE_MXFP4 else MOE_BF16)
+                plan = moe_expert_ffn_plan(N, E, d, f, t if t in (MOE_MXFP4, MOE_INT8) else MOE_BF16)
             except MoeError:   # a shape only the fp32 kernels serve
                 plan = dict(n_parts=1, path=MOE_FFN_STREAM)
             self.max_parts = max(self.max_parts, plan["n_parts"])

@@ -1,6 +1,7 @@
 // C ABI of libmoe_hip (include/moe.h): argument validation on the host, then
 // dispatch to the kernel launchers.  Nothing is enqueued when validation fails.
 #include "moe_internal.h"
+#include "moe_i8.h"
 #include "moe_mx.h"
 
 // mean rows per expert up to which AUTO names MID: no crossover, but the range in which it serves
@@ -85,6 +86,9 @@ static int ffn_args(const moe_weights_t* W, const void* xg, moe_dtype_t act_dtyp
         if (path == MOE_FFN_AUTO) path = moe_mx_auto_path(N, W->E, W->d, W->f);
         served = path == MOE_FFN_STREAM ? moe_mx_stream_serves(N, W->E, W->d, W->f)
                                         : path == MOE_FFN_GROUPED && moe_mx_gemm_supported(N, W->E, W->d, W->f);
+    } else if (W->dtype == MOE_INT8) {
+        if (path == MOE_FFN_AUTO) path = moe_i8_auto_path(N, W->E, W->d, W->f);
+        served = moe_i8_ffn_supported(path, N, W->E, W->d, W->f);
     } else {
         if (path == MOE_FFN_AUTO) path = moe_ffn_auto_path(N, W->E, W->d, W->f);
         served = path == MOE_FFN_STREAM ? moe_ffn_stream_serves(N, W->E, W->d, W->f)
@@ -128,6 +132,8 @@ static int ffn_launch(const moe_weights_t* W, const void* xg, moe_dtype_t act_dt
     if (W->dtype == MOE_MXFP4)
         return path == MOE_FFN_STREAM ? moe_mx_stream_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, nullptr, s)
                                       : moe_mx_gemm_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, true, nullptr, nullptr, s);
+    if (W->dtype == MOE_INT8)
+        return moe_i8_ffn_launch(W, xg, act_dtype, nullptr, perm ? N / k : N, perm, k, offsets, N, workspace, yg, path, s);
     if (path == MOE_FFN_STREAM)
         return moe_ffn_stream_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, nullptr, s);
     return moe_ffn_grouped_launch(path == MOE_FFN_MID, W, xg, act_dtype, perm, k, offsets, N, workspace, yg, s);
@@ -239,6 +245,194 @@ int moe_weights_pack_mxfp4(const uint8_t* w1_codes, const uint8_t* w1_scales, co
     return moe_mx_pack_impl(codes, scales, E, d, f, out, (hipStream_t)stream);
 }
 
+// ---- 8-bit integers ----
+static bool int8_k_ok(int K) { return K >= 16 && K % 16 == 0 && K <= I8_MAX_K; }
+static bool int8_dims_ok(int E, int K, int C) {
+    return E >= 1 && E <= MOE_MAX_E && int8_k_ok(K) && C >= 1 && C <= (1 << 20);
+}
+static bool float_dtype(moe_dtype_t t) { return t == MOE_F32 || t == MOE_BF16; }
+static size_t float_bytes(moe_dtype_t t, size_t n) { return n * (t == MOE_BF16 ? 2 : 4); }
+
+// The arguments of the four conversions: n values in floats against their codes and `scales` scales.
+static int int8_convert_args(const void* v, moe_dtype_t dtype, size_t n, const int8_t* codes, const float* scales,
+                             size_t n_scales) {
+    if (!v || !codes || !scales || !moe_aligned16(v) || !moe_aligned16(codes) || !moe_aligned16(scales))
+        return MOE_ERR_INVALID_ARG;
+    const size_t vb = float_bytes(dtype, n), sb = n_scales * sizeof(float);
+    return ranges_overlap(v, vb, codes, n) || ranges_overlap(v, vb, scales, sb) || ranges_overlap(codes, n, scales, sb)
+               ? MOE_ERR_INVALID_ARG
+               : MOE_OK;
+}
+
+int moe_int8_quantize(const void* w, moe_dtype_t w_dtype, int E, int K, int C, int8_t* codes, float* scales, void* stream) {
+    if (!int8_dims_ok(E, K, C) || !float_dtype(w_dtype)) return MOE_ERR_INVALID_ARG;
+    const int rc = int8_convert_args(w, w_dtype, (size_t)E * K * C, codes, scales, (size_t)E * C);
+    return rc != MOE_OK ? rc : moe_i8_quantize_launch(w, w_dtype, E, K, C, codes, scales, (hipStream_t)stream);
+}
+
+int moe_int8_dequantize(const int8_t* codes, const float* scales, int E, int K, int C, void* w, moe_dtype_t w_dtype,
+                        void* stream) {
+    if (!int8_dims_ok(E, K, C) || !float_dtype(w_dtype)) return MOE_ERR_INVALID_ARG;
+    const int rc = int8_convert_args(w, w_dtype, (size_t)E * K * C, codes, scales, (size_t)E * C);
+    return rc != MOE_OK ? rc : moe_i8_dequantize_launch(codes, scales, E, K, C, w, w_dtype, (hipStream_t)stream);
+}
+
+static bool int8_rows_ok(int T, int K) { return T >= 0 && int8_k_ok(K); }
+
+int moe_int8_quantize_rows(const void* x, moe_dtype_t x_dtype, int T, int K, int8_t* codes, float* scales, void* stream) {
+    if (!int8_rows_ok(T, K) || !float_dtype(x_dtype)) return MOE_ERR_INVALID_ARG;
+    if (T == 0) return MOE_OK;
+    const int rc = int8_convert_args(x, x_dtype, (size_t)T * K, codes, scales, (size_t)T);
+    return rc != MOE_OK ? rc : moe_i8_rows_launch(x, x_dtype, T, K, codes, scales, (hipStream_t)stream);
+}
+
+int moe_int8_dequantize_rows(const int8_t* codes, const float* scales, int T, int K, void* x, moe_dtype_t x_dtype,
+                             void* stream) {
+    if (!int8_rows_ok(T, K) || !float_dtype(x_dtype)) return MOE_ERR_INVALID_ARG;
+    if (T == 0) return MOE_OK;
+    const int rc = int8_convert_args(x, x_dtype, (size_t)T * K, codes, scales, (size_t)T);
+    return rc != MOE_OK ? rc : moe_i8_rows_back_launch(codes, scales, T, K, x, x_dtype, (hipStream_t)stream);
+}
+
+int moe_int8_matmul(const int8_t* x_codes, const float* x_scales, int M, const int8_t* w_codes, const float* w_scales, int E,
+                    int K, int C, const int32_t* offsets, void* y, moe_dtype_t y_dtype, void* stream) {
+    if (!int8_dims_ok(E, K, C) || M < 0 || M >= MOE_MAX_N || !float_dtype(y_dtype) || (!offsets && E != 1))
+        return MOE_ERR_INVALID_ARG;
+    if (M == 0) return MOE_OK;
+    if (!x_codes || !x_scales || !w_codes || !w_scales || !y || !moe_aligned16(x_codes) || !moe_aligned16(x_scales) ||
+        !moe_aligned16(w_codes) || !moe_aligned16(w_scales) || !moe_aligned16(y) || (offsets && !moe_aligned16(offsets)))
+        return MOE_ERR_INVALID_ARG;
+    const size_t yb = float_bytes(y_dtype, (size_t)M * C);
+    if (ranges_overlap(y, yb, x_codes, (size_t)M * K) || ranges_overlap(y, yb, x_scales, (size_t)M * 4) ||
+        ranges_overlap(y, yb, w_codes, (size_t)E * C * K) || ranges_overlap(y, yb, w_scales, (size_t)E * C * 4) ||
+        ranges_overlap(y, yb, offsets, (size_t)(E + 1) * 4))
+        return MOE_ERR_INVALID_ARG;
+    if (!moe_i8_product_supported(M, E, K, C)) return MOE_ERR_UNSUPPORTED;
+    I8Product p = {};
+    p.x = x_codes;
+    p.xs = x_scales;
+    p.k = 1;
+    p.offsets = offsets;
+    p.E = E;
+    p.N = M;
+    p.K = K;
+    p.C = C;
+    p.w = w_codes;
+    p.ws = w_scales;
+    p.y = y;
+    p.y_bf16 = y_dtype == MOE_BF16;
+    return moe_i8_product_launch(p, (hipStream_t)stream);
+}
+
+int moe_weights_pack_int8(const int8_t* w1_codes, const float* w1_scales, const int8_t* w3_codes, const float* w3_scales,
+                          const int8_t* w2_codes, const float* w2_scales, int E, int d, int f, moe_weights_t** out,
+                          void* stream) {
+    if (!out) return MOE_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (E < 1 || E > MOE_MAX_E || !dims_ok(d) || !dims_ok(f) || d > I8_MAX_K || f > I8_MAX_K) return MOE_ERR_INVALID_ARG;
+    const int8_t* codes[3] = {w1_codes, w3_codes, w2_codes};
+    const float* scales[3] = {w1_scales, w3_scales, w2_scales};
+    for (int i = 0; i < 3; i++)
+        if (!codes[i] || !scales[i] || !moe_aligned16(codes[i]) || !moe_aligned16(scales[i])) return MOE_ERR_INVALID_ARG;
+    return moe_i8_pack_impl(codes, scales, E, d, f, out, (hipStream_t)stream);
+}
+
+// what moe_layer_int8 keeps beside the expert FFN's scratch: the experts' rows
+static size_t i8_layer_rows(int N, int d) { return align256((size_t)N * d * sizeof(float)); }
+
+size_t moe_layer_int8_workspace(int T, int E, int k, int d, int f) {
+    if (!tek_ok(T, E, k) || !dims_ok(d) || !dims_ok(f)) return 0;
+    return align256(i8_layer_rows(T * k, d) + moe_i8_ffn_workspace(T * k, E, d, f)) + 256;
+}
+
+int moe_layer_int8(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, const float* x_scales, const float* logits,
+                   int T, int k, int32_t* idx, float* weights, int32_t* counts, int32_t* offsets, int32_t* perm,
+                   int32_t* inv_perm, void* workspace, size_t workspace_bytes, void* y, moe_dtype_t y_dtype, void* stream) {
+    if (!W || W->dtype != MOE_INT8) return MOE_ERR_INVALID_ARG;
+    const int E = W->E, d = W->d, f = W->f;
+    if (!tek_ok(T, E, k) || !counts || !offsets) return MOE_ERR_INVALID_ARG;
+    if ((!float_dtype(x_dtype) && x_dtype != MOE_INT8) || !float_dtype(y_dtype)) return MOE_ERR_INVALID_ARG;
+    const int N = T * k;
+    hipStream_t s = (hipStream_t)stream;
+    if (T == 0)
+        return moe_permute_launch(idx, 0, E, k, nullptr, d, MOE_F32, counts, offsets, perm, inv_perm, nullptr, s);
+    if (!x || !logits || !idx || !weights || !perm || !inv_perm || !y) return MOE_ERR_INVALID_ARG;
+    if ((x_dtype == MOE_INT8) != (x_scales != nullptr)) return MOE_ERR_INVALID_ARG;
+    if (!moe_aligned16(x) || !moe_aligned16(y) || !moe_aligned16(logits) || !moe_aligned16(idx) || !moe_aligned16(weights) ||
+        !moe_aligned16(perm) || !moe_aligned16(inv_perm) || (x_scales && !moe_aligned16(x_scales)))
+        return MOE_ERR_INVALID_ARG;
+    const int path = moe_i8_auto_path(N, E, d, f);
+    if (!moe_i8_ffn_supported(path, N, E, d, f)) return MOE_ERR_UNSUPPORTED;
+    if (!workspace || (((uintptr_t)workspace) & 255u)) return MOE_ERR_WORKSPACE;
+    if (workspace_bytes < moe_layer_int8_workspace(T, E, k, d, f)) return MOE_ERR_WORKSPACE;
+    const size_t td = (size_t)T * d, n4 = (size_t)N * 4, e4 = (size_t)E * 4;
+    const size_t xb = x_dtype == MOE_INT8 ? td : float_bytes(x_dtype, td);
+    const struct { const void* p; size_t bytes; } out[8] = {
+        {idx, n4}, {weights, n4}, {counts, e4}, {offsets, e4 + 4}, {perm, n4}, {inv_perm, n4},
+        {y, float_bytes(y_dtype, td)}, {workspace, workspace_bytes}};
+    for (const auto& o : out)
+        if (ranges_overlap(logits, (size_t)T * E * 4, o.p, o.bytes) || ranges_overlap(x, xb, o.p, o.bytes) ||
+            ranges_overlap(x_scales, (size_t)T * 4, o.p, o.bytes))
+            return MOE_ERR_INVALID_ARG;
+
+    int rc = moe_route_launch(logits, T, E, k, idx, weights, s);
+    if (rc == MOE_OK)
+        rc = moe_permute_launch(idx, T, E, k, nullptr, 0, MOE_F32, counts, offsets, perm, inv_perm, nullptr, s);
+    if (rc != MOE_OK) return rc;
+    float* yg = (float*)workspace;
+    rc = moe_i8_ffn_launch(W, x, x_dtype, x_scales, T, perm, k, offsets, N, (char*)workspace + i8_layer_rows(N, d), yg, path, s);
+    if (rc != MOE_OK) return rc;
+    return moe_mx_combine_launch(yg, 1, 0, inv_perm, weights, T, k, d, y, y_dtype, s);
+}
+
+int moe_block_norm(const void* x, moe_dtype_t x_dtype, const void* y, moe_dtype_t y_dtype, int T, int d, int norm_after,
+                   const float* gain_after, const float* gate, const float* row_gate, float residual_scale,
+                   const float* gain_before, float eps, void* x_out, void* h, moe_dtype_t h_dtype, int8_t* h_codes,
+                   float* h_scales, void* stream) {
+    if (T < 0 || !dims_ok(d) || !(eps > 0.f) || !(eps < INFINITY) || !float_dtype(x_dtype)) return MOE_ERR_INVALID_ARG;
+    if ((y && !float_dtype(y_dtype)) || (h && !float_dtype(h_dtype))) return MOE_ERR_INVALID_ARG;
+    if ((!y && (norm_after || gain_after || gate || row_gate)) || (gain_after && !norm_after)) return MOE_ERR_INVALID_ARG;
+    if ((h_codes == nullptr) != (h_scales == nullptr) || (h_codes && d > I8_MAX_K)) return MOE_ERR_INVALID_ARG;
+    if (T == 0) return MOE_OK;
+    if (!x || (!x_out && !h && !h_codes)) return MOE_ERR_INVALID_ARG;
+    const size_t td = (size_t)T * d, d4 = (size_t)d * 4, t4 = (size_t)T * 4;
+    const struct { const void* p; size_t bytes; } in[6] = {{x, float_bytes(x_dtype, td)}, {y, float_bytes(y_dtype, td)},
+                                                           {gain_after, d4}, {gate, d4}, {row_gate, t4}, {gain_before, d4}};
+    const struct { const void* p; size_t bytes; } out[4] = {{x_out, float_bytes(x_dtype, td)}, {h, float_bytes(h_dtype, td)},
+                                                            {h_codes, td}, {h_scales, t4}};
+    for (const auto& i : in)
+        if (i.p && !moe_aligned16(i.p)) return MOE_ERR_INVALID_ARG;
+    for (int o = 0; o < 4; o++) {
+        if (!out[o].p) continue;
+        if (!moe_aligned16(out[o].p)) return MOE_ERR_INVALID_ARG;
+        for (const auto& i : in)  // (x_out may be x: a thread reads what it writes before it writes it)
+            if (!(o == 0 && x_out == x && i.p == x) && ranges_overlap(i.p, i.bytes, out[o].p, out[o].bytes))
+                return MOE_ERR_INVALID_ARG;
+        for (int q = 0; q < o; q++)
+            if (ranges_overlap(out[q].p, out[q].bytes, out[o].p, out[o].bytes)) return MOE_ERR_INVALID_ARG;
+    }
+    MoeBlockNorm a = {};
+    a.x = x;
+    a.y = y;
+    a.gain_after = gain_after;
+    a.gate = gate;
+    a.row_gate = row_gate;
+    a.gain_before = gain_before;
+    a.x_out = x_out;
+    a.h = h;
+    a.codes = (unsigned*)h_codes;
+    a.scales = h_scales;
+    a.T = T;
+    a.d = d;
+    a.residual_scale = residual_scale;
+    a.eps = eps;
+    a.norm_after = norm_after != 0;
+    a.x_bf16 = x_dtype == MOE_BF16;
+    a.y_bf16 = y_dtype == MOE_BF16;
+    a.h_bf16 = h_dtype == MOE_BF16;
+    return moe_block_norm_launch(a, (hipStream_t)stream);
+}
+
 int moe_weights_free(moe_weights_t* w) { return moe_weights_free_impl(w); }
 
 size_t moe_weights_bytes(const moe_weights_t* w) { return w ? w->bytes : 0; }
@@ -247,9 +441,9 @@ size_t moe_expert_ffn_workspace(int N, int E, int d, int f, moe_dtype_t act_dtyp
     if (N < 0 || N >= MOE_MAX_N || E < 1 || E > MOE_MAX_E || !dims_ok(d) || !dims_ok(f)) return 0;
     if (act_dtype != MOE_F32 && act_dtype != MOE_BF16) return 0;
     size_t need = moe_ffn_f32_workspace(N, E, d, f);
-    const size_t other[4] = {moe_ffn_stream_workspace(N, E, d, f), moe_ffn_grouped_workspace(N, E, d, f),
+    const size_t other[5] = {moe_ffn_stream_workspace(N, E, d, f), moe_ffn_grouped_workspace(N, E, d, f),
                              moe_mx_stream_serves(N, E, d, f) ? moe_mx_stream_workspace(N, E, d, f) : 0,
-                             moe_mx_gemm_workspace(N, E, d, f)};
+                             moe_mx_gemm_workspace(N, E, d, f), moe_i8_ffn_workspace(N, E, d, f)};
     for (size_t o : other)
         if (o > need) need = o;
     return align256(need) + 256;
@@ -297,7 +491,7 @@ int moe_expert_ffn_plan(int N, int E, int d, int f, moe_dtype_t w_dtype, int pat
                         moe_ffn_plan_t* plan) {
     if (!plan || N < 0 || N >= MOE_MAX_N || E < 1 || E > MOE_MAX_E || !dims_ok(d) || !dims_ok(f))
         return MOE_ERR_INVALID_ARG;
-    if (w_dtype != MOE_F32 && w_dtype != MOE_BF16 && w_dtype != MOE_MXFP4) return MOE_ERR_INVALID_ARG;
+    if (w_dtype != MOE_F32 && w_dtype != MOE_BF16 && w_dtype != MOE_MXFP4 && w_dtype != MOE_INT8) return MOE_ERR_INVALID_ARG;
     if (path != MOE_FFN_AUTO && path != MOE_FFN_STREAM && path != MOE_FFN_GROUPED &&
         path != MOE_FFN_MID)
         return MOE_ERR_INVALID_ARG;
@@ -307,6 +501,10 @@ int moe_expert_ffn_plan(int N, int E, int d, int f, moe_dtype_t w_dtype, int pat
         plan->path = path == MOE_FFN_AUTO ? moe_mx_auto_path(N, E, d, f) : path;
         if (plan->path == MOE_FFN_STREAM) return moe_mx_stream_serves(N, E, d, f) ? MOE_OK : MOE_ERR_UNSUPPORTED;
         return plan->path == MOE_FFN_GROUPED ? moe_mx_gemm_plan(N, E, d, f, plan) : MOE_ERR_UNSUPPORTED;
+    }
+    if (w_dtype == MOE_INT8) {
+        plan->path = path == MOE_FFN_AUTO ? moe_i8_auto_path(N, E, d, f) : path;
+        return moe_i8_ffn_plan(N, E, d, f, plan);
     }
     if (w_dtype == MOE_F32) {
         if (path != MOE_FFN_AUTO) return MOE_ERR_UNSUPPORTED;

@@ -1,0 +1,99 @@
+// Matrices and rows in 8-bit integers: symmetric codes in [-127, 127] with one fp32 scale per output
+// channel of a matrix and one per row (token).  Layout of the packed handle, the code of a value,
+// and what the launchers are told.
+//
+// A product of codes is exact in the matrix cores' 32-bit integers (127^2 * 2^17 < 2^31), whatever the
+// order or split of the sum, so results depend on the codes alone; the scales enter once, at the end.
+#pragma once
+
+#include "moe_internal.h"
+
+// The unit of the packed layout is the A operand of one v_mfma_i32_16x16x64_i8: 16 output features by
+// 64 reduction indices, lane l of a wavefront feature l % 16 and the 16 indices 16*(l / 16) .. +15, one
+// 16-byte chunk at byte 16*l (1 KiB, one coalesced load).
+//   w13: [E][f/16][2 (w1,w3)][d/64] fragments, s13: [E][f/16][2][16] fp32
+//   w2 : [E][d/16][f/64]                       s2 : [E][d/16][16]
+#define I8_FRAG_K 64
+#define I8_MAX_K (1 << 17)  // products of a reduction: the sum stays within 32 bits
+
+#ifdef __HIPCC__
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+
+// The scale of a row whose largest magnitude has the bits `top` (as unsigned numbers NaN > inf > finite): top / 127
+// rounded to fp32, NaN where the row holds NaN or an infinity.
+__device__ __forceinline__ float i8_scale(unsigned top) {
+    return top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float(top) / 127.0f;
+}
+
+// v / s to the nearest integer, ties to even, for fp32 v and s.  The quotient by the reciprocal is off by a few parts
+// in 2^24, which is on the wrong side of a border between two codes at times; the remainder v - q*s is exact (v and
+// q*s agree in their leading bits) and says so.  Rows of tiny values are scaled up by 2^64 first (`lift`), where
+// scales would be subnormal.
+struct I8Coder {
+    float s, half, inv, lift;
+    __device__ __forceinline__ explicit I8Coder(float scale) {
+        lift = scale < 0x1p-60f ? 0x1p64f : 1.0f;
+        s = scale * lift;
+        half = 0.5f * s;
+        inv = s > 0.0f ? 1.0f / s : 0.0f;  // (zero and NaN rows: codes 0)
+    }
+    __device__ __forceinline__ int operator()(float v) const {
+        v = inv > 0.0f ? v * lift : 0.0f;
+        float q = rintf(v * inv);
+        const float r = __builtin_fmaf(-q, s, v);
+        const bool odd = ((int)q & 1) != 0;
+        if (r > half || (r == half && odd && half > 0.0f)) q += 1.0f;
+        else if (r < -half || (r == -half && odd && half > 0.0f)) q -= 1.0f;
+        return (int)fminf(fmaxf(q, -127.0f), 127.0f);
+    }
+};
+
+__device__ __forceinline__ unsigned i8_pack4(int a, int b, int c, int d) {
+    return (a & 255) | ((b & 255) << 8) | ((c & 255) << 16) | ((unsigned)d << 24);
+}
+
+// Sum of code products times the row's and the channel's scale.
+__device__ __forceinline__ float i8_value(int sum, float row_scale, float channel_scale) {
+    return (float)sum * row_scale * channel_scale;
+}
+#endif
+
+static inline __host__ __device__ int i8_frags(int K) { return (K + I8_FRAG_K - 1) / I8_FRAG_K; }
+
+// ---- launchers (moe_i8_convert.hip, moe_i8_stream.hip, moe_i8_gemm.hip) --------------------
+int moe_i8_quantize_launch(const void* w, moe_dtype_t w_dtype, int E, int K, int C, int8_t* codes, float* scales,
+                           hipStream_t s);
+int moe_i8_dequantize_launch(const int8_t* codes, const float* scales, int E, int K, int C, void* w, moe_dtype_t w_dtype,
+                             hipStream_t s);
+int moe_i8_rows_launch(const void* x, moe_dtype_t x_dtype, int T, int K, int8_t* codes, float* scales, hipStream_t s);
+int moe_i8_rows_back_launch(const int8_t* codes, const float* scales, int T, int K, void* x, moe_dtype_t x_dtype,
+                            hipStream_t s);
+int moe_i8_pack_impl(const int8_t* const codes[3], const float* const scales[3], int E, int d, int f, moe_weights** out,
+                     hipStream_t s);
+
+// One product: rows x[i], read as x[perm[i] / k] where perm is given, of the experts' segments of `offsets` (null:
+// one matrix for all N rows) with the experts' matrices.
+struct I8Product {
+    const int8_t* x;         // [rows,K]
+    const float* xs;         // [rows]
+    const int32_t* perm;
+    int k;
+    const int32_t* offsets;  // [E+1] or null
+    int E, N, K, C;          // C: output channels of y
+    const int8_t* w;         // packed fragments, or [E][C][K]
+    const float* ws;         // scales in the order of the fragments' features, or [E][C]
+    bool packed;             // w and ws as above
+    bool gated;              // w of pairs (w1, w3): y = silu(x.w1) * (x.w3)
+    void* y;                 // [N,C]
+    bool y_bf16;
+};
+int moe_i8_product_launch(const I8Product& p, hipStream_t s);
+bool moe_i8_product_supported(int N, int E, int K, int C);
+
+// The expert FFN.  `path` as moe_i8_auto_path names it.
+int moe_i8_auto_path(int N, int E, int d, int f);
+size_t moe_i8_ffn_workspace(int N, int E, int d, int f);
+bool moe_i8_ffn_supported(int path, int N, int E, int d, int f);
+int moe_i8_ffn_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan);  // plan->path given
+int moe_i8_ffn_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtype, const float* x_scales, int rows,
+                      const int32_t* perm, int k, const int32_t* offsets, int N, void* ws, float* yg, int path, hipStream_t s);

@@ -1,0 +1,273 @@
+// Conversion of rows and matrices between fp32 / bf16 and 8-bit codes, and the one-time repack of
+// converted expert matrices into the order the kernels stream them.  All of it is bound by memory.
+#include <new>
+
+#include "moe_i8.h"
+
+// ---------------------------------------------------------------------- rows ----
+// A workgroup takes a row: V chunks of four values a thread, kept in registers between the largest
+// magnitude and the codes, so that the row is read once.  Rows longer than 4 * V * blockDim.x are read twice.
+template <bool BF16>
+__device__ __forceinline__ float4 i8_load4(const void* x, size_t chunk) {
+    if (BF16) {
+        const uint2 u = ((const uint2*)x)[chunk];
+        return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
+                           __uint_as_float(u.y & 0xFFFF0000u));
+    }
+    return ((const float4*)x)[chunk];
+}
+__device__ __forceinline__ unsigned i8_top4(float4 v) {
+    const unsigned m = 0x7FFFFFFFu, a = __float_as_uint(v.x) & m, b = __float_as_uint(v.y) & m, c = __float_as_uint(v.z) & m,
+                   d = __float_as_uint(v.w) & m;
+    const unsigned p = a > b ? a : b, q = c > d ? c : d;
+    return p > q ? p : q;
+}
+
+// The largest of the workgroup's `top`, in every thread.
+__device__ __forceinline__ unsigned i8_block_top(unsigned top, unsigned* s_top) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const unsigned o = (unsigned)__shfl_xor((int)top, m, 64);
+        top = top > o ? top : o;
+    }
+    const int waves = blockDim.x >> 6;
+    if (waves == 1) return top;
+    if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
+    __syncthreads();
+    for (int w = 0; w < waves; w++) top = top > s_top[w] ? top : s_top[w];
+    return top;
+}
+
+template <bool BF16, int V>
+__global__ __launch_bounds__(1024) void i8_rows_kernel(const void* __restrict__ x, int T, int K4, unsigned* __restrict__ codes,
+                                                       float* __restrict__ scales) {
+    __shared__ unsigned s_top[16];
+    for (int t = blockIdx.x; t < T; t += gridDim.x) {
+        const size_t base = (size_t)t * K4;
+        float4 v[V];
+        unsigned top = 0u;
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const int c = threadIdx.x + i * blockDim.x;
+            v[i] = c < K4 ? i8_load4<BF16>(x, base + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const unsigned o = i8_top4(v[i]);
+            top = top > o ? top : o;
+        }
+        for (int c = threadIdx.x + V * blockDim.x; c < K4; c += blockDim.x) {
+            const unsigned o = i8_top4(i8_load4<BF16>(x, base + c));
+            top = top > o ? top : o;
+        }
+        top = i8_block_top(top, s_top);
+        const float scale = i8_scale(top);
+        const I8Coder code(scale);
+        if (threadIdx.x == 0) scales[t] = scale;
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const int c = threadIdx.x + i * blockDim.x;
+            if (c < K4) codes[base + c] = i8_pack4(code(v[i].x), code(v[i].y), code(v[i].z), code(v[i].w));
+        }
+        for (int c = threadIdx.x + V * blockDim.x; c < K4; c += blockDim.x) {
+            const float4 u = i8_load4<BF16>(x, base + c);
+            codes[base + c] = i8_pack4(code(u.x), code(u.y), code(u.z), code(u.w));
+        }
+        __syncthreads();
+    }
+}
+
+int moe_i8_rows_launch(const void* x, moe_dtype_t x_dtype, int T, int K, int8_t* codes, float* scales, hipStream_t s) {
+    const int K4 = K / 4;
+    int threads = 64;
+    while (threads < 1024 && threads * 4 < K4) threads *= 2;
+    const dim3 grid((unsigned)(T < (1 << 20) ? T : (1 << 20)));
+    auto* kernel = x_dtype == MOE_BF16 ? i8_rows_kernel<true, 4> : i8_rows_kernel<false, 4>;
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, x, T, K4, (unsigned*)codes, scales);
+    return moe_launch_status();
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void i8_rows_back_kernel(const unsigned* __restrict__ codes, const float* __restrict__ scales,
+                                                           int T, int K4, void* __restrict__ x) {
+    for (int t = blockIdx.y; t < T; t += gridDim.y) {
+        const float s = scales[t];
+        for (int c = blockIdx.x * 256 + threadIdx.x; c < K4; c += gridDim.x * 256) {
+            const size_t at = (size_t)t * K4 + c;
+            const int q = (int)codes[at];
+            const float4 v = make_float4((float)(q << 24 >> 24) * s, (float)(q << 16 >> 24) * s, (float)(q << 8 >> 24) * s,
+                                         (float)(q >> 24) * s);
+            if (BF16) {
+                typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                ((bf16x4*)x)[at] = bf16x4{(__bf16)v.x, (__bf16)v.y, (__bf16)v.z, (__bf16)v.w};
+            } else {
+                ((float4*)x)[at] = v;
+            }
+        }
+    }
+}
+
+int moe_i8_rows_back_launch(const int8_t* codes, const float* scales, int T, int K, void* x, moe_dtype_t x_dtype,
+                            hipStream_t s) {
+    const int K4 = K / 4;
+    const dim3 grid((unsigned)((K4 + 1023) / 1024), (unsigned)(T < 65535 ? T : 65535));
+    auto* kernel = x_dtype == MOE_BF16 ? i8_rows_back_kernel<true> : i8_rows_back_kernel<false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, (const unsigned*)codes, scales, T, K4, x);
+    return moe_launch_status();
+}
+
+// ------------------------------------------------------------------ matrices ----
+// W [K,C] has its channels along the rows and its codes along the reduction, so both directions are
+// transpositions through LDS, 64 channels wide.  To codes: a workgroup takes 64 channels and all of K, once
+// for the largest magnitudes and once for the codes.
+#define I8_CV_C 64
+#define I8_CV_K 256   // reduction indices of an LDS tile
+#define I8_CV_PAD 4   // bytes: a channel's row of the tile starts in another bank than its neighbour's
+
+template <bool BF16>
+__device__ __forceinline__ float i8_load1(const void* w, size_t at) {
+    return BF16 ? moe_bf16_to_f32(((const uint16_t*)w)[at]) : ((const float*)w)[at];
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(1024) void i8_quantize_kernel(const void* __restrict__ w, int K, int C, int ctiles,
+                                                           int8_t* __restrict__ codes, float* __restrict__ scales) {
+    __shared__ unsigned s_top[16][I8_CV_C];
+    __shared__ __align__(16) unsigned char s_q[I8_CV_C][I8_CV_K + I8_CV_PAD];
+    const size_t e = blockIdx.x / ctiles;
+    const int c0 = (int)(blockIdx.x % ctiles) * I8_CV_C;
+    const int cl = threadIdx.x & 63, kg = threadIdx.x >> 6;  // a wave: 64 channels of one index
+    const int c = c0 + cl < C ? c0 + cl : C - 1;
+    const size_t base = e * K * C + c;
+    unsigned top = 0u;
+    for (int k = kg; k < K; k += 16) {
+        const unsigned o = __float_as_uint(i8_load1<BF16>(w, base + (size_t)k * C)) & 0x7FFFFFFFu;
+        top = top > o ? top : o;
+    }
+    s_top[kg][cl] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 16; i++) top = top > s_top[i][cl] ? top : s_top[i][cl];
+    const float scale = i8_scale(top);
+    const I8Coder code(scale);
+    if (kg == 0 && c0 + cl < C) scales[e * C + c] = scale;
+    for (int k0 = 0; k0 < K; k0 += I8_CV_K) {
+        const int kn = K - k0 < I8_CV_K ? K - k0 : I8_CV_K;
+        for (int k = kg * 4; k < kn; k += 64) {
+            int q[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) q[i] = code(i8_load1<BF16>(w, base + (size_t)(k0 + k + i) * C));
+            *(unsigned*)&s_q[cl][k] = i8_pack4(q[0], q[1], q[2], q[3]);
+        }
+        __syncthreads();
+        // sixteen bytes of a channel a thread: K is a multiple of 16
+        const int cc = threadIdx.x >> 4, b = (threadIdx.x & 15) * 16;
+        if (c0 + cc < C && b < kn) {
+            const unsigned* p = (const unsigned*)&s_q[cc][b];
+            *(u32x4_t*)(codes + (e * C + c0 + cc) * K + k0 + b) = u32x4_t{p[0], p[1], p[2], p[3]};
+        }
+        __syncthreads();
+    }
+}
+
+int moe_i8_quantize_launch(const void* w, moe_dtype_t w_dtype, int E, int K, int C, int8_t* codes, float* scales,
+                           hipStream_t s) {
+    const int ctiles = (C + I8_CV_C - 1) / I8_CV_C;
+    auto* kernel = w_dtype == MOE_BF16 ? i8_quantize_kernel<true> : i8_quantize_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(E * ctiles)), dim3(1024), 0, s, w, K, C, ctiles, codes, scales);
+    return moe_launch_status();
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(1024) void i8_dequantize_kernel(const int8_t* __restrict__ codes, const float* __restrict__ scales,
+                                                             int K, int C, int ctiles, void* __restrict__ w) {
+    __shared__ __align__(16) unsigned char s_q[I8_CV_C][I8_CV_K + I8_CV_PAD];
+    const size_t e = blockIdx.x / ctiles;
+    const int c0 = (int)(blockIdx.x % ctiles) * I8_CV_C, k0 = (int)blockIdx.y * I8_CV_K;
+    const int kn = K - k0 < I8_CV_K ? K - k0 : I8_CV_K;
+    const int cc = threadIdx.x >> 4, b = (threadIdx.x & 15) * 16;
+    if (c0 + cc < C && b < kn) {
+        const u32x4_t v = *(const u32x4_t*)(codes + (e * C + c0 + cc) * K + k0 + b);
+        unsigned* p = (unsigned*)&s_q[cc][b];
+#pragma unroll
+        for (int i = 0; i < 4; i++) p[i] = v[i];
+    }
+    __syncthreads();
+    const int cl = threadIdx.x & 63, kg = threadIdx.x >> 6;
+    if (c0 + cl >= C) return;
+    const float s = scales[e * C + c0 + cl];
+    for (int k = kg * 4; k < kn; k += 64) {
+        const int q = *(const int*)&s_q[cl][k];
+        const float v[4] = {(float)(q << 24 >> 24) * s, (float)(q << 16 >> 24) * s, (float)(q << 8 >> 24) * s, (float)(q >> 24) * s};
+        const size_t at = (e * K + k0 + k) * C + c0 + cl;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if (BF16) ((__bf16*)w)[at + (size_t)i * C] = (__bf16)v[i];
+            else ((float*)w)[at + (size_t)i * C] = v[i];
+        }
+    }
+}
+
+int moe_i8_dequantize_launch(const int8_t* codes, const float* scales, int E, int K, int C, void* w, moe_dtype_t w_dtype,
+                             hipStream_t s) {
+    const int ctiles = (C + I8_CV_C - 1) / I8_CV_C;
+    const dim3 grid((unsigned)(E * ctiles), (unsigned)((K + I8_CV_K - 1) / I8_CV_K));
+    auto* kernel = w_dtype == MOE_BF16 ? i8_dequantize_kernel<true> : i8_dequantize_kernel<false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(1024), 0, s, codes, scales, K, C, ctiles, w);
+    return moe_launch_status();
+}
+
+// -------------------------------------------------------------------- handle ----
+// codes [E][C][K] -> fragments [E][C/16][nmat][K/64], this launch fills matrix slot `mat`, and the scales beside
+// them.  One thread writes one 16-byte chunk; the four chunks of 64 bytes of a feature go to lanes 16 apart.
+__global__ __launch_bounds__(256) void i8_pack_kernel(const int8_t* __restrict__ src, const float* __restrict__ scales,
+                                                      u32x4_t* __restrict__ dst, float* __restrict__ dscale, int E, int K, int C,
+                                                      int nmat, int mat) {
+    const size_t KS = (size_t)i8_frags(K), total = (size_t)E * C * KS * 4;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
+        const int j = (int)(i & 3);
+        const size_t ks = (i >> 2) % KS, c = (i >> 2) / KS;  // feature, counted through the experts
+        const u32x4_t v = *(const u32x4_t*)(src + c * K + ks * I8_FRAG_K + 16 * j);
+        dst[(((c / 16) * nmat + mat) * KS + ks) * 64 + 16 * j + (c & 15)] = v;
+        if (ks == 0 && j == 0) dscale[((c / 16) * nmat + mat) * 16 + (c & 15)] = scales[c];
+    }
+}
+
+int moe_i8_pack_impl(const int8_t* const codes[3], const float* const scales[3], int E, int d, int f, moe_weights** out,
+                     hipStream_t s) {
+    moe_weights* W = new (std::nothrow) moe_weights();
+    if (!W) return MOE_ERR_HIP;
+    W->E = E;
+    W->d = d;
+    W->f = f;
+    W->dtype = MOE_INT8;
+    if (hipGetDevice(&W->device) != hipSuccess) {
+        (void)hipGetLastError();
+        delete W;
+        return MOE_ERR_HIP;
+    }
+    const size_t n = (size_t)E * d * f;
+    const size_t bytes[4] = {2 * n, n, (size_t)E * 2 * f * 4, (size_t)E * d * 4};
+    void** dst[4] = {&W->w13, &W->w2, &W->s13, &W->s2};
+    for (int i = 0; i < 4; i++) {
+        if (hipMalloc(dst[i], bytes[i]) != hipSuccess) {
+            (void)hipGetLastError();
+            for (int j = 0; j < i; j++) (void)hipFree(*dst[j]);
+            delete W;
+            return MOE_ERR_HIP;
+        }
+        W->bytes += bytes[i];
+    }
+    for (int m = 0; m < 3; m++) {
+        const bool up = m < 2;
+        hipLaunchKernelGGL(i8_pack_kernel, dim3(4096), dim3(256), 0, s, codes[m], scales[m], (u32x4_t*)(up ? W->w13 : W->w2),
+                           (float*)(up ? W->s13 : W->s2), E, up ? d : f, up ? f : d, up ? 2 : 1, up ? m : 0);
+    }
+    if (moe_launch_status() != MOE_OK) {
+        for (int i = 0; i < 4; i++) (void)hipFree(*dst[i]);
+        delete W;
+        return MOE_ERR_HIP;
+    }
+    *out = W;
+    return MOE_OK;
+}

@@ -1,0 +1,386 @@
+// Products of 8-bit rows with 8-bit matrices on the integer matrix cores: one matrix, or one per expert
+// of a batch whose segments only the device knows.  The expert FFN is two of them: the first one's epilogue
+// applies silu(a)*b, its rows are brought to 8 bits again, and the second one reads them.
+//
+//   * tile: up to 32*RB rows of one expert x 256 channels (fragment rows of w); an expert's blocks of 32 rows
+//     are dealt evenly to its tiles, and the loop exists once per number of blocks.
+//   * both operands travel through a ring of NS stages of LDS, 64 reduction indices each, which the waves fill
+//     with direct-to-LDS loads NS - 1 steps ahead.  Rows (and matrices that are not packed) are read where
+//     they lie: four lanes take 64 bytes of a row, and the four chunks are stored rotated by the row, so that
+//     the matrix instructions' reads, one chunk of sixteen rows, meet no bank twice.
+//   * a step waits for its stage, meets the other waves at a barrier (which also frees the stage of the step
+//     before), requests the stage NS - 1 ahead, and multiplies.
+#include <atomic>
+#include <type_traits>
+
+#include "moe_i8.h"
+#include "moe_frag_pack.h"
+
+struct I8GemmArgs {
+    I8Product p;
+    int NR;   // 16-channel fragment rows of an expert's matrix (w1 and w3 counted both)
+    int KS;   // steps
+    int FT;   // feature tiles
+};
+
+struct I8Tile {
+    int e, row0, rows;  // the tile's rows of the batch
+    int nblk;           // its blocks of 16 * WT rows
+    int ft;
+};
+
+// Tile number blockIdx.x of the launch, order expert, groups of at most 8 row tiles, feature tile, row tile; an XCD
+// takes neighbours of the order, which share operands in its L2.  False past the end.  BR: rows of a block.
+template <int BR, int RBM>
+__device__ __forceinline__ bool i8_find_tile(const I8GemmArgs& a, int lane, I8Tile& ti) {
+    int lo = 0, rows = lane == 0 ? a.p.N : 0;
+    if (a.p.offsets) gg_segment_of_lane(a.p.offsets, a.p.E, a.p.N, lane, lo, rows);
+    const int nb = (rows + BR - 1) / BR, nt = (nb + RBM - 1) / RBM;
+    int it = nt;
+#pragma unroll
+    for (int dlt = 1; dlt < 64; dlt <<= 1) {
+        const int vt = __shfl_up(it, dlt, 64);
+        if (lane >= dlt) it += vt;
+    }
+    const int total = __builtin_amdgcn_readlane(it, 63) * a.FT;
+    const int chunk = (total + 7) / 8, me = blockIdx.x >> 3;
+    const int L = (blockIdx.x & 7) * chunk + me;
+    if (me >= chunk || L >= total) return false;
+    const int base = (it - nt) * a.FT;
+    const unsigned long long m = __ballot(L >= base && L < base + nt * a.FT);
+    const int e = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(m));
+    const int lo_e = __builtin_amdgcn_readlane(lo, e), rows_e = __builtin_amdgcn_readlane(rows, e);
+    const int tiles = __builtin_amdgcn_readlane(nt, e), blocks = __builtin_amdgcn_readlane(nb, e);
+    int r = L - __builtin_amdgcn_readlane(base, e);
+    const int grp = r / (8 * a.FT);
+    r -= grp * 8 * a.FT;
+    const int gw = (tiles - grp * 8) < 8 ? (tiles - grp * 8) : 8;
+    const int rt = grp * 8 + r % gw;
+    ti.ft = r / gw;
+    const int per = blocks / tiles, more = blocks % tiles;
+    const int b0 = rt * per + (rt < more ? rt : more);
+    ti.e = e;
+    ti.nblk = per + (rt < more ? 1 : 0);
+    ti.row0 = lo_e + b0 * BR;
+    ti.rows = rows_e - b0 * BR < ti.nblk * BR ? rows_e - b0 * BR : ti.nblk * BR;
+    return true;
+}
+
+// At most n vector-memory requests and no LDS read in flight, then the other waves.
+#define I8_MEET(n)                                                                 \
+    do {                                                                           \
+        __builtin_amdgcn_s_waitcnt(0x0070 | ((n) & 15) | (((n) >> 4) << 14));      \
+        asm volatile("" ::: "memory");                                             \
+        __builtin_amdgcn_s_barrier();                                              \
+        asm volatile("" ::: "memory");                                             \
+    } while (0)
+
+// WT x WF waves, RB blocks of 16 rows and FB fragment rows of w each.
+template <int WT, int WF, int FB, int NS, int RB, bool PACKED, bool GATED>
+__device__ __forceinline__ void i8_gemm_tile(const I8GemmArgs& a, const I8Tile& ti, int lane, int wave, unsigned char* smem) {
+    constexpr int NW = WT * WF, XF = WT * RB, WFR = WF * FB;
+    constexpr int XL = (XF + NW - 1) / NW, WL = (WFR + NW - 1) / NW;  // requests of a wave and step
+    constexpr int STAGE = (XF + WFR) * 1024, D = NS - 1;
+    static_assert(WFR % NW == 0 && (D - 1) * (XL + WL) < 64, "requests");
+    const I8Product& p = a.p;
+    const int K = p.K;
+    const int wt = wave / WF, wf = wave % WF;
+    const int fr0 = ti.ft * WFR;
+
+    // where this lane's part of a request lies: a row-major fragment is 16 rows of 64 bytes, lane l row l / 4
+    const int chunk = (lane & 3) ^ ((lane >> 4) & 3);
+    const int last = K - 16;  // (the last step of a K that is no multiple of 64 reads nothing behind the row)
+    const int8_t* xp[XL];
+    const int8_t* wp[WL];
+#pragma unroll
+    for (int i = 0; i < XL; i++) {
+        const int f = i * NW + wave < XF ? i * NW + wave : XF - 1;
+        int r = f * 16 + (lane >> 2);
+        r = ti.row0 + (r < ti.rows ? r : ti.rows - 1);
+        const size_t src = p.perm ? p.perm[r] / p.k : r;
+        xp[i] = p.x + src * K;
+    }
+#pragma unroll
+    for (int i = 0; i < WL; i++) {
+        int fr = fr0 + i * NW + wave;
+        if (PACKED) {
+            fr = fr < a.NR ? fr : a.NR - 1;
+            wp[i] = p.w + ((size_t)ti.e * a.NR + fr) * a.KS * 1024 + lane * 16;
+        } else {
+            int c = fr * 16 + (lane >> 2);
+            c = c < p.C ? c : p.C - 1;
+            wp[i] = p.w + ((size_t)ti.e * p.C + c) * K;
+        }
+    }
+    auto request = [&](int ks, int slot) __attribute__((always_inline)) {
+        // (past the end: the last step's operands again, so that every step counts the same requests)
+        const int kc = ks < a.KS ? ks : a.KS - 1;
+        int at = kc * I8_FRAG_K + chunk * 16;
+        at = at < last ? at : last;
+#pragma unroll
+        for (int i = 0; i < WL; i++) {
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void*)(wp[i] + (PACKED ? (size_t)kc * 1024 : (size_t)at)),
+                (__attribute__((address_space(3))) void*)(smem + slot * STAGE + (i * NW + wave) * 1024), 16, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < XL; i++) {
+            const int f = i * NW + wave < XF ? i * NW + wave : XF - 1;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(xp[i] + at),
+                                             (__attribute__((address_space(3))) void*)(smem + slot * STAGE + (WFR + f) * 1024),
+                                             16, 0, 0);
+        }
+    };
+
+    i32x4_t acc[FB][RB];
+#pragma unroll
+    for (int r = 0; r < FB; r++)
+#pragma unroll
+        for (int b = 0; b < RB; b++) acc[r][b] = i32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < D; i++) {
+        request(i, i);
+        asm volatile("" ::: "memory");
+    }
+
+    // the matrix instruction's operand: row l % 16, chunk l / 16
+    const int rl = lane & 15, cq = lane >> 4;
+    const int row_major = (rl * 4 + (cq ^ ((rl >> 2) & 3))) * 16;
+    const int w_at = PACKED ? lane * 16 : row_major;
+    const int tail = K % I8_FRAG_K;  // bytes of the last step, 0: all
+    auto step = [&](int k, auto slot_) __attribute__((always_inline)) {
+        constexpr int u = decltype(slot_)::value;
+        // this step's operands have arrived, and every wave has read the stage that is refilled now
+        I8_MEET((D - 1) * (XL + WL));
+        request(k + D, (u + D) % NS);
+        const unsigned char* st = smem + u * STAGE;
+        i32x4_t w[FB], x[RB];
+#pragma unroll
+        for (int r = 0; r < FB; r++) w[r] = *(const i32x4_t*)(st + (wf * FB + r) * 1024 + w_at);
+#pragma unroll
+        for (int b = 0; b < RB; b++) x[b] = *(const i32x4_t*)(st + (WFR + wt * RB + b) * 1024 + row_major);
+        if (tail && k == a.KS - 1 && cq * 16 >= tail) {
+#pragma unroll
+            for (int b = 0; b < RB; b++) x[b] = i32x4_t{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int b = 0; b < RB; b++)
+#pragma unroll
+            for (int r = 0; r < FB; r++) acc[r][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[r], x[b], acc[r][b], 0, 0, 0);
+    };
+    using std::integral_constant;
+    int k = 0;
+    for (; k + NS <= a.KS; k += NS) {
+        step(k, integral_constant<int, 0>{});
+        step(k + 1, integral_constant<int, 1>{});
+        step(k + 2, integral_constant<int, 2>{});
+        if constexpr (NS > 3) step(k + 3, integral_constant<int, 3>{});
+        static_assert(NS == 3 || NS == 4, "steps of the ring");
+    }
+    if (k < a.KS) step(k, integral_constant<int, 0>{});
+    if (k + 1 < a.KS) step(k + 1, integral_constant<int, 1>{});
+    if constexpr (NS > 3) if (k + 2 < a.KS) step(k + 2, integral_constant<int, 2>{});
+    // no request for LDS outlives the workgroup
+    __builtin_amdgcn_s_waitcnt(0x0070);
+
+    // lane: row l % 16 of a block, four neighbouring channels of a fragment row
+    const int frw = fr0 + wf * FB;
+#pragma unroll
+    for (int b = 0; b < RB; b++) {
+        const int rr = (wt * RB + b) * 16 + rl;
+        if (rr >= ti.rows) continue;
+        const size_t row = ti.row0 + rr;
+        const float sx = p.xs[p.perm ? p.perm[row] / p.k : (int)row];
+        if (GATED) {
+#pragma unroll
+            for (int n = 0; n < FB / 2; n++) {
+                const int fr = frw + 2 * n;  // w1's; w3's follows it
+                if (fr >= a.NR) continue;
+                const float4 s1 = *(const float4*)(p.ws + ((size_t)ti.e * a.NR + fr) * 16 + 4 * cq);
+                const float4 s3 = *(const float4*)(p.ws + ((size_t)ti.e * a.NR + fr + 1) * 16 + 4 * cq);
+                const i32x4_t g = acc[2 * n][b], v = acc[2 * n + 1][b];
+                const float sa[4] = {s1.x, s1.y, s1.z, s1.w}, sb[4] = {s3.x, s3.y, s3.z, s3.w};
+                float h[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const float t = i8_value(g[i], sx, sa[i]);
+                    h[i] = t / (1.0f + __expf(-t)) * i8_value(v[i], sx, sb[i]);
+                }
+                *(float4*)((float*)p.y + row * p.C + fr * 8 + 4 * cq) = make_float4(h[0], h[1], h[2], h[3]);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < FB; r++) {
+                const int c = (frw + r) * 16 + 4 * cq;
+                if (c >= p.C) continue;
+                const float* ws = p.ws + (size_t)ti.e * p.C + c;
+                if (p.C % 4 == 0) {
+                    const float4 sw = *(const float4*)ws;
+                    const float4 v = make_float4(i8_value(acc[r][b][0], sx, sw.x), i8_value(acc[r][b][1], sx, sw.y),
+                                                 i8_value(acc[r][b][2], sx, sw.z), i8_value(acc[r][b][3], sx, sw.w));
+                    if (p.y_bf16) {
+                        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                        *(bf16x4*)((__bf16*)p.y + row * p.C + c) = bf16x4{(__bf16)v.x, (__bf16)v.y, (__bf16)v.z, (__bf16)v.w};
+                    } else {
+                        *(float4*)((float*)p.y + row * p.C + c) = v;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        if (c + i >= p.C) continue;
+                        const float v = i8_value(acc[r][b][i], sx, ws[i]);
+                        if (p.y_bf16) ((__bf16*)p.y)[row * p.C + c + i] = (__bf16)v;
+                        else ((float*)p.y)[row * p.C + c + i] = v;
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <int WT, int WF, int FB, int NS, int RBM, bool PACKED, bool GATED>
+__global__ __launch_bounds__(64 * WT * WF, WT * WF == 8 ? 2 : 2) void i8_gemm_kernel(I8GemmArgs a) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    I8Tile ti;
+    if (!i8_find_tile<16 * WT, RBM>(a, lane, ti)) return;
+#define I8_TILE(n) if (ti.nblk == n) i8_gemm_tile<WT, WF, FB, NS, n, PACKED, GATED>(a, ti, lane, wave, smem)
+    I8_TILE(1);
+    else I8_TILE(2);
+    if constexpr (RBM >= 4) {
+        I8_TILE(3);
+        else I8_TILE(4);
+    }
+    if constexpr (RBM >= 8) {
+        I8_TILE(5);
+        else I8_TILE(6);
+        else I8_TILE(7);
+        else I8_TILE(8);
+    }
+#undef I8_TILE
+}
+
+// ------------------------------------------------------------------ host ----
+static inline size_t i8_align256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+// Tiles of `rows` rows of one expert, at most: min(N, E) experts have rows, and a last tile of at least one.
+static inline size_t i8_tiles(int N, int E, int rows) {
+    const size_t used = N < E ? N : E;
+    return ((size_t)N + (size_t)(rows - 1) * used) / rows;
+}
+
+bool moe_i8_product_supported(int N, int E, int K, int C) {
+    return K <= I8_MAX_K && ((long long)i8_tiles(N, E, 64) + 1) * ((2ll * C + 15) / 16 / 16 + 1) < (1ll << 28);
+}
+
+template <int WT, int WF, int FB, int NS, int RBM, bool PACKED, bool GATED>
+static int i8_gemm_go(I8GemmArgs& a, hipStream_t s) {
+    a.FT = (a.NR + WF * FB - 1) / (WF * FB);
+    const size_t grid = (i8_tiles(a.p.N, a.p.E, 16 * WT * RBM) * a.FT + 7) / 8 * 8;
+    constexpr int lds = NS * (WT * RBM + WF * FB) * 1024;
+    auto* kernel = i8_gemm_kernel<WT, WF, FB, NS, RBM, PACKED, GATED>;
+    if (lds > 65536) {
+        static std::atomic<bool> ready[MOE_MAX_DEVICES];  // one-time permission for more than 64 KiB of LDS
+        const int dev = moe_current_device();
+        if (dev < 0) return MOE_ERR_HIP;
+        if (!ready[dev].load(std::memory_order_acquire)) {
+            MOE_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+            ready[dev].store(true, std::memory_order_release);
+        }
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * WT * WF), lds, s, a);
+    return moe_launch_status();
+}
+
+static bool i8_large(int N, int E) { return N > 64 * (N < E ? N : E); }
+template <bool PACKED, bool GATED>
+static int i8_gemm_pick(I8GemmArgs& a, hipStream_t s) {
+    if (!i8_large(a.p.N, a.p.E)) return i8_gemm_go<1, 4, 4, 3, 4, PACKED, GATED>(a, s);
+    return i8_gemm_go<2, 4, 4, 4, 8, PACKED, GATED>(a, s);
+}
+
+int moe_i8_product_launch(const I8Product& p, hipStream_t s) {
+    I8GemmArgs a = {};
+    a.p = p;
+    a.NR = p.gated ? 2 * (p.C / 16) : (p.C + 15) / 16;
+    a.KS = i8_frags(p.K);
+    if (p.gated) return i8_gemm_pick<true, true>(a, s);
+    return p.packed ? i8_gemm_pick<true, false>(a, s) : i8_gemm_pick<false, false>(a, s);
+}
+
+// ---- the expert FFN: rows to 8 bits, w1 and w3 with silu*mul, h to 8 bits, w2 ----
+// workspace: codes and scales of the rows, h in fp32, its codes and scales
+struct I8FfnSpace {
+    size_t xq, xs, h, hq, hs, bytes;
+};
+static I8FfnSpace i8_ffn_space(int N, int d, int f) {
+    I8FfnSpace w;
+    w.xq = 0;
+    w.xs = i8_align256((size_t)N * d);
+    w.h = w.xs + i8_align256((size_t)N * 4);
+    w.hq = w.h + i8_align256((size_t)N * f * 4);
+    w.hs = w.hq + i8_align256((size_t)N * f);
+    w.bytes = w.hs + i8_align256((size_t)N * 4);
+    return w;
+}
+size_t moe_i8_ffn_workspace(int N, int E, int d, int f) {
+    return d <= I8_MAX_K && f <= I8_MAX_K ? i8_ffn_space(N, d, f).bytes : 0;
+}
+int moe_i8_auto_path(int N, int E, int d, int f) { return MOE_FFN_GROUPED; }
+bool moe_i8_ffn_supported(int path, int N, int E, int d, int f) {
+    return path == MOE_FFN_GROUPED && moe_i8_product_supported(N, E, d, f) && moe_i8_product_supported(N, E, f, d);
+}
+int moe_i8_ffn_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan) {
+    if (!moe_i8_ffn_supported(plan->path, N, E, d, f)) return MOE_ERR_UNSUPPORTED;
+    plan->up_tile_rows = plan->down_tile_rows = i8_large(N, E) ? 256 : 64;
+    plan->up_tile_features = plan->down_tile_features = 256;
+    return MOE_OK;
+}
+
+// x: `rows` rows of act_dtype; MOE_INT8: codes with x_scales.
+int moe_i8_ffn_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtype, const float* x_scales, int rows,
+                      const int32_t* perm, int k, const int32_t* offsets, int N, void* ws, float* yg, int path, hipStream_t s) {
+    const int E = W->E, d = W->d, f = W->f;
+    const I8FfnSpace sp = i8_ffn_space(N, d, f);
+    char* base = (char*)ws;
+    int rc = MOE_OK;
+    I8Product up = {};
+    up.x = (const int8_t*)x;
+    up.xs = x_scales;
+    if (act_dtype != MOE_INT8) {
+        up.x = (const int8_t*)(base + sp.xq);
+        up.xs = (const float*)(base + sp.xs);
+        rc = moe_i8_rows_launch(x, act_dtype, rows, d, (int8_t*)(base + sp.xq), (float*)(base + sp.xs), s);
+        if (rc != MOE_OK) return rc;
+    }
+    up.perm = perm;
+    up.k = k;
+    up.offsets = offsets;
+    up.E = E;
+    up.N = N;
+    up.K = d;
+    up.C = f;
+    up.w = (const int8_t*)W->w13;
+    up.ws = (const float*)W->s13;
+    up.packed = up.gated = true;
+    up.y = base + sp.h;
+    if ((rc = moe_i8_product_launch(up, s)) != MOE_OK) return rc;
+    moe_record_mid_event(s);
+    rc = moe_i8_rows_launch(base + sp.h, MOE_F32, N, f, (int8_t*)(base + sp.hq), (float*)(base + sp.hs), s);
+    if (rc != MOE_OK) return rc;
+    I8Product down = {};
+    down.x = (const int8_t*)(base + sp.hq);
+    down.xs = (const float*)(base + sp.hs);
+    down.k = 1;
+    down.offsets = offsets;
+    down.E = E;
+    down.N = N;
+    down.K = f;
+    down.C = d;
+    down.w = (const int8_t*)W->w2;
+    down.ws = (const float*)W->s2;
+    down.packed = true;
+    down.y = yg;
+    return moe_i8_product_launch(down, s);
+}

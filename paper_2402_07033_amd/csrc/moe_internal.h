@@ -35,7 +35,7 @@ struct moe_weights {
     float* w3f;
     float* w2f;
     size_t bytes;
-    // MXFP4: w13 and w2 hold code fragments, these their scales (moe_mx.h)
+    // MXFP4 and 8 bits: w13 and w2 hold code fragments, these their scales (moe_mx.h, moe_i8.h)
     void* s13;
     void* s2;
 };
@@ -164,3 +164,18 @@ int moe_combine_residual_launch(const float* yg, const int32_t* inv_perm, const 
 int moe_combine_parts_launch(const float* parts, int n_parts, size_t part_stride,
                              const int32_t* inv_perm, const float* weights, int T, int k, int d,
                              float* y, bool residual, float* yg_out, hipStream_t s);
+
+// moe_block_norm's arguments (moe_block_norm.hip); x_out, h and codes or null.
+struct MoeBlockNorm {
+    const void* x;
+    const void* y;
+    const float *gain_after, *gate, *row_gate, *gain_before;
+    void* x_out;
+    void* h;
+    unsigned* codes;
+    float* scales;
+    int T, d;
+    float residual_scale, eps;
+    bool norm_after, x_bf16, y_bf16, h_bf16;
+};
+int moe_block_norm_launch(const MoeBlockNorm& a, hipStream_t s);

@@ -4,6 +4,7 @@
 #include <atomic>
 
 #include "moe_internal.h"
+#include "moe_i8.h"
 #include "moe_mx.h"
 
 // 32 MiB: the decode kernels' scratch (h [N,f] fp32 and the second projection's reduction
@@ -44,12 +45,15 @@ int moe_expert_ffn_noalloc(const moe_weights_t* W, const void* xg, moe_dtype_t a
     if (W->dtype == MOE_F32 && act_dtype != MOE_F32) return MOE_ERR_UNSUPPORTED;
     // scratch of the kernel family that would run (the workspace query of the allocating
     // entry point covers every family at once, which is far more than a decode step needs)
-    const bool mx = W->dtype == MOE_MXFP4;
+    const bool mx = W->dtype == MOE_MXFP4, i8 = W->dtype == MOE_INT8;
     const int path = W->dtype == MOE_F32 ? MOE_FFN_AUTO
-                     : mx ? moe_mx_auto_path(N, W->E, W->d, W->f) : moe_ffn_auto_path(N, W->E, W->d, W->f);
+                     : mx ? moe_mx_auto_path(N, W->E, W->d, W->f)
+                     : i8 ? moe_i8_auto_path(N, W->E, W->d, W->f) : moe_ffn_auto_path(N, W->E, W->d, W->f);
     if (mx && path == MOE_FFN_GROUPED && !moe_mx_gemm_supported(N, W->E, W->d, W->f)) return MOE_ERR_UNSUPPORTED;
+    if (i8 && !moe_i8_ffn_supported(path, N, W->E, W->d, W->f)) return MOE_ERR_UNSUPPORTED;
     size_t need;
-    if (mx) need = path == MOE_FFN_STREAM ? moe_mx_stream_workspace(N, W->E, W->d, W->f)
+    if (i8) need = moe_i8_ffn_workspace(N, W->E, W->d, W->f);
+    else if (mx) need = path == MOE_FFN_STREAM ? moe_mx_stream_workspace(N, W->E, W->d, W->f)
                                           : moe_mx_gemm_workspace(N, W->E, W->d, W->f);
     else if (W->dtype == MOE_F32) need = moe_ffn_f32_workspace(N, W->E, W->d, W->f);
     else if (path == MOE_FFN_STREAM) need = moe_ffn_stream_workspace(N, W->E, W->d, W->f);
@@ -58,6 +62,7 @@ int moe_expert_ffn_noalloc(const moe_weights_t* W, const void* xg, moe_dtype_t a
     void* ptr = noalloc_scratch_ptr();
     if (!ptr) return MOE_ERR_HIP;
     hipStream_t s = (hipStream_t)stream;
+    if (i8) return moe_i8_ffn_launch(W, xg, act_dtype, nullptr, N, nullptr, 1, offsets, N, ptr, yg, path, s);
     if (mx)
         return path == MOE_FFN_STREAM ? moe_mx_stream_launch(W, xg, act_dtype, nullptr, 1, offsets, N, ptr, yg, nullptr, s)
                                       : moe_mx_gemm_launch(W, xg, act_dtype, nullptr, 1, offsets, N, ptr, yg, true, nullptr, nullptr, s);

@@ -87,7 +87,7 @@ static int ffn_args(const moe_weights_t* W, const void* xg, moe_dtype_t act_dtyp
         served = path == MOE_FFN_STREAM ? moe_mx_stream_serves(N, W->E, W->d, W->f)
                                         : path == MOE_FFN_GROUPED && moe_mx_gemm_supported(N, W->E, W->d, W->f);
     } else if (W->dtype == MOE_INT8) {
-        if (path == MOE_FFN_AUTO) path = moe_i8_auto_path(N, W->E, W->d, W->f);
+        if (path == MOE_FFN_AUTO) path = moe_i8_auto_path(N, W->E);
         served = moe_i8_ffn_supported(path, N, W->E, W->d, W->f);
     } else {
         if (path == MOE_FFN_AUTO) path = moe_ffn_auto_path(N, W->E, W->d, W->f);
@@ -133,7 +133,7 @@ static int ffn_launch(const moe_weights_t* W, const void* xg, moe_dtype_t act_dt
         return path == MOE_FFN_STREAM ? moe_mx_stream_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, nullptr, s)
                                       : moe_mx_gemm_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, true, nullptr, nullptr, s);
     if (W->dtype == MOE_INT8)
-        return moe_i8_ffn_launch(W, xg, act_dtype, nullptr, perm ? N / k : N, perm, k, offsets, N, workspace, yg, path, s);
+        return moe_i8_ffn_launch(W, xg, act_dtype, perm ? N / k : N, perm, k, offsets, N, workspace, yg, path, s);
     if (path == MOE_FFN_STREAM)
         return moe_ffn_stream_launch(W, xg, act_dtype, perm, k, offsets, N, workspace, yg, nullptr, s);
     return moe_ffn_grouped_launch(path == MOE_FFN_MID, W, xg, act_dtype, perm, k, offsets, N, workspace, yg, s);
@@ -321,7 +321,7 @@ int moe_int8_matmul(const int8_t* x_codes, const float* x_scales, int M, const i
     p.ws = w_scales;
     p.y = y;
     p.y_bf16 = y_dtype == MOE_BF16;
-    return moe_i8_product_launch(p, (hipStream_t)stream);
+    return moe_i8_product_launch(p, moe_i8_auto_path(M, E), (hipStream_t)stream);
 }
 
 int moe_weights_pack_int8(const int8_t* w1_codes, const float* w1_scales, const int8_t* w3_codes, const float* w3_scales,
@@ -361,7 +361,7 @@ int moe_layer_int8(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, c
     if (!moe_aligned16(x) || !moe_aligned16(y) || !moe_aligned16(logits) || !moe_aligned16(idx) || !moe_aligned16(weights) ||
         !moe_aligned16(perm) || !moe_aligned16(inv_perm) || (x_scales && !moe_aligned16(x_scales)))
         return MOE_ERR_INVALID_ARG;
-    const int path = moe_i8_auto_path(N, E, d, f);
+    const int path = moe_i8_auto_path(N, E);
     if (!moe_i8_ffn_supported(path, N, E, d, f)) return MOE_ERR_UNSUPPORTED;
     if (!workspace || (((uintptr_t)workspace) & 255u)) return MOE_ERR_WORKSPACE;
     if (workspace_bytes < moe_layer_int8_workspace(T, E, k, d, f)) return MOE_ERR_WORKSPACE;
@@ -375,14 +375,23 @@ int moe_layer_int8(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, c
             ranges_overlap(x_scales, (size_t)T * 4, o.p, o.bytes))
             return MOE_ERR_INVALID_ARG;
 
-    int rc = moe_route_launch(logits, T, E, k, idx, weights, s);
-    if (rc == MOE_OK)
-        rc = moe_permute_launch(idx, T, E, k, nullptr, 0, MOE_F32, counts, offsets, perm, inv_perm, nullptr, s);
-    if (rc != MOE_OK) return rc;
-    float* yg = (float*)workspace;
-    rc = moe_i8_ffn_launch(W, x, x_dtype, x_scales, T, perm, k, offsets, N, (char*)workspace + i8_layer_rows(N, d), yg, path, s);
-    if (rc != MOE_OK) return rc;
-    return moe_mx_combine_launch(yg, 1, 0, inv_perm, weights, T, k, d, y, y_dtype, s);
+    I8Front fr = {};
+    fr.logits = logits;
+    fr.T = T;
+    fr.k = k;
+    fr.idx = idx;
+    fr.counts = counts;
+    fr.offsets = offsets;
+    fr.perm = perm;
+    fr.inv_perm = inv_perm;
+    fr.weights = weights;
+    if (x_dtype == MOE_INT8) {
+        fr.codes = (unsigned*)x;
+        fr.scales = (float*)x_scales;
+    } else {
+        fr.x = x;
+    }
+    return moe_i8_layer_launch(W, fr, x_dtype, workspace, y, y_dtype, path, s);
 }
 
 int moe_block_norm(const void* x, moe_dtype_t x_dtype, const void* y, moe_dtype_t y_dtype, int T, int d, int norm_after,
@@ -503,7 +512,7 @@ int moe_expert_ffn_plan(int N, int E, int d, int f, moe_dtype_t w_dtype, int pat
         return plan->path == MOE_FFN_GROUPED ? moe_mx_gemm_plan(N, E, d, f, plan) : MOE_ERR_UNSUPPORTED;
     }
     if (w_dtype == MOE_INT8) {
-        plan->path = path == MOE_FFN_AUTO ? moe_i8_auto_path(N, E, d, f) : path;
+        plan->path = path == MOE_FFN_AUTO ? moe_i8_auto_path(N, E) : path;
         return moe_i8_ffn_plan(N, E, d, f, plan);
     }
     if (w_dtype == MOE_F32) {

@@ -139,3 +139,86 @@ __device__ __forceinline__ int permute_indices_wave(const int* __restrict__ s_id
     }
     return my_off;
 }
+
+// Per-expert batching of N <= 64 slots by one wave, E <= 64: lane p owns slot p and finds the slots
+// of its expert with one ballot per bit of the expert's number.  Lane e < E gets its expert's rows
+// [lo, lo + cnt); s_pos[p]: the slot's position; s_cnt [64]: scratch.
+template <class Step>
+__device__ __forceinline__ void gate_batch_any(const int* s_idx, int N, int E, int lane, bool write, const Step& st,
+                                               int* s_pos, int* s_cnt, int& lo, int& cnt) {
+    const bool live = lane < N;
+    const int e = live ? s_idx[lane] : 0;
+    unsigned long long same = __ballot(live);
+#pragma unroll
+    for (int b = 0; b < 6; b++) {
+        const unsigned long long m = __ballot((e >> b) & 1);
+        same &= ((e >> b) & 1) ? m : ~m;
+    }
+    const int rank = __popcll(same & ((lane == 0) ? 0ull : (~0ull >> (64 - lane))));
+    s_cnt[lane] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (live && rank == 0) s_cnt[e] = __popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    cnt = s_cnt[lane];
+    int inc = cnt;
+#pragma unroll
+    for (int dlt = 1; dlt < 64; dlt <<= 1) {
+        const int v = __shfl_up(inc, dlt, 64);
+        if (lane >= dlt) inc += v;
+    }
+    lo = inc - cnt;
+    const int pos = __shfl(lo, e, 64) + rank;
+    if (live) {
+        s_pos[lane] = pos;
+        if (write) {
+            st.perm[pos] = lane;
+            st.inv_perm[lane] = pos;
+        }
+    }
+    if (write) {
+        if (lane < E) {
+            st.counts[lane] = cnt;
+            st.offsets[lane] = lo;
+        }
+        if (lane == E - 1) st.offsets[E] = inc;
+    }
+}
+
+// The workgroup's waves route the tokens, one at a time each, lane e holding expert e's logit: k
+// rounds of the wave's maximum and, of the lanes that have it, the lowest.  The weights, which only
+// the writing workgroup needs, are moe_route's to the bit.
+template <class Step>
+__device__ __forceinline__ void gate_route_any(const float* logits, const Step& st, int E, int wave, int W, int lane,
+                                               int* s_idx, bool write) {
+    for (int t = wave; t < st.T; t += W) {
+        float v = lane < E ? logits[(size_t)t * E + lane] : -INFINITY;
+        float my_v = 0.f, top = 0.f;
+        int my_e = 0;
+        unsigned long long open = E < 64 ? (1ull << E) - 1 : ~0ull;  // experts not taken yet
+        for (int j = 0; j < st.k; j++) {
+            const float m = wave_max(v);
+            unsigned long long have = __ballot(v == m) & open;
+            if (have == 0ull) have = open;  // (logits that are NaN, or all that is left is -infinity's end)
+            const int e = (int)__builtin_ctzll(have);
+            open &= ~(1ull << e);
+            if (j == 0) top = m;
+            if (lane == j) {
+                my_v = m;
+                my_e = e;
+            }
+            if (lane == e) v = -INFINITY;
+        }
+        if (lane < st.k) s_idx[t * st.k + lane] = my_e;
+        if (!write) continue;
+        const float u = lane < st.k ? expf(my_v - top) : 0.f;
+        float sum = u;
+#pragma unroll
+        for (int m = 1; m < MOE_MAX_K; m <<= 1) sum += __shfl_xor(sum, m, 64);
+        if (lane < st.k) {
+            st.idx[(size_t)t * st.k + lane] = my_e;
+            st.weights[(size_t)t * st.k + lane] = u / sum;
+        }
+    }
+}

@@ -2,6 +2,7 @@
 // converted expert matrices into the order the kernels stream them.  All of it is bound by memory.
 #include <new>
 
+#include "moe_gate_wave.h"
 #include "moe_i8.h"
 
 // ---------------------------------------------------------------------- rows ----
@@ -38,52 +39,84 @@ __device__ __forceinline__ unsigned i8_block_top(unsigned top, unsigned* s_top) 
     return top;
 }
 
+// Row t of K4 chunks to codes, by the whole workgroup.
+template <bool BF16, int V>
+__device__ __forceinline__ void i8_row(const void* x, int t, int K4, unsigned* codes, float* scales, unsigned* s_top) {
+    const size_t base = (size_t)t * K4;
+    float4 v[V];
+    unsigned top = 0u;
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        const int c = threadIdx.x + i * blockDim.x;
+        v[i] = c < K4 ? i8_load4<BF16>(x, base + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        const unsigned o = i8_top4(v[i]);
+        top = top > o ? top : o;
+    }
+    for (int c = threadIdx.x + V * blockDim.x; c < K4; c += blockDim.x) {
+        const unsigned o = i8_top4(i8_load4<BF16>(x, base + c));
+        top = top > o ? top : o;
+    }
+    const float scale = i8_scale(i8_block_top(top, s_top));
+    const I8Coder code(scale);
+    if (threadIdx.x == 0) scales[t] = scale;
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        const int c = threadIdx.x + i * blockDim.x;
+        if (c < K4) codes[base + c] = code(v[i]);
+    }
+    for (int c = threadIdx.x + V * blockDim.x; c < K4; c += blockDim.x) {
+        const float4 u = i8_load4<BF16>(x, base + c);
+        codes[base + c] = code(u);
+    }
+}
+
 template <bool BF16, int V>
 __global__ __launch_bounds__(1024) void i8_rows_kernel(const void* __restrict__ x, int T, int K4, unsigned* __restrict__ codes,
                                                        float* __restrict__ scales) {
     __shared__ unsigned s_top[16];
     for (int t = blockIdx.x; t < T; t += gridDim.x) {
-        const size_t base = (size_t)t * K4;
-        float4 v[V];
-        unsigned top = 0u;
-#pragma unroll
-        for (int i = 0; i < V; i++) {
-            const int c = threadIdx.x + i * blockDim.x;
-            v[i] = c < K4 ? i8_load4<BF16>(x, base + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-#pragma unroll
-        for (int i = 0; i < V; i++) {
-            const unsigned o = i8_top4(v[i]);
-            top = top > o ? top : o;
-        }
-        for (int c = threadIdx.x + V * blockDim.x; c < K4; c += blockDim.x) {
-            const unsigned o = i8_top4(i8_load4<BF16>(x, base + c));
-            top = top > o ? top : o;
-        }
-        top = i8_block_top(top, s_top);
-        const float scale = i8_scale(top);
-        const I8Coder code(scale);
-        if (threadIdx.x == 0) scales[t] = scale;
-#pragma unroll
-        for (int i = 0; i < V; i++) {
-            const int c = threadIdx.x + i * blockDim.x;
-            if (c < K4) codes[base + c] = i8_pack4(code(v[i].x), code(v[i].y), code(v[i].z), code(v[i].w));
-        }
-        for (int c = threadIdx.x + V * blockDim.x; c < K4; c += blockDim.x) {
-            const float4 u = i8_load4<BF16>(x, base + c);
-            codes[base + c] = i8_pack4(code(u.x), code(u.y), code(u.z), code(u.w));
-        }
+        i8_row<BF16, V>(x, t, K4, codes, scales, s_top);
         __syncthreads();
     }
 }
 
-int moe_i8_rows_launch(const void* x, moe_dtype_t x_dtype, int T, int K, int8_t* codes, float* scales, hipStream_t s) {
-    const int K4 = K / 4;
+static int i8_row_threads(int K4) {
     int threads = 64;
     while (threads < 1024 && threads * 4 < K4) threads *= 2;
+    return threads;
+}
+
+int moe_i8_rows_launch(const void* x, moe_dtype_t x_dtype, int T, int K, int8_t* codes, float* scales, hipStream_t s) {
     const dim3 grid((unsigned)(T < (1 << 20) ? T : (1 << 20)));
     auto* kernel = x_dtype == MOE_BF16 ? i8_rows_kernel<true, 4> : i8_rows_kernel<false, 4>;
-    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, x, T, K4, (unsigned*)codes, scales);
+    hipLaunchKernelGGL(kernel, grid, dim3(i8_row_threads(K / 4)), 0, s, x, T, K / 4, (unsigned*)codes, scales);
+    return moe_launch_status();
+}
+
+// Workgroup 0 routes and batches, the others take a row each.
+template <bool BF16>
+__global__ __launch_bounds__(1024) void i8_front_kernel(I8Front f) {
+    __shared__ unsigned s_top[16];
+    __shared__ int s_idx[I8_FRONT_SLOTS], s_pos[I8_FRONT_SLOTS], s_cnt[64];
+    if (blockIdx.x > 0) {
+        i8_row<BF16, 4>(f.x, blockIdx.x - 1, f.d / 4, f.codes, f.scales, s_top);
+        return;
+    }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), N = f.T * f.k;
+    gate_route_any(f.logits, f, f.E, wave, blockDim.x >> 6, lane, s_idx, true);
+    __syncthreads();
+    if (wave > 0) return;
+    int lo, cnt;
+    gate_batch_any(s_idx, N, f.E, lane, true, f, s_pos, s_cnt, lo, cnt);
+}
+
+int moe_i8_front_launch(const I8Front& f, moe_dtype_t x_dtype, hipStream_t s) {
+    auto* kernel = x_dtype == MOE_BF16 ? i8_front_kernel<true> : i8_front_kernel<false>;
+    const int threads = f.x ? i8_row_threads(f.d / 4) : 256;
+    hipLaunchKernelGGL(kernel, dim3(f.x ? f.T + 1 : 1), dim3(threads < 256 ? 256 : threads), 0, s, f);
     return moe_launch_status();
 }
 
@@ -154,10 +187,10 @@ __global__ __launch_bounds__(1024) void i8_quantize_kernel(const void* __restric
     for (int k0 = 0; k0 < K; k0 += I8_CV_K) {
         const int kn = K - k0 < I8_CV_K ? K - k0 : I8_CV_K;
         for (int k = kg * 4; k < kn; k += 64) {
-            int q[4];
+            float v[4];
 #pragma unroll
-            for (int i = 0; i < 4; i++) q[i] = code(i8_load1<BF16>(w, base + (size_t)(k0 + k + i) * C));
-            *(unsigned*)&s_q[cl][k] = i8_pack4(q[0], q[1], q[2], q[3]);
+            for (int i = 0; i < 4; i++) v[i] = i8_load1<BF16>(w, base + (size_t)(k0 + k + i) * C);
+            *(unsigned*)&s_q[cl][k] = code(make_float4(v[0], v[1], v[2], v[3]));
         }
         __syncthreads();
         // sixteen bytes of a channel a thread: K is a multiple of 16

@@ -15,6 +15,8 @@
 
 #include "moe_i8.h"
 #include "moe_frag_pack.h"
+#include "moe_i8_value.h"
+#include "moe_mx.h"
 
 struct I8GemmArgs {
     I8Product p;
@@ -193,47 +195,12 @@ __device__ __forceinline__ void i8_gemm_tile(const I8GemmArgs& a, const I8Tile& 
         const float sx = p.xs[p.perm ? p.perm[row] / p.k : (int)row];
         if (GATED) {
 #pragma unroll
-            for (int n = 0; n < FB / 2; n++) {
-                const int fr = frw + 2 * n;  // w1's; w3's follows it
-                if (fr >= a.NR) continue;
-                const float4 s1 = *(const float4*)(p.ws + ((size_t)ti.e * a.NR + fr) * 16 + 4 * cq);
-                const float4 s3 = *(const float4*)(p.ws + ((size_t)ti.e * a.NR + fr + 1) * 16 + 4 * cq);
-                const i32x4_t g = acc[2 * n][b], v = acc[2 * n + 1][b];
-                const float sa[4] = {s1.x, s1.y, s1.z, s1.w}, sb[4] = {s3.x, s3.y, s3.z, s3.w};
-                float h[4];
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const float t = i8_value(g[i], sx, sa[i]);
-                    h[i] = t / (1.0f + __expf(-t)) * i8_value(v[i], sx, sb[i]);
-                }
-                *(float4*)((float*)p.y + row * p.C + fr * 8 + 4 * cq) = make_float4(h[0], h[1], h[2], h[3]);
-            }
+            for (int n = 0; n < FB / 2; n++)
+                if (frw + 2 * n < a.NR)
+                    i8_put_gated(p, ti.e, a.NR, frw + 2 * n, cq, row, sx, acc[GATED ? 2 * n : 0][b], acc[GATED ? 2 * n + 1 : 0][b]);
         } else {
 #pragma unroll
-            for (int r = 0; r < FB; r++) {
-                const int c = (frw + r) * 16 + 4 * cq;
-                if (c >= p.C) continue;
-                const float* ws = p.ws + (size_t)ti.e * p.C + c;
-                if (p.C % 4 == 0) {
-                    const float4 sw = *(const float4*)ws;
-                    const float4 v = make_float4(i8_value(acc[r][b][0], sx, sw.x), i8_value(acc[r][b][1], sx, sw.y),
-                                                 i8_value(acc[r][b][2], sx, sw.z), i8_value(acc[r][b][3], sx, sw.w));
-                    if (p.y_bf16) {
-                        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-                        *(bf16x4*)((__bf16*)p.y + row * p.C + c) = bf16x4{(__bf16)v.x, (__bf16)v.y, (__bf16)v.z, (__bf16)v.w};
-                    } else {
-                        *(float4*)((float*)p.y + row * p.C + c) = v;
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        if (c + i >= p.C) continue;
-                        const float v = i8_value(acc[r][b][i], sx, ws[i]);
-                        if (p.y_bf16) ((__bf16*)p.y)[row * p.C + c + i] = (__bf16)v;
-                        else ((float*)p.y)[row * p.C + c + i] = v;
-                    }
-                }
-            }
+            for (int r = 0; r < FB; r++) i8_put(p, ti.e, (frw + r) * 16 + 4 * cq, row, sx, acc[r][b]);
         }
     }
 }
@@ -300,7 +267,8 @@ static int i8_gemm_pick(I8GemmArgs& a, hipStream_t s) {
     return i8_gemm_go<2, 4, 4, 4, 8, PACKED, GATED>(a, s);
 }
 
-int moe_i8_product_launch(const I8Product& p, hipStream_t s) {
+int moe_i8_product_launch(const I8Product& p, int path, hipStream_t s) {
+    if (path == MOE_FFN_STREAM) return moe_i8_stream_launch(p, s);
     I8GemmArgs a = {};
     a.p = p;
     a.NR = p.gated ? 2 * (p.C / 16) : (p.C + 15) / 16;
@@ -310,9 +278,9 @@ int moe_i8_product_launch(const I8Product& p, hipStream_t s) {
 }
 
 // ---- the expert FFN: rows to 8 bits, w1 and w3 with silu*mul, h to 8 bits, w2 ----
-// workspace: codes and scales of the rows, h in fp32, its codes and scales
+// workspace: codes and scales of the rows, h in fp32, its codes and scales, or the bits of its largest magnitudes (a few rows)
 struct I8FfnSpace {
-    size_t xq, xs, h, hq, hs, bytes;
+    size_t xq, xs, h, hq, hs, top, bytes;
 };
 static I8FfnSpace i8_ffn_space(int N, int d, int f) {
     I8FfnSpace w;
@@ -321,39 +289,34 @@ static I8FfnSpace i8_ffn_space(int N, int d, int f) {
     w.h = w.xs + i8_align256((size_t)N * 4);
     w.hq = w.h + i8_align256((size_t)N * f * 4);
     w.hs = w.hq + i8_align256((size_t)N * f);
+    w.top = w.hq;
     w.bytes = w.hs + i8_align256((size_t)N * 4);
     return w;
 }
 size_t moe_i8_ffn_workspace(int N, int E, int d, int f) {
     return d <= I8_MAX_K && f <= I8_MAX_K ? i8_ffn_space(N, d, f).bytes : 0;
 }
-int moe_i8_auto_path(int N, int E, int d, int f) { return MOE_FFN_GROUPED; }
+int moe_i8_auto_path(int N, int E) { return N <= 16 * (N < E ? N : E) ? MOE_FFN_STREAM : MOE_FFN_GROUPED; }
 bool moe_i8_ffn_supported(int path, int N, int E, int d, int f) {
-    return path == MOE_FFN_GROUPED && moe_i8_product_supported(N, E, d, f) && moe_i8_product_supported(N, E, f, d);
+    return (path == MOE_FFN_GROUPED || path == MOE_FFN_STREAM) && moe_i8_product_supported(N, E, d, f) && moe_i8_product_supported(N, E, f, d);
 }
 int moe_i8_ffn_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan) {
     if (!moe_i8_ffn_supported(plan->path, N, E, d, f)) return MOE_ERR_UNSUPPORTED;
+    if (plan->path == MOE_FFN_STREAM) return MOE_OK;
     plan->up_tile_rows = plan->down_tile_rows = i8_large(N, E) ? 256 : 64;
     plan->up_tile_features = plan->down_tile_features = 256;
     return MOE_OK;
 }
 
-// x: `rows` rows of act_dtype; MOE_INT8: codes with x_scales.
-int moe_i8_ffn_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtype, const float* x_scales, int rows,
-                      const int32_t* perm, int k, const int32_t* offsets, int N, void* ws, float* yg, int path, hipStream_t s) {
+// yg, or the layer's y where `c` is given: then yg is scratch.
+static int i8_experts(const moe_weights* W, const int8_t* codes, const float* scales, const int32_t* perm, int k,
+                      const int32_t* offsets, int N, char* base, const I8FfnSpace& sp, float* yg, const I8Combine* c, int path,
+                      hipStream_t s) {
     const int E = W->E, d = W->d, f = W->f;
-    const I8FfnSpace sp = i8_ffn_space(N, d, f);
-    char* base = (char*)ws;
-    int rc = MOE_OK;
+    const bool small = path == MOE_FFN_STREAM && moe_i8_down_small_serves(N, f);
     I8Product up = {};
-    up.x = (const int8_t*)x;
-    up.xs = x_scales;
-    if (act_dtype != MOE_INT8) {
-        up.x = (const int8_t*)(base + sp.xq);
-        up.xs = (const float*)(base + sp.xs);
-        rc = moe_i8_rows_launch(x, act_dtype, rows, d, (int8_t*)(base + sp.xq), (float*)(base + sp.xs), s);
-        if (rc != MOE_OK) return rc;
-    }
+    up.x = codes;
+    up.xs = scales;
     up.perm = perm;
     up.k = k;
     up.offsets = offsets;
@@ -365,8 +328,11 @@ int moe_i8_ffn_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtype
     up.ws = (const float*)W->s13;
     up.packed = up.gated = true;
     up.y = base + sp.h;
-    if ((rc = moe_i8_product_launch(up, s)) != MOE_OK) return rc;
+    up.ytop = small ? (unsigned*)(base + sp.top) : nullptr;
+    int rc = moe_i8_product_launch(up, path, s);
+    if (rc != MOE_OK) return rc;
     moe_record_mid_event(s);
+    if (small) return moe_i8_down_small_launch(W, (const float*)(base + sp.h), up.ytop, offsets, N, c ? nullptr : yg, c, s);
     rc = moe_i8_rows_launch(base + sp.h, MOE_F32, N, f, (int8_t*)(base + sp.hq), (float*)(base + sp.hs), s);
     if (rc != MOE_OK) return rc;
     I8Product down = {};
@@ -382,5 +348,42 @@ int moe_i8_ffn_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtype
     down.ws = (const float*)W->s2;
     down.packed = true;
     down.y = yg;
-    return moe_i8_product_launch(down, s);
+    rc = moe_i8_product_launch(down, path, s);
+    if (rc != MOE_OK || !c) return rc;
+    return moe_mx_combine_launch(yg, 1, 0, c->inv_perm, c->weights, c->T, c->k, d, c->y, c->y_bf16 ? MOE_BF16 : MOE_F32, s);
+}
+
+int moe_i8_ffn_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtype, int rows, const int32_t* perm, int k,
+                      const int32_t* offsets, int N, void* ws, float* yg, int path, hipStream_t s) {
+    const I8FfnSpace sp = i8_ffn_space(N, W->d, W->f);
+    char* base = (char*)ws;
+    int8_t* codes = (int8_t*)(base + sp.xq);
+    float* scales = (float*)(base + sp.xs);
+    const int rc = moe_i8_rows_launch(x, act_dtype, rows, W->d, codes, scales, s);
+    return rc != MOE_OK ? rc : i8_experts(W, codes, scales, perm, k, offsets, N, base, sp, yg, nullptr, path, s);
+}
+
+int moe_i8_layer_launch(const moe_weights* W, I8Front f, moe_dtype_t x_dtype, void* ws, void* y, moe_dtype_t y_dtype, int path,
+                        hipStream_t s) {
+    const int N = f.T * f.k;
+    const I8FfnSpace sp = i8_ffn_space(N, W->d, W->f);
+    char* base = (char*)ws;
+    f.E = W->E;
+    f.d = W->d;
+    if (f.x) {
+        f.codes = (unsigned*)(base + sp.xq);
+        f.scales = (float*)(base + sp.xs);
+    }
+    int rc;
+    if (N <= I8_FRONT_SLOTS) {
+        rc = moe_i8_front_launch(f, x_dtype, s);
+    } else {
+        rc = moe_route_launch(f.logits, f.T, f.E, f.k, f.idx, f.weights, s);
+        if (rc == MOE_OK)
+            rc = moe_permute_launch(f.idx, f.T, f.E, f.k, nullptr, 0, MOE_F32, f.counts, f.offsets, f.perm, f.inv_perm, nullptr, s);
+        if (rc == MOE_OK && f.x) rc = moe_i8_rows_launch(f.x, x_dtype, f.T, f.d, (int8_t*)f.codes, f.scales, s);
+    }
+    if (rc != MOE_OK) return rc;
+    const I8Combine c = {f.inv_perm, f.weights, f.T, f.k, y, y_dtype == MOE_BF16};
+    return i8_experts(W, (const int8_t*)f.codes, f.scales, f.perm, f.k, f.offsets, N, base, sp, (float*)(base + sp.bytes), &c, path, s);
 }

@@ -48,7 +48,7 @@ int moe_expert_ffn_noalloc(const moe_weights_t* W, const void* xg, moe_dtype_t a
     const bool mx = W->dtype == MOE_MXFP4, i8 = W->dtype == MOE_INT8;
     const int path = W->dtype == MOE_F32 ? MOE_FFN_AUTO
                      : mx ? moe_mx_auto_path(N, W->E, W->d, W->f)
-                     : i8 ? moe_i8_auto_path(N, W->E, W->d, W->f) : moe_ffn_auto_path(N, W->E, W->d, W->f);
+                     : i8 ? moe_i8_auto_path(N, W->E) : moe_ffn_auto_path(N, W->E, W->d, W->f);
     if (mx && path == MOE_FFN_GROUPED && !moe_mx_gemm_supported(N, W->E, W->d, W->f)) return MOE_ERR_UNSUPPORTED;
     if (i8 && !moe_i8_ffn_supported(path, N, W->E, W->d, W->f)) return MOE_ERR_UNSUPPORTED;
     size_t need;
@@ -62,7 +62,7 @@ int moe_expert_ffn_noalloc(const moe_weights_t* W, const void* xg, moe_dtype_t a
     void* ptr = noalloc_scratch_ptr();
     if (!ptr) return MOE_ERR_HIP;
     hipStream_t s = (hipStream_t)stream;
-    if (i8) return moe_i8_ffn_launch(W, xg, act_dtype, nullptr, N, nullptr, 1, offsets, N, ptr, yg, path, s);
+    if (i8) return moe_i8_ffn_launch(W, xg, act_dtype, N, nullptr, 1, offsets, N, ptr, yg, path, s);
     if (mx)
         return path == MOE_FFN_STREAM ? moe_mx_stream_launch(W, xg, act_dtype, nullptr, 1, offsets, N, ptr, yg, nullptr, s)
                                       : moe_mx_gemm_launch(W, xg, act_dtype, nullptr, 1, offsets, N, ptr, yg, true, nullptr, nullptr, s);

@@ -325,7 +325,7 @@ def _here(*tensors):
     """The calls run on the current device's stream: its tensors, or none."""
     dev = _getDevice() if _getDevice is not None else torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device.index != dev:
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
 
 
@@ -385,75 +385,93 @@ def _float_type(dtype) -> int:
     raise TypeError(f"unsupported dtype {dtype}")
 
 
-def _out(t, shape, dtype, device, what: str):
-    """The caller's output tensor, checked, or a new one."""
+def _arg(t: torch.Tensor, dtype, dev: int, what: str) -> int:
+    """The address of a contiguous tensor of `dtype` on device number `dev`, the current one."""
+    if t.dtype is not dtype or not t.is_contiguous() or t.get_device() != dev:
+        _dev(t, dtype, what)
+        _here(t)
+    return t.data_ptr()
+
+
+def _opt(t: Optional[torch.Tensor], dtype, dev: int, n: int, what: str):
+    """_arg of an optional vector of n elements."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return None
+    if t.numel() != n:
+        raise ValueError(f"{what}: expected [{n}]")
+    return _arg(t, dtype, dev, what)
+
+
+def _out(t, shape, dtype, like: torch.Tensor, what: str):
+    """The caller's output tensor, or a new one where `like` is."""
+    if t is None:
+        return like.new_empty(shape, dtype=dtype)
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{what}: expected {list(shape)}")
-    return _dev(t, dtype, what)
+    return t
 
 
-def _int8_pair(pair, dims: int, what: str):
-    """(codes int8 [..., K], scales fp32 [...]) of a stack of matrices (dims 3) or of rows (dims 2)."""
+def _current() -> int:
+    return _getDevice() if _getDevice is not None else torch.cuda.current_device()
+
+
+def _int8_pair(pair, dims: int, dev: int, what: str):
+    """(codes int8 [..., K], scales fp32 [...]) of a stack of matrices (dims 3) or of rows (dims 2) -> their
+    addresses and the codes' shape."""
     codes, scales = pair
-    _dev(codes, torch.int8, what + " codes")
-    _dev(scales, torch.float32, what + " scales")
-    if codes.dim() != dims or tuple(scales.shape) != tuple(codes.shape[:-1]):
+    shape = codes.shape
+    if len(shape) != dims or scales.shape != shape[:-1]:
         raise ValueError(f"{what}: expected codes [{'E,C' if dims == 3 else 'T'},K] and scales without the K")
-    _here(codes, scales)
-    return codes, scales
+    return _arg(codes, torch.int8, dev, what + " codes"), _arg(scales, torch.float32, dev, what + " scales"), shape
 
 
 def moe_int8_quantize(w: torch.Tensor, codes=None, scales=None, stream=None):
     """w [E,K,C] (fp32 or bf16, K a multiple of 16 along the reduction) -> 8-bit (codes int8 [E,C,K],
     scales fp32 [E,C], one per output channel)."""
-    dt = _act_dtype(w)
-    _dev(w, w.dtype, "w")
+    dt, dev = _act_dtype(w), _current()
+    wp = _arg(w, w.dtype, dev, "w")
     if w.dim() != 3:
         raise ValueError("w: expected [E,K,C]")
     E, K, c = w.shape
-    codes = _out(codes, (E, c, K), torch.int8, w.device, "codes")
-    scales = _out(scales, (E, c), torch.float32, w.device, "scales")
-    _here(w, codes, scales)
-    _check(lib().moe_int8_quantize(_ptr(w), dt, E, K, c, _ptr(codes), _ptr(scales), _stream(stream)),
-           "moe_int8_quantize")
+    codes = _out(codes, (E, c, K), torch.int8, w, "codes")
+    scales = _out(scales, (E, c), torch.float32, w, "scales")
+    _check(lib().moe_int8_quantize(wp, dt, E, K, c, _arg(codes, torch.int8, dev, "codes"),
+                                   _arg(scales, torch.float32, dev, "scales"), _stream(stream)), "moe_int8_quantize")
     return codes, scales
 
 
 def moe_int8_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.bfloat16, w=None, stream=None):
     """codes [E,C,K], scales [E,C] -> code * scale, [E,K,C] of `dtype` (fp32 or bf16)."""
-    _int8_pair((codes, scales), 3, "matrix")
-    E, c, K = codes.shape
-    w = _out(w, (E, K, c), dtype if w is None else w.dtype, codes.device, "w")
-    _here(w)
-    _check(lib().moe_int8_dequantize(_ptr(codes), _ptr(scales), E, K, c, _ptr(w), _float_type(w.dtype), _stream(stream)),
+    dev = _current()
+    cp, sp, (E, c, K) = _int8_pair((codes, scales), 3, dev, "matrix")
+    w = _out(w, (E, K, c), dtype, codes, "w")
+    _check(lib().moe_int8_dequantize(cp, sp, E, K, c, _arg(w, w.dtype, dev, "w"), _float_type(w.dtype), _stream(stream)),
            "moe_int8_dequantize")
     return w
 
 
 def moe_int8_quantize_rows(x: torch.Tensor, codes=None, scales=None, stream=None):
     """x [T,K] (fp32 or bf16, K a multiple of 16) -> 8-bit rows (codes int8 [T,K], scales fp32 [T], one per row)."""
-    dt = _act_dtype(x)
-    _dev(x, x.dtype, "x")
+    dt, dev = _act_dtype(x), _current()
+    xp = _arg(x, x.dtype, dev, "x")
     if x.dim() != 2:
         raise ValueError("x: expected [T,K]")
     T, K = x.shape
-    codes = _out(codes, (T, K), torch.int8, x.device, "codes")
-    scales = _out(scales, (T,), torch.float32, x.device, "scales")
-    _here(x, codes, scales)
-    _check(lib().moe_int8_quantize_rows(_ptr(x), dt, T, K, _ptr(codes), _ptr(scales), _stream(stream)),
+    codes = _out(codes, (T, K), torch.int8, x, "codes")
+    scales = _out(scales, (T,), torch.float32, x, "scales")
+    _check(lib().moe_int8_quantize_rows(xp, dt, T, K, _arg(codes, torch.int8, dev, "codes"),
+                                        _arg(scales, torch.float32, dev, "scales"), _stream(stream)),
            "moe_int8_quantize_rows")
     return codes, scales
 
 
 def moe_int8_dequantize_rows(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.bfloat16, x=None, stream=None):
     """codes [T,K], scales [T] -> code * scale, [T,K] of `dtype` (fp32 or bf16)."""
-    _int8_pair((codes, scales), 2, "rows")
-    x = _out(x, tuple(codes.shape), dtype if x is None else x.dtype, codes.device, "x")
-    _here(x)
-    _check(lib().moe_int8_dequantize_rows(_ptr(codes), _ptr(scales), codes.shape[0], codes.shape[1], _ptr(x),
-                                          _float_type(x.dtype), _stream(stream)), "moe_int8_dequantize_rows")
+    dev = _current()
+    cp, sp, (T, K) = _int8_pair((codes, scales), 2, dev, "rows")
+    x = _out(x, (T, K), dtype, codes, "x")
+    _check(lib().moe_int8_dequantize_rows(cp, sp, T, K, _arg(x, x.dtype, dev, "x"), _float_type(x.dtype), _stream(stream)),
+           "moe_int8_dequantize_rows")
     return x
 
 
@@ -461,33 +479,27 @@ def moe_int8_matmul(x, w, offsets=None, dtype=torch.bfloat16, y=None, stream=Non
     """8-bit rows x = (codes [M,K], scales [M]) times 8-bit matrices w = (codes [E,C,K], scales [E,C]) -> y [M,C]
     of `dtype` (fp32 or bf16).  offsets int32 [E+1] on the device: expert e's rows are [offsets[e], offsets[e+1]);
     without them E = 1."""
-    xq, xs = _int8_pair(x, 2, "x")
-    wq, ws = _int8_pair(w, 3, "w")
-    M, K = xq.shape
-    E, c = wq.shape[:2]
-    if wq.shape[2] != K:
+    dev = _current()
+    xq, xs, (M, K) = _int8_pair(x, 2, dev, "x")
+    wq, ws, (E, c, wk) = _int8_pair(w, 3, dev, "w")
+    if wk != K:
         raise ValueError("x and w have different reductions")
-    if offsets is not None:
-        _dev(offsets, torch.int32, "offsets")
-        if offsets.numel() != E + 1:
-            raise ValueError("offsets: expected [E+1]")
-    y = _out(y, (M, c), dtype if y is None else y.dtype, xq.device, "y")
-    _here(y, offsets)
-    _check(lib().moe_int8_matmul(_ptr(xq), _ptr(xs), M, _ptr(wq), _ptr(ws), E, K, c, _ptr(offsets), _ptr(y),
-                                 _float_type(y.dtype), _stream(stream)), "moe_int8_matmul")
+    off = _opt(offsets, torch.int32, dev, E + 1, "offsets")
+    y = _out(y, (M, c), dtype, x[0], "y")
+    _check(lib().moe_int8_matmul(xq, xs, M, wq, ws, E, K, c, off, _arg(y, y.dtype, dev, "y"), _float_type(y.dtype),
+                                 _stream(stream)), "moe_int8_matmul")
     return y
 
 
 def moe_weights_pack_int8(w1, w3, w2, stream=None) -> PackedWeights:
     """A handle over 8-bit expert matrices: w1, w3 and w2 are pairs (codes, scales) as moe_int8_quantize
     leaves them for w1, w3 [E,d,f] and w2 [E,f,d]."""
-    (c1, s1), (c3, s3), (c2, s2) = (_int8_pair(w, 3, n) for w, n in ((w1, "w1"), (w3, "w3"), (w2, "w2")))
-    E, f, d = c1.shape
-    if tuple(c3.shape) != (E, f, d) or tuple(c2.shape) != (E, d, f):
+    dev = _current()
+    (c1, s1, (E, f, d)), (c3, s3, k3), (c2, s2, k2) = (_int8_pair(w, 3, dev, n) for w, n in ((w1, "w1"), (w3, "w3"), (w2, "w2")))
+    if tuple(k3) != (E, f, d) or tuple(k2) != (E, d, f):
         raise ValueError("the matrices must be w1,w3 [E,d,f] and w2 [E,f,d]")
     h = C.c_void_p()
-    _check(lib().moe_weights_pack_int8(_ptr(c1), _ptr(s1), _ptr(c3), _ptr(s3), _ptr(c2), _ptr(s2), E, d, f, C.byref(h),
-                                       _stream(stream)), "moe_weights_pack_int8")
+    _check(lib().moe_weights_pack_int8(c1, s1, c3, s3, c2, s2, E, d, f, C.byref(h), _stream(stream)), "moe_weights_pack_int8")
     return PackedWeights(h.value, E, d, f, MOE_INT8)
 
 
@@ -898,43 +910,42 @@ def moe_layer_int8(W: PackedWeights, x, logits: torch.Tensor, k: int, idx=None, 
     """The whole layer over 8-bit experts: x [T,d] (fp32 or bf16, or a pair (codes, scales) of 8-bit rows), logits
     fp32 [T,E] -> y [T,d] of `dtype` (x's type if it is none; bf16 for 8-bit rows).  `out` = (counts, offsets, perm,
     inv_perm)."""
-    _dev(logits, torch.float32, "logits")
-    scales = None
+    dev, scales, sp = _current(), None, None
+    lp = _arg(logits, torch.float32, dev, "logits")
     if isinstance(x, (tuple, list)):
-        x, scales = _int8_pair(x, 2, "x")
+        xp, sp, _ = _int8_pair(x, 2, dev, "x")
+        x, scales = x
         xdt = MOE_INT8
     else:
         xdt = _act_dtype(x)
-        _dev(x, x.dtype, "x")
+        xp = _arg(x, x.dtype, dev, "x")
     T, E = logits.shape
-    d, N, dev = W.d, T * k, x.device
+    d, N = W.d, T * k
     if E != W.E or tuple(x.shape) != (T, d):
         raise ValueError(f"expected x [T,{d}] and logits [T,{W.E}]")
     if not 1 <= k <= min(E, _MAX_K) or N >= _MAX_N:
         raise MoeError(_INVALID_ARG, "moe_layer_int8")  # before N rows are allocated
     i32 = torch.int32
-    idx = torch.empty((T, k), dtype=i32, device=dev) if idx is None else idx
-    weights = torch.empty((T, k), dtype=torch.float32, device=dev) if weights is None else weights
+    if idx is None:
+        idx = logits.new_empty((T, k), dtype=i32)
+    if weights is None:
+        weights = logits.new_empty((T, k))
     if out is None:
-        out = tuple(torch.empty(n, dtype=i32, device=dev) for n in (E, E + 1, N, N))
+        out = tuple(logits.new_empty(n, dtype=i32) for n in (E, E + 1, N, N))
     counts, offsets, perm, inv_perm = out[:4]
     if workspace is None:
-        workspace = _scratch(moe_layer_int8_workspace(T, E, k, d, W.f), dev, stream)
+        workspace = _scratch(moe_layer_int8_workspace(T, E, k, d, W.f), x.device, stream)
     if y is None:
-        if dtype is None:
-            dtype = torch.bfloat16 if scales is not None else x.dtype
-        y = torch.empty((T, d), dtype=dtype, device=dev)
+        y = x.new_empty((T, d), dtype=dtype if dtype is not None else torch.bfloat16 if scales is not None else x.dtype)
+    p = []
     for t, n, dt, what in ((idx, N, i32, "idx"), (weights, N, torch.float32, "weights"), (counts, E, i32, "counts"),
                            (offsets, E + 1, i32, "offsets"), (perm, N, i32, "perm"), (inv_perm, N, i32, "inv_perm"),
-                           (y, T * d, y.dtype, "y"), (workspace, 0, workspace.dtype, "workspace")):
-        _dev(t, dt, what)
+                           (workspace, 0, workspace.dtype, "workspace"), (y, T * d, y.dtype, "y")):
         if t.numel() < n:
             raise ValueError(f"{what}: {t.numel()} elements, {n} are written")
-    _here(x, logits, idx, weights, counts, offsets, perm, inv_perm, workspace, y)
-    _check(lib().moe_layer_int8(W.handle, x.data_ptr(), xdt, _ptr(scales), logits.data_ptr(), T, k, idx.data_ptr(),
-                                weights.data_ptr(), counts.data_ptr(), offsets.data_ptr(), perm.data_ptr(),
-                                inv_perm.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                y.data_ptr(), _float_type(y.dtype), _stream(stream)), "moe_layer_int8")
+        p.append(_arg(t, dt, dev, what))
+    _check(lib().moe_layer_int8(W.handle, xp, xdt, sp, lp, T, k, *p[:7], workspace.numel() * workspace.element_size(), p[7],
+                                _float_type(y.dtype), _stream(stream)), "moe_layer_int8")
     return dict(idx=idx, w=weights, counts=counts, offsets=offsets, perm=perm, inv_perm=inv_perm, y=y)
 
 
@@ -945,34 +956,32 @@ def moe_block_norm(x: torch.Tensor, y=None, norm_after: bool = False, gain_after
     row_gate * u (gate [d], row_gate [T]); h = rmsnorm(x') * gain_before.  x, y [T,d] fp32 or bf16, gains and gates
     fp32.  Returns x (x', of x's type; x_out may be x itself; x itself where there is no y), h of `h_dtype` (None: no
     h) and with int8=True codes [T,d] and scales [T], h in 8 bits."""
-    xdt = _act_dtype(x)
-    _dev(x, x.dtype, "x")
+    xdt, dev, f32 = _act_dtype(x), _current(), torch.float32
+    xp = _arg(x, x.dtype, dev, "x")
     if x.dim() != 2:
         raise ValueError("x: expected [T,d]")
-    T, d = x.shape
+    T, d = shape = x.shape
+    ydt, yp, xop, hp, hdt, cp, sp = MOE_F32, None, None, None, MOE_F32, None, None
     if y is not None:
-        _dev(y, y.dtype, "y")
-        if tuple(y.shape) != (T, d):
+        if y.shape != shape:
             raise ValueError("y: expected x's shape")
-        x_out = _out(x_out, (T, d), x.dtype, x.device, "x_out")
-    elif x_out is not None:
-        x_out = _out(x_out, (T, d), x.dtype, x.device, "x_out")
-    for t, n, what in ((gain_after, d, "gain_after"), (gate, d, "gate"), (row_gate, T, "row_gate"),
-                       (gain_before, d, "gain_before")):
-        if t is not None and _dev(t, torch.float32, what).numel() != n:
-            raise ValueError(f"{what}: expected [{n}]")
+        ydt, yp = _act_dtype(y), _arg(y, y.dtype, dev, "y")
+    if y is not None or x_out is not None:
+        x_out = _out(x_out, shape, x.dtype, x, "x_out")
+        xop = _arg(x_out, x.dtype, dev, "x_out")
     if h is not None or h_dtype is not None:
-        h = _out(h, (T, d), h_dtype if h is None else h.dtype, x.device, "h")
+        h = _out(h, shape, h_dtype, x, "h")
+        hdt, hp = _float_type(h.dtype), _arg(h, h.dtype, dev, "h")
     if int8:
-        codes = _out(codes, (T, d), torch.int8, x.device, "codes")
-        scales = _out(scales, (T,), torch.float32, x.device, "scales")
+        codes = _out(codes, shape, torch.int8, x, "codes")
+        scales = _out(scales, (T,), f32, x, "scales")
+        cp, sp = _arg(codes, torch.int8, dev, "codes"), _arg(scales, f32, dev, "scales")
     elif codes is not None or scales is not None:
         raise ValueError("codes and scales are outputs of int8=True")
-    _here(x, y, gain_after, gate, row_gate, gain_before, x_out, h, codes, scales)
-    _check(lib().moe_block_norm(_ptr(x), xdt, _ptr(y), MOE_F32 if y is None else _act_dtype(y), T, d, int(norm_after),
-                                _ptr(gain_after), _ptr(gate), _ptr(row_gate), residual_scale, _ptr(gain_before), eps,
-                                _ptr(x_out), _ptr(h), MOE_F32 if h is None else _float_type(h.dtype), _ptr(codes),
-                                _ptr(scales), _stream(stream)), "moe_block_norm")
+    _check(lib().moe_block_norm(xp, xdt, yp, ydt, T, d, norm_after, _opt(gain_after, f32, dev, d, "gain_after"),
+                                _opt(gate, f32, dev, d, "gate"), _opt(row_gate, f32, dev, T, "row_gate"), residual_scale,
+                                _opt(gain_before, f32, dev, d, "gain_before"), eps, xop, hp, hdt, cp, sp, _stream(stream)),
+           "moe_block_norm")
     return dict(x=x if x_out is None else x_out, h=h, codes=codes, scales=scales)
 
 

@@ -8,6 +8,8 @@
 // The arithmetic is in 64 bits: a code of the 8-bit rows lies next to a border between two codes for one value in
 // some ten thousand, and sums of 32 bits would put them on either side.  The vector units do this in a third
 // of the time that the bytes take.
+#include <type_traits>
+
 #include "moe_i8.h"
 
 __device__ __forceinline__ float4 bn_load4(const void* p, bool bf16, size_t chunk) {
@@ -27,17 +29,35 @@ __device__ __forceinline__ void bn_store4(void* p, bool bf16, size_t chunk, cons
     }
 }
 
-// Sum (or maximum) over the workgroup, in every thread, in a fixed order; s: one double per wave.
+// Sum (or maximum) over a wave, in every lane: inside a row of 16 lanes by DPP, across rows by the two lane swaps.
+template <bool MAX>
+__device__ __forceinline__ double bn_wave(double v) {
+    auto join = [](double a, double b) { return MAX ? fmax(a, b) : a + b; };
+    auto dpp = [](double a, auto ctrl) {
+        const int lo = __double2loint(a), hi = __double2hiint(a);
+        return __hiloint2double(__builtin_amdgcn_update_dpp(hi, hi, decltype(ctrl)::value, 0xF, 0xF, false),
+                                __builtin_amdgcn_update_dpp(lo, lo, decltype(ctrl)::value, 0xF, 0xF, false));
+    };
+    v = join(v, dpp(v, std::integral_constant<int, 0xB1>{}));   // quad_perm 1,0,3,2
+    v = join(v, dpp(v, std::integral_constant<int, 0x4E>{}));   // quad_perm 2,3,0,1
+    v = join(v, dpp(v, std::integral_constant<int, 0x141>{}));  // row_half_mirror
+    v = join(v, dpp(v, std::integral_constant<int, 0x140>{}));  // row_mirror
+    unsigned lo = (unsigned)__double2loint(v), hi = (unsigned)__double2hiint(v);
+    auto a = __builtin_amdgcn_permlane16_swap(lo, lo, false, false), b = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+    v = join(__hiloint2double((int)b[0], (int)a[0]), __hiloint2double((int)b[1], (int)a[1]));
+    lo = (unsigned)__double2loint(v);
+    hi = (unsigned)__double2hiint(v);
+    a = __builtin_amdgcn_permlane32_swap(lo, lo, false, false);
+    b = __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+    return join(__hiloint2double((int)b[0], (int)a[0]), __hiloint2double((int)b[1], (int)a[1]));
+}
+
+// The same over the workgroup, in a fixed order; s: a double per wave, not in use by another such call.
 template <bool MAX>
 __device__ __forceinline__ double bn_block(double v, double* s) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const double o = __shfl_xor(v, m, 64);
-        v = MAX ? fmax(v, o) : v + o;
-    }
+    v = bn_wave<MAX>(v);
     const int waves = blockDim.x >> 6;
     if (waves == 1) return v;
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
     __syncthreads();
     v = s[0];
@@ -45,160 +65,139 @@ __device__ __forceinline__ double bn_block(double v, double* s) {
     return v;
 }
 
-// x' of one chunk.
-__device__ __forceinline__ void bn_stream4(const MoeBlockNorm& a, size_t row, int c, double r_after, double row_scale,
-                                           const float4& x, const float4& y, double (&v)[4]) {
-    const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-    float4 g = make_float4(1.f, 1.f, 1.f, 1.f), t = g;
-    if (a.gain_after) g = ((const float4*)a.gain_after)[c];
-    if (a.gate) t = ((const float4*)a.gate)[c];
-    const float gs[4] = {g.x, g.y, g.z, g.w}, ts[4] = {t.x, t.y, t.z, t.w};
+// Chunk c of an optional vector of d floats, ones where it is null: a descriptor of no bytes answers with zeros.
+struct BnGain {
+    __amdgpu_buffer_rsrc_t r;
+    float add;
+    __device__ __forceinline__ BnGain(const float* p, int d)
+        : r(__builtin_amdgcn_make_buffer_rsrc((void*)p, 0, p ? d * 4 : 0, 0x00027000)), add(p ? 0.f : 1.f) {}
+    __device__ __forceinline__ void get(int c, double (&g)[4]) const {
+        const u32x4_t u = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, c * 16, 0, 0));
 #pragma unroll
-    for (int i = 0; i < 4; i++)
-        v[i] = a.y ? (double)xs[i] + row_scale * ((double)ys[i] * r_after * (double)gs[i] * (double)ts[i]) : (double)xs[i];
-}
+        for (int j = 0; j < 4; j++) g[j] = (double)(__uint_as_float(u[j]) + add);
+    }
+};
 
-// V chunks of four values a thread in registers; longer rows are read again for every pass.
-template <int V>
+// A workgroup takes a row, V chunks of four values a thread: in registers (HELD), or read again for every pass.
+template <int V, bool HELD>
 __global__ __launch_bounds__(1024) void block_norm_kernel(MoeBlockNorm a) {
-    __shared__ double s[16];
-    const int d4 = a.d / 4, n = blockDim.x;
+    __shared__ double s[3][16];
+    const int d4 = a.d / 4, n = blockDim.x, t = blockIdx.x;
+    const size_t base = (size_t)t * d4;
     const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
-        const size_t base = (size_t)t * d4;
-        const bool held = d4 <= V * n;
-        float4 x[V], y[V];
-        double v[V][4];
-        if (held) {
+    const BnGain gain_after(a.gain_after, a.d), gate(a.gate, a.d), gain_before(a.gain_before, a.d);
+    float4 hx[HELD ? V : 1], hy[HELD ? V : 1];
+    double held[HELD ? V : 1][4];  // x', then h
+    // f(i, c) for this thread's chunks
+    auto each = [&](auto f) __attribute__((always_inline)) {
+        if constexpr (HELD) {
 #pragma unroll
             for (int i = 0; i < V; i++) {
                 const int c = threadIdx.x + i * n;
-                x[i] = c < d4 ? bn_load4(a.x, a.x_bf16, base + c) : zero;
-                y[i] = c < d4 && a.y ? bn_load4(a.y, a.y_bf16, base + c) : zero;
-            }
-        }
-        double r_after = 1.0;
-        if (a.norm_after) {
-            double sum = 0.0;
-            auto add = [&](const float4& u) __attribute__((always_inline)) {
-                sum += (double)u.x * u.x + (double)u.y * u.y + (double)u.z * u.z + (double)u.w * u.w;
-            };
-            if (held) {
-#pragma unroll
-                for (int i = 0; i < V; i++) add(y[i]);
-            } else {
-                for (int c = threadIdx.x; c < d4; c += n) add(bn_load4(a.y, a.y_bf16, base + c));
-            }
-            r_after = 1.0 / sqrt(bn_block<false>(sum, s) / a.d + (double)a.eps);
-        }
-        const double row_scale = (double)a.residual_scale * (a.row_gate ? (double)a.row_gate[t] : 1.0);
-        double sum = 0.0;
-        if (held) {
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                const int c = threadIdx.x + i * n;
-                if (c < d4) {
-                    bn_stream4(a, base, c, r_after, row_scale, x[i], y[i], v[i]);
-                    if (a.x_out) bn_store4(a.x_out, a.x_bf16, base + c, v[i]);
-                } else {
-                    v[i][0] = v[i][1] = v[i][2] = v[i][3] = 0.0;
-                }
-#pragma unroll
-                for (int j = 0; j < 4; j++) sum += v[i][j] * v[i][j];
+                if (c < d4) f(i, c);
             }
         } else {
-            for (int c = threadIdx.x; c < d4; c += n) {
-                double u[4];
-                bn_stream4(a, base, c, r_after, row_scale, bn_load4(a.x, a.x_bf16, base + c),
-                           a.y ? bn_load4(a.y, a.y_bf16, base + c) : zero, u);
-#pragma unroll
-                for (int j = 0; j < 4; j++) sum += u[j] * u[j];
-            }
+            for (int c = threadIdx.x; c < d4; c += n) f(0, c);
         }
-        if (a.h || a.codes) {
-            const double r = 1.0 / sqrt(bn_block<false>(sum, s) / a.d + (double)a.eps);
-            auto before = [&](int c, double (&u)[4]) __attribute__((always_inline)) {
-                float4 g = make_float4(1.f, 1.f, 1.f, 1.f);
-                if (a.gain_before) g = ((const float4*)a.gain_before)[c];
-                u[0] *= r * (double)g.x;
-                u[1] *= r * (double)g.y;
-                u[2] *= r * (double)g.z;
-                u[3] *= r * (double)g.w;
-            };
-            double top = 0.0;
-            auto largest = [&](const double (&u)[4]) __attribute__((always_inline)) {
+    };
+    auto load_y = [&](int c) __attribute__((always_inline)) { return a.y ? bn_load4(a.y, a.y_bf16, base + c) : zero; };
+    if (HELD) {
+        each([&](int i, int c) __attribute__((always_inline)) { hx[i] = bn_load4(a.x, a.x_bf16, base + c); });
+        each([&](int i, int c) __attribute__((always_inline)) { hy[i] = load_y(c); });
+    }
+    double r_after = 1.0;
+    if (a.norm_after) {
+        double sum = 0.0;
+        each([&](int i, int c) __attribute__((always_inline)) {
+            const float4 u = HELD ? hy[i] : load_y(c);
+            sum += ((double)u.x * u.x + (double)u.y * u.y) + ((double)u.z * u.z + (double)u.w * u.w);
+        });
+        r_after = 1.0 / sqrt(bn_block<false>(sum, s[0]) / a.d + (double)a.eps);
+    }
+    const double scale_y = a.y ? (double)a.residual_scale * (a.row_gate ? (double)a.row_gate[t] : 1.0) * r_after : 0.0;
+    auto stream = [&](int i, int c, double (&v)[4]) __attribute__((always_inline)) {
+        const float4 x = HELD ? hx[i] : bn_load4(a.x, a.x_bf16, base + c), y = HELD ? hy[i] : load_y(c);
+        const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+        double g[4], q[4];
+        gain_after.get(c, g);
+        gate.get(c, q);
+#pragma unroll
+        for (int j = 0; j < 4; j++) v[j] = __builtin_fma((double)ys[j] * g[j] * q[j], scale_y, (double)xs[j]);
+    };
+    double sum = 0.0;
+    each([&](int i, int c) __attribute__((always_inline)) {
+        double u[4];
+        double(&v)[4] = HELD ? held[i] : u;
+        stream(i, c, v);
+        if (HELD && a.x_out) bn_store4(a.x_out, a.x_bf16, base + c, v);
+        sum += (v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3]);
+    });
+    if (a.h || a.codes) {
+        const double r = 1.0 / sqrt(bn_block<false>(sum, s[1]) / a.d + (double)a.eps);
+        // h of a chunk: left in `held` by the first pass that asks
+        auto next = [&](int i, int c, double (&v)[4]) __attribute__((always_inline)) {
+            if (!HELD) stream(i, c, v);
+            double g[4];
+            gain_before.get(c, g);
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[j] *= r * g[j];
+        };
+        double top = 0.0;
+        unsigned odd = 0u;  // the largest high word: an infinity's or a NaN's is seen in it
+        each([&](int i, int c) __attribute__((always_inline)) {
+            double u[4];
+            double(&v)[4] = HELD ? held[i] : u;
+            next(i, c, v);
+            if (a.h) bn_store4(a.h, a.h_bf16, base + c, v);
+            if (a.codes) {
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
-                    const double m = fabs(u[j]);
-                    top = m <= top ? top : m == m ? m : INFINITY;  // (NaN counts as infinite)
-                }
-            };
-            auto again = [&](int c, double (&u)[4]) __attribute__((always_inline)) {
-                bn_stream4(a, base, c, r_after, row_scale, bn_load4(a.x, a.x_bf16, base + c),
-                           a.y ? bn_load4(a.y, a.y_bf16, base + c) : zero, u);
-                before(c, u);
-            };
-            if (held) {
-#pragma unroll
-                for (int i = 0; i < V; i++) {
-                    const int c = threadIdx.x + i * n;
-                    if (c >= d4) continue;
-                    before(c, v[i]);
-                    if (a.h) bn_store4(a.h, a.h_bf16, base + c, v[i]);
-                    largest(v[i]);
-                }
-            } else if (a.codes) {
-                for (int c = threadIdx.x; c < d4; c += n) {
-                    double u[4];
-                    again(c, u);
-                    largest(u);
+                    top = fmax(top, fabs(v[j]));
+                    const unsigned w = (unsigned)__double2hiint(v[j]) & 0x7FFFFFFFu;
+                    odd = odd > w ? odd : w;
                 }
             }
-            double inv = 0.0;
-            if (a.codes) {
-                top = bn_block<true>(top, s);
-                const float scale = top < INFINITY ? (float)(top / 127.0) : __uint_as_float(0x7FC00000u);
-                if (threadIdx.x == 0) a.scales[t] = scale;
-                inv = scale > 0.f ? 1.0 / (double)scale : 0.0;
-            }
-            auto code = [&](double u) __attribute__((always_inline)) {
-                return inv > 0.0 ? (int)fmin(fmax(rint(u * inv), -127.0), 127.0) : 0;
-            };
-            if (held) {
-                if (a.codes) {
-#pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        const int c = threadIdx.x + i * n;
-                        if (c < d4) a.codes[base + c] = i8_pack4(code(v[i][0]), code(v[i][1]), code(v[i][2]), code(v[i][3]));
-                    }
-                }
-            } else {
-                for (int c = threadIdx.x; c < d4; c += n) {
-                    double u[4];
-                    again(c, u);
-                    if (a.h) bn_store4(a.h, a.h_bf16, base + c, u);
-                    if (a.codes) a.codes[base + c] = i8_pack4(code(u[0]), code(u[1]), code(u[2]), code(u[3]));
-                }
-            }
-        }
-        // rows that are not held: last, when nothing reads x and y any more (x_out may be either)
-        if (!held && a.x_out) {
-            for (int c = threadIdx.x; c < d4; c += n) {
+        });
+        if (a.codes) {
+            if (__ballot(odd >= 0x7FF00000u) != 0ull) top = INFINITY;
+            top = bn_block<true>(top, s[2]);
+            const float scale = top < INFINITY ? (float)(top / 127.0) : __uint_as_float(0x7FC00000u);
+            if (threadIdx.x == 0) a.scales[t] = scale;
+            const double inv = scale > 0.f ? 1.0 / (double)scale : 0.0;
+            const bool plain = scale >= 0x1p-126f;  // (a subnormal scale may be too small for the largest values)
+            const double magic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low word is the rounded quotient
+            each([&](int i, int c) __attribute__((always_inline)) {
                 double u[4];
-                bn_stream4(a, base, c, r_after, row_scale, bn_load4(a.x, a.x_bf16, base + c),
-                           a.y ? bn_load4(a.y, a.y_bf16, base + c) : zero, u);
-                bn_store4(a.x_out, a.x_bf16, base + c, u);
-            }
+                double(&v)[4] = HELD ? held[i] : u;
+                if (!HELD) next(i, c, v);
+                int q[4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    if (plain) q[j] = __double2loint(__builtin_fma(v[j], inv, magic));
+                    else q[j] = inv > 0.0 ? (int)fmin(fmax(rint(v[j] * inv), -127.0), 127.0) : 0;
+                }
+                a.codes[base + c] = i8_pack4(q[0], q[1], q[2], q[3]);
+            });
         }
-        __syncthreads();
+    }
+    // rows that are not held: last, when nothing reads x any more (x_out may be x)
+    if (!HELD && a.x_out) {
+        each([&](int i, int c) __attribute__((always_inline)) {
+            double v[4];
+            stream(i, c, v);
+            bn_store4(a.x_out, a.x_bf16, base + c, v);
+        });
     }
 }
 
+// Two chunks a thread: a row's requests are all out at once and its passes short.  4096 rows of 4096 (fp32, bf16 -> fp32,
+// bf16) with 1 / 2 / 4 / 8 chunks a thread (1024 .. 128 threads) 67.7 / 50.7 / 54.7 / 57.5 us, 1000 rows (8-bit codes too) 21.8 /
+// 16.4 / 15.2 / 16.8, 301 of 2048 6.7 / 6.0 / 7.9 / 10.8, one 5.6 / 4.8 / 5.1 / 6.9; 2000 of 8192 - / 58.4 / 55.7 / 52.8.
 int moe_block_norm_launch(const MoeBlockNorm& a, hipStream_t s) {
-    const int d4 = a.d / 4;
-    int threads = 64;
-    while (threads < 1024 && threads * 2 < d4) threads *= 2;
-    const dim3 grid((unsigned)(a.T < (1 << 20) ? a.T : (1 << 20)));
-    hipLaunchKernelGGL(block_norm_kernel<2>, grid, dim3(threads), 0, s, a);
+    const int d4 = a.d / 4, V = d4 <= 2048 ? 2 : 4;
+    const bool held = d4 <= 1024 * V;
+    const int waves = held ? (d4 + 64 * V - 1) / (64 * V) : 16;
+    auto* kernel = !held ? block_norm_kernel<1, false> : V == 2 ? block_norm_kernel<2, true> : block_norm_kernel<4, true>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.T), dim3(64 * waves), 0, s, a);
     return moe_launch_status();
 }

@@ -1,6 +1,7 @@
 // Conversion of rows and matrices between fp32 / bf16 and 8-bit codes, and the one-time repack of
 // converted expert matrices into the order the kernels stream them.  All of it is bound by memory.
 #include <new>
+#include <type_traits>
 
 #include "moe_gate_wave.h"
 #include "moe_i8.h"
@@ -150,67 +151,134 @@ int moe_i8_rows_back_launch(const int8_t* codes, const float* scales, int T, int
 }
 
 // ------------------------------------------------------------------ matrices ----
-// W [K,C] has its channels along the rows and its codes along the reduction, so both directions are
-// transpositions through LDS, 64 channels wide.  To codes: a workgroup takes 64 channels and all of K, once
-// for the largest magnitudes and once for the codes.
-#define I8_CV_C 64
-#define I8_CV_K 256   // reduction indices of an LDS tile
-#define I8_CV_PAD 4   // bytes: a channel's row of the tile starts in another bank than its neighbour's
-
-template <bool BF16>
-__device__ __forceinline__ float i8_load1(const void* w, size_t at) {
-    return BF16 ? moe_bf16_to_f32(((const uint16_t*)w)[at]) : ((const float*)w)[at];
-}
-
-template <bool BF16>
-__global__ __launch_bounds__(1024) void i8_quantize_kernel(const void* __restrict__ w, int K, int C, int ctiles,
-                                                           int8_t* __restrict__ codes, float* __restrict__ scales) {
-    __shared__ unsigned s_top[16][I8_CV_C];
-    __shared__ __align__(16) unsigned char s_q[I8_CV_C][I8_CV_K + I8_CV_PAD];
-    const size_t e = blockIdx.x / ctiles;
-    const int c0 = (int)(blockIdx.x % ctiles) * I8_CV_C;
-    const int cl = threadIdx.x & 63, kg = threadIdx.x >> 6;  // a wave: 64 channels of one index
-    const int c = c0 + cl < C ? c0 + cl : C - 1;
-    const size_t base = e * K * C + c;
-    unsigned top = 0u;
-    for (int k = kg; k < K; k += 16) {
-        const unsigned o = __float_as_uint(i8_load1<BF16>(w, base + (size_t)k * C)) & 0x7FFFFFFFu;
-        top = top > o ? top : o;
+// W [K,C] has its channels along the rows and its codes along the reduction, so both directions are transpositions.
+//
+// To codes: a workgroup takes the channels of 64 bytes of a row and all of K.  A thread takes V neighbouring channels of 16
+// consecutive indices at a time, all requested at once and, up to HOLD times, kept in registers between the largest
+// magnitudes and the codes: such matrices are read once.  Longer reductions are read again, from the last-level cache.  The
+// two halves of a 128-byte line go to workgroups of one XCD.  Codes leave as 16 bytes a channel, 128 bytes and more of a
+// channel side by side.
+#define I8_QT 512
+#define I8_SEG 32
+template <bool BF16, int V>
+struct I8Quant {
+    static constexpr int LC = I8_SEG / (V * (BF16 ? 2 : 4));  // lanes across the channels
+    static constexpr int RG = I8_QT / LC;                 // groups of 16 indices of a round
+    static constexpr int HOLD = BF16 && V == 4 ? 2 : BF16 ? 4 : 2;
+    static constexpr int BYTES = V * (BF16 ? 2 : 4);      // of a thread's channels in a row
+    typedef std::conditional_t<BYTES == 8, uint2, std::conditional_t<BYTES == 4, unsigned, uint16_t>> Word;
+    struct Elems {
+        Word word;
+        __device__ __forceinline__ float at(int n) const {
+            unsigned u;
+            if constexpr (BYTES == 8) u = BF16 ? (n < 2 ? word.x : word.y) : n == 0 ? word.x : word.y;
+            else u = word;
+            if constexpr (BF16) return __uint_as_float((n & 1) ? u & 0xFFFF0000u : u << 16);
+            else return __uint_as_float(u);
+        }
+    };
+    // sixteen rows of V channels from element `at` on
+    static __device__ __forceinline__ void load(const void* w, size_t at, int C, Elems (&v)[16]) {
+        const char* p = (const char*)w + at * (BF16 ? 2 : 4);
+        const size_t step = (size_t)C * (BF16 ? 2 : 4);
+#pragma unroll
+        for (int i = 0; i < 16; i++) v[i].word = *(const Word*)(p + i * step);
     }
-    s_top[kg][cl] = top;
+};
+
+template <bool BF16, int V>
+__global__ __launch_bounds__(I8_QT) void i8_quantize_kernel(const void* __restrict__ w, int K, int C, int strips,
+                                                            int8_t* __restrict__ codes, float* __restrict__ scales) {
+    typedef I8Quant<BF16, V> Q;
+    constexpr int LC = Q::LC, HOLD = Q::HOLD;
+    __shared__ unsigned s_top[I8_QT / 64][LC * V];
+    const size_t e = blockIdx.y;
+    const int strip = (blockIdx.x & ~31) + (blockIdx.x & 7) * 4 + ((blockIdx.x >> 3) & 3);
+    if (strip >= strips) return;
+    const int cl = threadIdx.x % LC, rg0 = threadIdx.x / LC, wave = threadIdx.x >> 6;
+    const int c0 = (strip * LC + cl) * V;
+    const int c = c0 < C ? c0 : C - V;  // (C is a multiple of V)
+    const size_t base = e * K * C + c;
+    const int groups = K / 16;
+    typename Q::Elems v[HOLD][16];
+    unsigned top[V];
+#pragma unroll
+    for (int n = 0; n < V; n++) top[n] = 0u;
+    auto raise = [&](const typename Q::Elems (&u)[16]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+#pragma unroll
+            for (int n = 0; n < V; n++) {
+                const unsigned o = __float_as_uint(u[i].at(n)) & 0x7FFFFFFFu;
+                top[n] = top[n] > o ? top[n] : o;
+            }
+    };
+#pragma unroll
+    for (int h = 0; h < HOLD; h++)
+        if (rg0 + h * Q::RG < groups) Q::load(w, base + (size_t)(rg0 + h * Q::RG) * 16 * C, C, v[h]);
+#pragma unroll
+    for (int h = 0; h < HOLD; h++)
+        if (rg0 + h * Q::RG < groups) raise(v[h]);
+    for (int g = rg0 + HOLD * Q::RG; g < groups; g += Q::RG) {
+        typename Q::Elems u[16];
+        Q::load(w, base + (size_t)g * 16 * C, C, u);
+        raise(u);
+    }
+#pragma unroll
+    for (int n = 0; n < V; n++) {
+#pragma unroll
+        for (int m = LC; m < 64; m <<= 1) {
+            const unsigned o = (unsigned)__shfl_xor((int)top[n], m, 64);
+            top[n] = top[n] > o ? top[n] : o;
+        }
+        if ((threadIdx.x & 63) < LC) s_top[wave][cl * V + n] = top[n];
+    }
     __syncthreads();
+    float scale[V];
 #pragma unroll
-    for (int i = 0; i < 16; i++) top = top > s_top[i][cl] ? top : s_top[i][cl];
-    const float scale = i8_scale(top);
-    const I8Coder code(scale);
-    if (kg == 0 && c0 + cl < C) scales[e * C + c] = scale;
-    for (int k0 = 0; k0 < K; k0 += I8_CV_K) {
-        const int kn = K - k0 < I8_CV_K ? K - k0 : I8_CV_K;
-        for (int k = kg * 4; k < kn; k += 64) {
-            float v[4];
+    for (int n = 0; n < V; n++) {
+        unsigned t = 0u;
+        for (int i = 0; i < I8_QT / 64; i++) t = t > s_top[i][cl * V + n] ? t : s_top[i][cl * V + n];
+        scale[n] = i8_scale(t);
+        if (rg0 == 0 && c0 < C) scales[e * C + c + n] = scale[n];
+    }
+    if (c0 >= C) return;
+    auto put = [&](int g, const typename Q::Elems (&u)[16]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 4; i++) v[i] = i8_load1<BF16>(w, base + (size_t)(k0 + k + i) * C);
-            *(unsigned*)&s_q[cl][k] = code(make_float4(v[0], v[1], v[2], v[3]));
+        for (int n = 0; n < V; n++) {
+            const I8Coder code(scale[n]);
+            u32x4_t q;
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                q[i] = code(make_float4(u[4 * i].at(n), u[4 * i + 1].at(n), u[4 * i + 2].at(n), u[4 * i + 3].at(n)));
+            *(u32x4_t*)(codes + (e * C + c + n) * K + (size_t)g * 16) = q;
         }
-        __syncthreads();
-        // sixteen bytes of a channel a thread: K is a multiple of 16
-        const int cc = threadIdx.x >> 4, b = (threadIdx.x & 15) * 16;
-        if (c0 + cc < C && b < kn) {
-            const unsigned* p = (const unsigned*)&s_q[cc][b];
-            *(u32x4_t*)(codes + (e * C + c0 + cc) * K + k0 + b) = u32x4_t{p[0], p[1], p[2], p[3]};
-        }
-        __syncthreads();
+    };
+#pragma unroll
+    for (int h = 0; h < HOLD; h++)
+        if (rg0 + h * Q::RG < groups) put(rg0 + h * Q::RG, v[h]);
+    for (int g = rg0 + HOLD * Q::RG; g < groups; g += Q::RG) {
+        typename Q::Elems u[16];
+        Q::load(w, base + (size_t)g * 16 * C, C, u);
+        put(g, u);
     }
 }
 
 int moe_i8_quantize_launch(const void* w, moe_dtype_t w_dtype, int E, int K, int C, int8_t* codes, float* scales,
                            hipStream_t s) {
-    const int ctiles = (C + I8_CV_C - 1) / I8_CV_C;
-    auto* kernel = w_dtype == MOE_BF16 ? i8_quantize_kernel<true> : i8_quantize_kernel<false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(E * ctiles)), dim3(1024), 0, s, w, K, C, ctiles, codes, scales);
+    const bool bf16 = w_dtype == MOE_BF16;
+    const int V = bf16 && C % 4 == 0 ? 4 : C % 2 == 0 ? 2 : 1;
+    const int wide = I8_SEG / (bf16 ? 2 : 4), strips = (C + wide - 1) / wide;
+    auto* kernel = bf16 ? (V == 4 ? i8_quantize_kernel<true, 4> : V == 2 ? i8_quantize_kernel<true, 2> : i8_quantize_kernel<true, 1>)
+                        : (V == 2 ? i8_quantize_kernel<false, 2> : i8_quantize_kernel<false, 1>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(strips + 31) & ~31u, (unsigned)E), dim3(I8_QT), 0, s, w, K, C, strips, codes, scales);
     return moe_launch_status();
 }
 
+// From codes: a tile of 64 channels by 256 indices through LDS.
+#define I8_CV_C 64
+#define I8_CV_K 256
+#define I8_CV_PAD 4  // bytes: a channel's row of the tile starts in another bank than its neighbour's
 template <bool BF16>
 __global__ __launch_bounds__(1024) void i8_dequantize_kernel(const int8_t* __restrict__ codes, const float* __restrict__ scales,
                                                              int K, int C, int ctiles, void* __restrict__ w) {

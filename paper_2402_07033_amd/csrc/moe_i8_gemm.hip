@@ -2,8 +2,8 @@
 // of a batch whose segments only the device knows.  The expert FFN is two of them: the first one's epilogue
 // applies silu(a)*b, its rows are brought to 8 bits again, and the second one reads them.
 //
-//   * tile: up to 32*RB rows of one expert x 256 channels (fragment rows of w); an expert's blocks of 32 rows
-//     are dealt evenly to its tiles, and the loop exists once per number of blocks.
+//   * tile: up to 16*WT*RB rows of one expert x 16*WF*FB channels (fragment rows of w) for WT x WF waves; an expert's
+//     blocks of 16*WT rows are dealt evenly to its tiles, and the loop exists once per number of blocks.
 //   * both operands travel through a ring of NS stages of LDS, 64 reduction indices each, which the waves fill
 //     with direct-to-LDS loads NS - 1 steps ahead.  Rows (and matrices that are not packed) are read where
 //     they lie: four lanes take 64 bytes of a row, and the four chunks are stored rotated by the row, so that
@@ -260,11 +260,29 @@ static int i8_gemm_go(I8GemmArgs& a, hipStream_t s) {
     return moe_launch_status();
 }
 
-static bool i8_large(int N, int E) { return N > 64 * (N < E ? N : E); }
+// Tiles, rows x channels: 256 x 256 where they fill the chip and an expert in use has more than 128 rows on average; else 128 x
+// 128 where those do; else 32 x 128.  us with 32 x 128 / 128 x 128 / 256 x 256: first projection (d 4096, f 14336) of 8
+// experts of 24 rows 159 / 157 / 165, of 64 207 / 175 / 178, of 128 338 / 214 / 204, of 512 1190 / 658 / 518; the second of 24 rows 82 / 83 /
+// 104, of 128 185 / 116 / 151, of 512 649 / 317 / 239; one 4096 x 4096 matrix, 77 rows 15 / 22 / 31, 512 28 / 28 / 61, 1024 49 / 30 / 63,
+// 4096 193 / 96 / 79.
+struct I8Shape {
+    int rows, channels;
+};
+static I8Shape i8_shape(int N, int E, int NR) {
+    const int used = N < E ? N : E;
+    auto fills = [&](int rows, int channels) {
+        return ((long long)N / rows + used) * ((NR * 16 + channels - 1) / channels) >= 200;
+    };
+    if (N > 128 * used && fills(256, 256)) return {256, 256};
+    return fills(128, 128) ? I8Shape{128, 128} : I8Shape{32, 128};
+}
+
 template <bool PACKED, bool GATED>
 static int i8_gemm_pick(I8GemmArgs& a, hipStream_t s) {
-    if (!i8_large(a.p.N, a.p.E)) return i8_gemm_go<1, 4, 4, 3, 4, PACKED, GATED>(a, s);
-    return i8_gemm_go<2, 4, 4, 4, 8, PACKED, GATED>(a, s);
+    const int rows = i8_shape(a.p.N, a.p.E, a.NR).rows;
+    if (rows == 32) return i8_gemm_go<1, 4, 2, 4, 2, PACKED, GATED>(a, s);
+    if (rows == 128) return i8_gemm_go<2, 2, 4, 4, 4, PACKED, GATED>(a, s);
+    return i8_gemm_go<2, 4, 4, 3, 8, PACKED, GATED>(a, s);
 }
 
 int moe_i8_product_launch(const I8Product& p, int path, hipStream_t s) {
@@ -296,15 +314,24 @@ static I8FfnSpace i8_ffn_space(int N, int d, int f) {
 size_t moe_i8_ffn_workspace(int N, int E, int d, int f) {
     return d <= I8_MAX_K && f <= I8_MAX_K ? i8_ffn_space(N, d, f).bytes : 0;
 }
-int moe_i8_auto_path(int N, int E) { return N <= 16 * (N < E ? N : E) ? MOE_FFN_STREAM : MOE_FFN_GROUPED; }
+// STREAM reads a matrix once for every 16 rows, so skewed batches leave it before balanced ones: 8 experts of 4 / 12 / 16 / 20 rows,
+// first projection, STREAM 139 / 144 / 151 / 280 us, 128 x 128 tiles 154 / 156 / 155 / 156; 64 experts (d 2048, f 1408) of 8 / 16 / 20 rows
+// 60 / 68 / 100 and 65 / 67 / 68; one 4096 x 4096 matrix, which stays in the caches, 32 / 64 rows 9.5 / 15.5 and 14.3 / 14.5.
+int moe_i8_auto_path(int N, int E) {
+    const int used = N < E ? N : E;
+    return N <= (E == 1 ? 32 : 8 * used) ? MOE_FFN_STREAM : MOE_FFN_GROUPED;
+}
 bool moe_i8_ffn_supported(int path, int N, int E, int d, int f) {
     return (path == MOE_FFN_GROUPED || path == MOE_FFN_STREAM) && moe_i8_product_supported(N, E, d, f) && moe_i8_product_supported(N, E, f, d);
 }
 int moe_i8_ffn_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan) {
     if (!moe_i8_ffn_supported(plan->path, N, E, d, f)) return MOE_ERR_UNSUPPORTED;
     if (plan->path == MOE_FFN_STREAM) return MOE_OK;
-    plan->up_tile_rows = plan->down_tile_rows = i8_large(N, E) ? 256 : 64;
-    plan->up_tile_features = plan->down_tile_features = 256;
+    const I8Shape up = i8_shape(N, E, f / 8), down = i8_shape(N, E, d / 16);
+    plan->up_tile_rows = up.rows;
+    plan->up_tile_features = up.channels;
+    plan->down_tile_rows = down.rows;
+    plan->down_tile_features = down.channels;
     return MOE_OK;
 }
 

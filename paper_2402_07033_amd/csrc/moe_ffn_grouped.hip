@@ -70,6 +70,21 @@
 #include "moe_gg_ring.h"
 #include "moe_gg_sched.h"
 
+// The loop, its schedule and the fix-up serve 8-bit operands as well (GG_INT8, compiled by moe_i8_grouped.hip): a fragment
+// of 16 rows by 64 indices is the same KiB, v_mfma_i32_16x16x64_i8 takes the clocks of v_mfma_f32_16x16x32_bf16, and only
+// the sums' type and the epilogues differ.  "Steps" are then of 64 indices.
+#ifdef GG_INT8
+#include "moe_i8_value.h"
+namespace gg_int8 {
+constexpr bool GG_I8 = true;
+typedef i32x4_t gg_acc_t;
+#define GG_MFMA "v_mfma_i32_16x16x64_i8"
+#else
+constexpr bool GG_I8 = false;
+typedef f32x4_t gg_acc_t;
+#define GG_MFMA "v_mfma_f32_16x16x32_bf16"
+#endif
+
 // Tile shapes (token rows x weight fragment rows of 16 features per workgroup), by the mean
 // number of rows per expert:
 //   256 x 16 (256 tokens x 256 features): the default;
@@ -124,7 +139,12 @@ struct GroupedArgs {
     int KS_out;  // up: f/32 (fragment columns of hp); down: unused
     int C;       // down: d (row length of yg)
     int split;   // gg_split_limit, or 0: nothing is cut
-    float* part; // split: partial tiles [8 XCDs][workgroups per XCD][2][256*256] fp32
+    float* part; // split: partial tiles [8 XCDs][workgroups per XCD][2][256*256] sums
+    // 8 bits: scales of the packed rows [blocks][16] and of the channels in the order of the fragment rows; up: out is h
+    // [N,C] fp32, and top [C/32][N] the bits of the largest magnitude of 32 channels of a row
+    const float* bscale;
+    const float* wscale;
+    unsigned* top;
 };
 
 // s_waitcnt with only one counter constrained (gfx9 encoding: vmcnt = bits 3:0 and
@@ -202,7 +222,7 @@ __device__ __forceinline__ int gg_seg_table(const GroupedArgs& a, int wgs, int l
 
 // The schedule's turn, decided by one wave from the table (moe_gg_sched.h).
 __device__ __forceinline__ bool gg_turned(const int (*tab)[64], int lane, int total, int NT, int KS) {
-    return gg_turned(__popcll(__ballot(tab[GG_SEG_TILES][lane] == 1)), total, NT, KS);
+    return ::gg_turned(__popcll(__ballot(tab[GG_SEG_TILES][lane] == 1)), total, NT, KS);
 }
 
 // Logical tile index -> tile, from the table.  UB: blocks of a unit.
@@ -289,19 +309,19 @@ __device__ __forceinline__ int gg_lane_opaque() {
 // MFMA with the accumulator pinned to the accumulation registers: 256 of them
 // are live per wave, and left to itself the register allocator shuffles them
 // through the vector registers inside the loop.
-__device__ __forceinline__ void gg_mfma(f32x4_t& c, const u32x4_t& a, const u32x4_t& b) {
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+__device__ __forceinline__ void gg_mfma(gg_acc_t& c, const u32x4_t& a, const u32x4_t& b) {
+    asm volatile(GG_MFMA " %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
 // ... with a zero accumulator going in (the first step of a tile)
-__device__ __forceinline__ void gg_mfma_first(f32x4_t& c, const u32x4_t& a, const u32x4_t& b) {
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(c) : "v"(a), "v"(b));
+__device__ __forceinline__ void gg_mfma_first(gg_acc_t& c, const u32x4_t& a, const u32x4_t& b) {
+    asm volatile(GG_MFMA " %0, %1, %2, 0" : "=a"(c) : "v"(a), "v"(b));
 }
 // ... in vector registers: the tiles beyond the 64th of a wave
-__device__ __forceinline__ void gg_mfma_v(f32x4_t& c, const u32x4_t& a, const u32x4_t& b) {
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
+__device__ __forceinline__ void gg_mfma_v(gg_acc_t& c, const u32x4_t& a, const u32x4_t& b) {
+    asm volatile(GG_MFMA " %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
 }
-__device__ __forceinline__ void gg_mfma_first_v(f32x4_t& c, const u32x4_t& a, const u32x4_t& b) {
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "v"(b));
+__device__ __forceinline__ void gg_mfma_first_v(gg_acc_t& c, const u32x4_t& a, const u32x4_t& b) {
+    asm volatile(GG_MFMA " %0, %1, %2, 0" : "=&v"(c) : "v"(a), "v"(b));
 }
 
 // Buffer descriptor over the 2 GiB of addresses from p on (p is wave-uniform, which the compiler does not
@@ -356,21 +376,6 @@ struct GgInt {
     static constexpr int value = V;
 };
 
-// a / (1 + exp(-a)), to the bits of the fp32 division (16 M values of each of N(0,1), N(0,16) and
-// -90..90, infinities, NaN): the reciprocal estimate, then one correction of the quotient by its
-// exact residual.  The estimate is taken of a quarter of the denominator, because v_rcp_f32 flushes the
-// reciprocals of denominators above 2^126 (a < -87.3) to zero.  (ldexp: 0.25 is no inline constant,
-// and a register for it spills in the 256-row tile.)  The compiler's division takes 11 instructions
-// where these are 8: layer of 4096 tokens 2.419 -> 2.409 ms; with the estimate alone (mean error 12 %
-// larger, zero below -87.3) 2.392.
-__device__ __forceinline__ float gg_silu(float a) {
-    const float e = __expf(-a), den = 1.0f + e;
-    const float r = __builtin_ldexpf(__builtin_amdgcn_rcpf(__builtin_ldexpf(den, -2)), -2);
-    float q = a * r;
-    q = __builtin_fmaf(__builtin_fmaf(-q, den, a), r, q);
-    return __builtin_amdgcn_div_fixupf(q, den, a);
-}
-
 // First projection: h = silu(x.w1) * (x.w3) of two neighbouring 16-column blocks (a0, b0: the
 // w1 and w3 tiles of the even block; a1, b1: of the odd one), rounded to bf16, as B fragments of
 // the second GEMM.  Lane l of a tile holds token l % 16 and columns 4*(l/16) .. +3; after
@@ -400,6 +405,84 @@ __device__ __forceinline__ u32x4_t gg_make_h(const f32x4_t& a0, const f32x4_t& b
 __device__ __forceinline__ unsigned gg_h_off(int lane) {
     return (unsigned)(((((lane >> 4) & 1) * 2 + (lane >> 5)) * 16 + (lane & 15)) * 16);
 }
+
+#ifdef GG_INT8
+// Eight 32-bit values: where the lane's 16-byte store goes inside a tile of rows of C floats, or behind the descriptor.
+template <int FRW, bool FLEX>
+__device__ __forceinline__ bool gg_int8_has(const TileInfo& ti, int wave, int j) {
+    return !FLEX || wave + (j / 4) * 4 < ti.groups;
+}
+// h of fragment rows (w1, w3) at fr and fr + 1, or y of one: four channels of a row, and the bits of their largest magnitude.
+__device__ __forceinline__ f32x4_t gg_int8_h(const i32x4_t& a, const i32x4_t& b, float sx, const f32x4_t& sa, const f32x4_t& sb,
+                                             unsigned& top) {
+    f32x4_t h;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        h[i] = gg_silu(i8_value(a[i], sx, sa[i])) * i8_value(b[i], sx, sb[i]);
+        const unsigned m = __float_as_uint(h[i]) & 0x7FFFFFFFu;
+        top = top > m ? top : m;
+    }
+    return h;
+}
+// The largest of the four lanes that hold a row's channels, in all of them.
+__device__ __forceinline__ unsigned gg_int8_top(unsigned v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = a[0] > a[1] ? a[0] : a[1];
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return b[0] > b[1] ? b[0] : b[1];
+}
+// A whole tile's results; returns the number of stores.
+template <bool UP, int B, int FRW, bool FLEX>
+__device__ __forceinline__ int gg_int8_epilogue(const GroupedArgs& a, const TileInfo& cur, int wave, int lane,
+                                                gg_acc_t (&acc)[B][FRW]) {
+    const int t = lane & 15, r0 = cur.blk0 * 16, rows = cur.si.rows - r0;
+    const int frow = cur.frow + gg_wave_row<FRW, FLEX>(wave, 0);
+    f32x4_t ws[FRW];
+    float sx[B];
+    const float* wsp = a.wscale + ((size_t)cur.si.e * a.FR + frow) * 16 + 4 * (lane >> 4);
+    const float* bsp = a.bscale + (size_t)(cur.si.bbase + cur.blk0) * 16 + t;
+#pragma unroll
+    for (int j = 0; j < FRW; j++)
+        ws[j] = gg_int8_has<FRW, FLEX>(cur, wave, j) ? *(const f32x4_t*)(wsp + gg_wave_row<FRW, FLEX>(0, j) * 16) : f32x4_t{};
+#pragma unroll
+    for (int i = 0; i < B; i++) sx[i] = bsp[(i < cur.nblk ? i : 0) * 16];
+    // first row and channel of the tile
+    const __amdgpu_buffer_rsrc_t rs = gg_rsrc((const char*)((float*)a.out + (size_t)(cur.si.row0 + r0) * a.C + frow * (UP ? 8 : 16)));
+    const unsigned vo = (unsigned)t * (unsigned)a.C * 4u + (unsigned)(lane >> 4) * 16u;
+#pragma unroll
+    for (int i = 0; i < B; i++) {
+        const unsigned row = i * 16 + t < rows ? vo + (unsigned)(i * 16) * (unsigned)a.C * 4u : GG_RSRC_BYTES;
+        if constexpr (UP) {
+#pragma unroll
+            for (int jj = 0; jj < FRW / 4; jj++) {
+                const bool has = gg_int8_has<FRW, FLEX>(cur, wave, 4 * jj);
+                unsigned top = 0u;
+#pragma unroll
+                for (int q = 0; q < 2; q++) {
+                    const int j = 4 * jj + 2 * q;
+                    const f32x4_t h = gg_int8_h(acc[i][j], acc[i][j + 1], sx[i], ws[j], ws[j + 1], top);
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, h), rs, has ? row : GG_RSRC_BYTES,
+                                                           gg_wave_row<FRW, FLEX>(0, j) * 32, 0);
+                }
+                top = gg_int8_top(top);
+                if (lane < 16 && has && i * 16 + t < rows)
+                    a.top[(size_t)((frow + gg_wave_row<FRW, FLEX>(0, 4 * jj)) / 4) * a.N + cur.si.row0 + r0 + i * 16 + t] = top;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < FRW; j++) {
+                f32x4_t y;
+#pragma unroll
+                for (int q = 0; q < 4; q++) y[q] = i8_value(acc[i][j][q], sx[i], ws[j][q]);
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, y), rs,
+                                                       gg_int8_has<FRW, FLEX>(cur, wave, j) ? row : GG_RSRC_BYTES,
+                                                       gg_wave_row<FRW, FLEX>(0, j) * 64, 0);
+            }
+        }
+    }
+    return UP ? B * (FRW / 2) : B * FRW;
+}
+#endif
 
 // MODE: which units of work this copy of the loop covers: 0 = whole tiles and pieces, 1 = whole tiles
 // only, 2 = pieces only.
@@ -570,7 +653,7 @@ __device__ __forceinline__ void gg_gemm_body(const GroupedArgs& a, int NT, int t
         // token fragments in registers: a whole step's, or a ring of half as many where the accumulators
         // need the registers
         constexpr int RB = B * FRW > 64 ? B / 2 : B;
-        f32x4_t acc[B][FRW];
+        gg_acc_t acc[B][FRW];
         u32x4_t breg[RB];
         g = __builtin_amdgcn_readfirstlane(g);
         const __amdgpu_buffer_rsrc_t ra = gg_rsrc(pa), rb = gg_rsrc(pb), ra_n = gg_rsrc(pa_n), rb_n = gg_rsrc(pb_n);
@@ -717,6 +800,8 @@ __device__ __forceinline__ void gg_gemm_body(const GroupedArgs& a, int NT, int t
                                                            (i * FRW + j) * 1024, 0);
             }
             stores = B * FRW;
+        } else if constexpr (GG_I8) {
+            stores = gg_int8_epilogue<UP, B, FRW, FLEX>(a, cur, wave, lane_e, acc);
         } else if (UP) {
             // fragment rows 4jj..4jj+3 of this wave: w1, w3 of an even and of the next column block
             const int ks_o = (cur.frow + gg_wave_row<FRW, FLEX>(wave, 0)) / 4;  // h fragment column of jj = 0
@@ -865,9 +950,9 @@ __global__ __launch_bounds__(256) void gg_fixup_kernel(GroupedArgs a, int wgs, i
             }
         }
         unsigned long long m = __ballot(slot >= 0);
-        f32x4_t c[FRW];
+        gg_acc_t c[FRW];
 #pragma unroll
-        for (int j = 0; j < FRW; j++) c[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < FRW; j++) c[j] = gg_acc_t{0, 0, 0, 0};
         const float* src = a.part + (size_t)(wave * NBW + i) * (FRW * 256) + lane * 4;
         while (m) {
             const float* p0 = src + (size_t)__builtin_amdgcn_readlane(slot, (int)__builtin_ctzll(m)) * (256 * 256);
@@ -875,11 +960,11 @@ __global__ __launch_bounds__(256) void gg_fixup_kernel(GroupedArgs a, int wgs, i
             const bool two = m != 0ull;
             const float* p1 = two ? src + (size_t)__builtin_amdgcn_readlane(slot, (int)__builtin_ctzll(m)) * (256 * 256) : p0;
             m &= m - 1;
-            f32x4_t v0[FRW], v1[FRW];
+            gg_acc_t v0[FRW], v1[FRW];
 #pragma unroll
-            for (int j = 0; j < FRW; j++) v0[j] = *(const f32x4_t*)(p0 + j * 256);
+            for (int j = 0; j < FRW; j++) v0[j] = *(const gg_acc_t*)(p0 + j * 256);
 #pragma unroll
-            for (int j = 0; j < FRW; j++) v1[j] = *(const f32x4_t*)(p1 + j * 256);
+            for (int j = 0; j < FRW; j++) v1[j] = *(const gg_acc_t*)(p1 + j * 256);
 #pragma unroll
             for (int j = 0; j < FRW; j++) {
                 c[j] += v0[j];
@@ -887,7 +972,17 @@ __global__ __launch_bounds__(256) void gg_fixup_kernel(GroupedArgs a, int wgs, i
             }
         }
         const int blk = ti.blk0 + i;  // block inside the segment
-        if (UP) {
+        if constexpr (GG_I8) {
+            // the block alone, as a tile of its own
+            gg_acc_t one[1][FRW];
+#pragma unroll
+            for (int j = 0; j < FRW; j++) one[0][j] = c[j];
+            TileInfo tb = ti;
+            tb.blk0 = blk;
+            tb.nblk = 1;
+            tb.frow = ti.nt * FROWS;
+            gg_int8_epilogue<UP, 1, FRW, false>(a, tb, wave, lane, one);
+        } else if (UP) {
             const int ks_o = ti.nt * (FROWS / 4) + (FRW / 4) * wave;
             unsigned char* dst = (unsigned char*)a.out + ((size_t)(ti.si.bbase + blk) * a.KS_out + ks_o) * 1024 +
                                  gg_h_off(lane);
@@ -900,7 +995,7 @@ __global__ __launch_bounds__(256) void gg_fixup_kernel(GroupedArgs a, int wgs, i
                 float* dst = (float*)a.out + (size_t)(ti.si.row0 + row) * a.C + (ti.nt * FROWS + FRW * wave) * 16 +
                              4 * (lane >> 4);
 #pragma unroll
-                for (int j = 0; j < FRW; j++) *(f32x4_t*)(dst + j * 16) = c[j];
+                for (int j = 0; j < FRW; j++) *(gg_acc_t*)(dst + j * 16) = c[j];
             }
         }
     }
@@ -963,8 +1058,10 @@ int gg_launch_projection(GroupedArgs& a, GgVariant v, unsigned pgrid, hipStream_
     return MOE_OK;
 }
 
+#ifdef GG_INT8
+}  // namespace gg_int8
 // The second projection's kernels are compiled in a file of their own, beside the first's (a minute and a half each).
-#ifdef GG_SECOND_PROJECTION
+#elif defined(GG_SECOND_PROJECTION)
 template const void* gg_kernel_ptr<false>(GgVariant);
 template int gg_launch_projection<false>(GroupedArgs&, GgVariant, unsigned, hipStream_t);
 #else

@@ -5,6 +5,21 @@
 
 #include "moe_internal.h"
 
+// a / (1 + exp(-a)), to the bits of the fp32 division (16 M values of each of N(0,1), N(0,16) and
+// -90..90, infinities, NaN): the reciprocal estimate, then one correction of the quotient by its
+// exact residual.  The estimate is taken of a quarter of the denominator, because v_rcp_f32 flushes the
+// reciprocals of denominators above 2^126 (a < -87.3) to zero.  (ldexp: 0.25 is no inline constant,
+// and a register for it spills in the 256-row tile.)  The compiler's division takes 11 instructions
+// where these are 8: layer of 4096 tokens 2.419 -> 2.409 ms; with the estimate alone (mean error 12 %
+// larger, zero below -87.3) 2.392.
+__device__ __forceinline__ float gg_silu(float a) {
+    const float e = __expf(-a), den = 1.0f + e;
+    const float r = __builtin_ldexpf(__builtin_amdgcn_rcpf(__builtin_ldexpf(den, -2)), -2);
+    float q = a * r;
+    q = __builtin_fmaf(__builtin_fmaf(-q, den, a), r, q);
+    return __builtin_amdgcn_div_fixupf(q, den, a);
+}
+
 // ---- segment bookkeeping: expert e owns blocks [bbase_e, bbase_e + ceil(M_e/16)) ----
 struct SegInfo {
     int e;        // expert

@@ -152,3 +152,10 @@ int moe_i8_down_small_launch(const moe_weights* W, const float* h, const unsigne
 // given, the rest filled in here.  ws: the FFN's workspace and [N,d] floats behind it.
 int moe_i8_layer_launch(const moe_weights* W, I8Front f, moe_dtype_t x_dtype, void* ws, void* y, moe_dtype_t y_dtype, int path,
                         hipStream_t s);
+
+// The expert FFN of many rows per expert (moe_i8_grouped.hip), from codes.
+bool moe_i8_grouped_supported(int N, int E, int d, int f);
+size_t moe_i8_grouped_workspace(int N, int E, int d, int f);
+int moe_i8_grouped_tile_rows(int N, int E);
+int moe_i8_grouped_launch(const moe_weights* W, const int8_t* codes, const float* scales, const int32_t* perm, int k,
+                          const int32_t* offsets, int N, void* ws, float* yg, hipStream_t s);

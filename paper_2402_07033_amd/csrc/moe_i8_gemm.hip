@@ -300,7 +300,12 @@ int moe_i8_product_launch(const I8Product& p, int path, hipStream_t s) {
 struct I8FfnSpace {
     size_t xq, xs, h, hq, hs, top, bytes;
 };
-static I8FfnSpace i8_ffn_space(int N, int d, int f) {
+// Do both projections take the persistent loop?
+static bool i8_persistent(int N, int E, int d, int f) {
+    return i8_shape(N, E, f / 8).rows == 256 && i8_shape(N, E, d / 16).rows == 256 && moe_i8_grouped_supported(N, E, d, f);
+}
+
+static I8FfnSpace i8_ffn_space(int N, int E, int d, int f) {
     I8FfnSpace w;
     w.xq = 0;
     w.xs = i8_align256((size_t)N * d);
@@ -309,10 +314,14 @@ static I8FfnSpace i8_ffn_space(int N, int d, int f) {
     w.hs = w.hq + i8_align256((size_t)N * f);
     w.top = w.hq;
     w.bytes = w.hs + i8_align256((size_t)N * 4);
+    if (i8_persistent(N, E, d, f)) {
+        const size_t b = w.h + moe_i8_grouped_workspace(N, E, d, f);
+        w.bytes = b > w.bytes ? i8_align256(b) : w.bytes;
+    }
     return w;
 }
 size_t moe_i8_ffn_workspace(int N, int E, int d, int f) {
-    return d <= I8_MAX_K && f <= I8_MAX_K ? i8_ffn_space(N, d, f).bytes : 0;
+    return d <= I8_MAX_K && f <= I8_MAX_K ? i8_ffn_space(N, E, d, f).bytes : 0;
 }
 // STREAM reads a matrix once for every 16 rows, so skewed batches leave it before balanced ones: 8 experts of 4 / 12 / 16 / 20 rows,
 // first projection, STREAM 139 / 144 / 151 / 280 us, 128 x 128 tiles 154 / 156 / 155 / 156; 64 experts (d 2048, f 1408) of 8 / 16 / 20 rows
@@ -328,9 +337,10 @@ int moe_i8_ffn_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan) {
     if (!moe_i8_ffn_supported(plan->path, N, E, d, f)) return MOE_ERR_UNSUPPORTED;
     if (plan->path == MOE_FFN_STREAM) return MOE_OK;
     const I8Shape up = i8_shape(N, E, f / 8), down = i8_shape(N, E, d / 16);
-    plan->up_tile_rows = up.rows;
+    const bool persistent = i8_persistent(N, E, d, f);
+    plan->up_tile_rows = persistent ? moe_i8_grouped_tile_rows(N, E) : up.rows;
     plan->up_tile_features = up.channels;
-    plan->down_tile_rows = down.rows;
+    plan->down_tile_rows = persistent ? plan->up_tile_rows : down.rows;
     plan->down_tile_features = down.channels;
     return MOE_OK;
 }
@@ -340,6 +350,11 @@ static int i8_experts(const moe_weights* W, const int8_t* codes, const float* sc
                       const int32_t* offsets, int N, char* base, const I8FfnSpace& sp, float* yg, const I8Combine* c, int path,
                       hipStream_t s) {
     const int E = W->E, d = W->d, f = W->f;
+    if (path == MOE_FFN_GROUPED && i8_persistent(N, E, d, f)) {
+        const int rc = moe_i8_grouped_launch(W, codes, scales, perm, k, offsets, N, base + sp.h, yg, s);
+        if (rc != MOE_OK || !c) return rc;
+        return moe_mx_combine_launch(yg, 1, 0, c->inv_perm, c->weights, c->T, c->k, d, c->y, c->y_bf16 ? MOE_BF16 : MOE_F32, s);
+    }
     const bool small = path == MOE_FFN_STREAM && moe_i8_down_small_serves(N, f);
     I8Product up = {};
     up.x = codes;
@@ -382,7 +397,7 @@ static int i8_experts(const moe_weights* W, const int8_t* codes, const float* sc
 
 int moe_i8_ffn_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtype, int rows, const int32_t* perm, int k,
                       const int32_t* offsets, int N, void* ws, float* yg, int path, hipStream_t s) {
-    const I8FfnSpace sp = i8_ffn_space(N, W->d, W->f);
+    const I8FfnSpace sp = i8_ffn_space(N, W->E, W->d, W->f);
     char* base = (char*)ws;
     int8_t* codes = (int8_t*)(base + sp.xq);
     float* scales = (float*)(base + sp.xs);
@@ -393,7 +408,7 @@ int moe_i8_ffn_launch(const moe_weights* W, const void* x, moe_dtype_t act_dtype
 int moe_i8_layer_launch(const moe_weights* W, I8Front f, moe_dtype_t x_dtype, void* ws, void* y, moe_dtype_t y_dtype, int path,
                         hipStream_t s) {
     const int N = f.T * f.k;
-    const I8FfnSpace sp = i8_ffn_space(N, W->d, W->f);
+    const I8FfnSpace sp = i8_ffn_space(N, W->E, W->d, W->f);
     char* base = (char*)ws;
     f.E = W->E;
     f.d = W->d;

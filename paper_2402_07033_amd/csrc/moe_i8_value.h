@@ -2,6 +2,7 @@
 // family ends in these, so their results are the same bits.  Device code only.
 #pragma once
 
+#include "moe_frag_pack.h"
 #include "moe_i8.h"
 
 // y[row, c .. c+3] of expert e; channels past C are dropped.
@@ -38,7 +39,7 @@ __device__ __forceinline__ unsigned i8_put_gated(const I8Product& p, int e, int 
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const float t = i8_value(a[i], sx, sa[i]);
-        h[i] = t / (1.0f + __expf(-t)) * i8_value(b[i], sx, sb[i]);
+        h[i] = gg_silu(t) * i8_value(b[i], sx, sb[i]);
     }
     *(float4*)((float*)p.y + row * p.C + fr * 8 + 4 * cq) = make_float4(h[0], h[1], h[2], h[3]);
     unsigned top = 0u;

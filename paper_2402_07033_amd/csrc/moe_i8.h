@@ -87,7 +87,7 @@ int moe_i8_rows_launch(const void* x, moe_dtype_t x_dtype, int T, int K, int8_t*
 
 // What a layer of a few tokens does before its products, in one launch: routing and batching (N = T*k slots), rows to 8
 // bits (x null: they are already).
-#define I8_FRONT_SLOTS 64
+#define I8_FRONT_SLOTS 512
 struct I8Front {
     const float* logits;
     int T, k, E;

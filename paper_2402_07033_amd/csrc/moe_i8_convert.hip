@@ -101,23 +101,70 @@ int moe_i8_rows_launch(const void* x, moe_dtype_t x_dtype, int T, int K, int8_t*
 template <bool BF16>
 __global__ __launch_bounds__(1024) void i8_front_kernel(I8Front f) {
     __shared__ unsigned s_top[16];
-    __shared__ int s_idx[I8_FRONT_SLOTS], s_pos[I8_FRONT_SLOTS], s_cnt[64];
+    __shared__ int s_idx[I8_FRONT_SLOTS], s_pos[I8_FRONT_SLOTS], s_next[64];
     if (blockIdx.x > 0) {
         i8_row<BF16, 4>(f.x, blockIdx.x - 1, f.d / 4, f.codes, f.scales, s_top);
         return;
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), N = f.T * f.k;
     gate_route_any(f.logits, f, f.E, wave, blockDim.x >> 6, lane, s_idx, true);
+    if (threadIdx.x < 64) s_next[threadIdx.x] = 0;
     __syncthreads();
-    if (wave > 0) return;
-    int lo, cnt;
-    gate_batch_any(s_idx, N, f.E, lane, true, f, s_pos, s_cnt, lo, cnt);
+    if (wave == 0) {
+        // places inside the experts' segments, 64 slots at a time: a ballot for each bit of the expert's number finds the
+        // slots of the same one
+        const unsigned long long below = lane == 0 ? 0ull : ~0ull >> (64 - lane);
+        for (int g = 0; g < N; g += 64) {
+            const bool live = g + lane < N;
+            const int e = live ? s_idx[g + lane] : 0;
+            unsigned long long same = __ballot(live);
+#pragma unroll
+            for (int b = 0; b < 6; b++) {
+                const unsigned long long m = __ballot((e >> b) & 1);
+                same &= ((e >> b) & 1) ? m : ~m;
+            }
+            const int rank = __popcll(same & below);
+            int at = 0;
+            if (live) at = s_next[e] + rank;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            if (live) {
+                if (rank == 0) s_next[e] = at + __popcll(same);
+                s_pos[g + lane] = at;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        const int cnt = s_next[lane];  // 0 for lanes >= E
+        int inc = cnt;
+#pragma unroll
+        for (int dlt = 1; dlt < 64; dlt <<= 1) {
+            const int v = __shfl_up(inc, dlt, 64);
+            if (lane >= dlt) inc += v;
+        }
+        __builtin_amdgcn_wave_barrier();
+        s_next[lane] = inc - cnt;
+        if (lane < f.E) {
+            f.counts[lane] = cnt;
+            f.offsets[lane] = inc - cnt;
+        }
+        if (lane == f.E - 1) f.offsets[f.E] = inc;
+    }
+    __syncthreads();
+    for (int p = threadIdx.x; p < N; p += blockDim.x) {
+        const int pos = s_next[s_idx[p]] + s_pos[p];
+        f.perm[pos] = p;
+        f.inv_perm[p] = pos;
+    }
 }
 
 int moe_i8_front_launch(const I8Front& f, moe_dtype_t x_dtype, hipStream_t s) {
     auto* kernel = x_dtype == MOE_BF16 ? i8_front_kernel<true> : i8_front_kernel<false>;
-    const int threads = f.x ? i8_row_threads(f.d / 4) : 256;
-    hipLaunchKernelGGL(kernel, dim3(f.x ? f.T + 1 : 1), dim3(threads < 256 ? 256 : threads), 0, s, f);
+    // a wave routes a token at a time
+    int threads = f.x ? i8_row_threads(f.d / 4) : 64;
+    const int waves = f.T < 4 ? 4 : f.T < 16 ? f.T : 16;
+    threads = threads < 64 * waves ? 64 * waves : threads;
+    hipLaunchKernelGGL(kernel, dim3(f.x ? f.T + 1 : 1), dim3(threads), 0, s, f);
     return moe_launch_status();
 }
 

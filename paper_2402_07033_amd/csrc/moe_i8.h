@@ -122,6 +122,7 @@ struct I8Product {
     unsigned* ytop;          // [N][C/16] or null; gated, STREAM: the bits of the largest magnitude of 16 channels of a row
 };
 int moe_i8_stream_launch(const I8Product& p, hipStream_t s);
+bool moe_i8_streams(const I8Product& p, int NR);  // do loads of the matrices (NR fragment rows each) go past the caches?
 int moe_i8_product_launch(const I8Product& p, int path, hipStream_t s);  // path: as moe_i8_auto_path names it
 bool moe_i8_product_supported(int N, int E, int K, int C);
 

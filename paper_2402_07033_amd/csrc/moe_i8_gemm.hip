@@ -78,7 +78,7 @@ __device__ __forceinline__ bool i8_find_tile(const I8GemmArgs& a, int lane, I8Ti
     } while (0)
 
 // WT x WF waves, RB blocks of 16 rows and FB fragment rows of w each.
-template <int WT, int WF, int FB, int NS, int RB, bool PACKED, bool GATED>
+template <int WT, int WF, int FB, int NS, int RB, bool PACKED, bool GATED, bool ONCE>
 __device__ __forceinline__ void i8_gemm_tile(const I8GemmArgs& a, const I8Tile& ti, int lane, int wave, unsigned char* smem) {
     constexpr int NW = WT * WF, XF = WT * RB, WFR = WF * FB;
     constexpr int XL = (XF + NW - 1) / NW, WL = (WFR + NW - 1) / NW;  // requests of a wave and step
@@ -123,7 +123,7 @@ __device__ __forceinline__ void i8_gemm_tile(const I8GemmArgs& a, const I8Tile& 
         for (int i = 0; i < WL; i++) {
             __builtin_amdgcn_global_load_lds(
                 (const __attribute__((address_space(1))) void*)(wp[i] + (PACKED ? (size_t)kc * 1024 : (size_t)at)),
-                (__attribute__((address_space(3))) void*)(smem + slot * STAGE + (i * NW + wave) * 1024), 16, 0, 0);
+                (__attribute__((address_space(3))) void*)(smem + slot * STAGE + (i * NW + wave) * 1024), 16, 0, ONCE ? 2 : 0);
         }
 #pragma unroll
         for (int i = 0; i < XL; i++) {
@@ -205,14 +205,14 @@ __device__ __forceinline__ void i8_gemm_tile(const I8GemmArgs& a, const I8Tile& 
     }
 }
 
-template <int WT, int WF, int FB, int NS, int RBM, bool PACKED, bool GATED>
+template <int WT, int WF, int FB, int NS, int RBM, bool PACKED, bool GATED, bool ONCE>
 __global__ __launch_bounds__(64 * WT * WF, WT * WF == 8 ? 2 : 2) void i8_gemm_kernel(I8GemmArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     I8Tile ti;
     if (!i8_find_tile<16 * WT, RBM>(a, lane, ti)) return;
-#define I8_TILE(n) if (ti.nblk == n) i8_gemm_tile<WT, WF, FB, NS, n, PACKED, GATED>(a, ti, lane, wave, smem)
+#define I8_TILE(n) if (ti.nblk == n) i8_gemm_tile<WT, WF, FB, NS, n, PACKED, GATED, ONCE>(a, ti, lane, wave, smem)
     I8_TILE(1);
     else I8_TILE(2);
     if constexpr (RBM >= 4) {
@@ -241,12 +241,12 @@ bool moe_i8_product_supported(int N, int E, int K, int C) {
     return K <= I8_MAX_K && ((long long)i8_tiles(N, E, 64) + 1) * ((2ll * C + 15) / 16 / 16 + 1) < (1ll << 28);
 }
 
-template <int WT, int WF, int FB, int NS, int RBM, bool PACKED, bool GATED>
+template <int WT, int WF, int FB, int NS, int RBM, bool PACKED, bool GATED, bool ONCE>
 static int i8_gemm_go(I8GemmArgs& a, hipStream_t s) {
     a.FT = (a.NR + WF * FB - 1) / (WF * FB);
     const size_t grid = (i8_tiles(a.p.N, a.p.E, 16 * WT * RBM) * a.FT + 7) / 8 * 8;
     constexpr int lds = NS * (WT * RBM + WF * FB) * 1024;
-    auto* kernel = i8_gemm_kernel<WT, WF, FB, NS, RBM, PACKED, GATED>;
+    auto* kernel = i8_gemm_kernel<WT, WF, FB, NS, RBM, PACKED, GATED, ONCE>;
     if (lds > 65536) {
         static std::atomic<bool> ready[MOE_MAX_DEVICES];  // one-time permission for more than 64 KiB of LDS
         const int dev = moe_current_device();
@@ -277,12 +277,21 @@ static I8Shape i8_shape(int N, int E, int NR) {
     return fills(128, 128) ? I8Shape{128, 128} : I8Shape{32, 128};
 }
 
-template <bool PACKED, bool GATED>
+// ONCE: matrices that most tiles read alone go past the caches (a plain read streams at 6.9 TB/s that way, at 6.0 otherwise).
+template <bool PACKED, bool GATED, bool ONCE>
 static int i8_gemm_pick(I8GemmArgs& a, hipStream_t s) {
     const int rows = i8_shape(a.p.N, a.p.E, a.NR).rows;
-    if (rows == 32) return i8_gemm_go<1, 4, 2, 4, 2, PACKED, GATED>(a, s);
-    if (rows == 128) return i8_gemm_go<2, 2, 4, 4, 4, PACKED, GATED>(a, s);
-    return i8_gemm_go<2, 4, 4, 3, 8, PACKED, GATED>(a, s);
+    if (rows == 32) return i8_gemm_go<1, 4, 2, 4, 2, PACKED, GATED, ONCE>(a, s);
+    if (rows == 128) return i8_gemm_go<2, 2, 4, 4, 4, PACKED, GATED, ONCE>(a, s);
+    return i8_gemm_go<2, 4, 4, 3, 8, PACKED, GATED, false>(a, s);
+}
+
+// Are the matrices in use too large for the last-level cache to hold from one call to the next?  Then loads past it are faster:
+// 128 x 128 tiles, first projection of 8 experts of 24 rows (d 4096, f 14336) 156 -> 147 us, the second 83 -> 72; 64 experts of 28
+// rows (d 2048, f 1408) 70 -> 66; but one 4096 x 4096 matrix, which stays, 64 rows 19 -> 23.
+bool moe_i8_streams(const I8Product& p, int NR) {
+    const size_t used = p.N < p.E ? p.N : p.E;
+    return used * NR * 16 * p.K > ((size_t)96 << 20);
 }
 
 int moe_i8_product_launch(const I8Product& p, int path, hipStream_t s) {
@@ -291,8 +300,10 @@ int moe_i8_product_launch(const I8Product& p, int path, hipStream_t s) {
     a.p = p;
     a.NR = p.gated ? 2 * (p.C / 16) : (p.C + 15) / 16;
     a.KS = i8_frags(p.K);
-    if (p.gated) return i8_gemm_pick<true, true>(a, s);
-    return p.packed ? i8_gemm_pick<true, false>(a, s) : i8_gemm_pick<false, false>(a, s);
+    const bool once = moe_i8_streams(p, a.NR) && p.N <= 128 * (p.N < p.E ? p.N : p.E);
+    if (p.gated) return once ? i8_gemm_pick<true, true, true>(a, s) : i8_gemm_pick<true, true, false>(a, s);
+    if (p.packed) return once ? i8_gemm_pick<true, false, true>(a, s) : i8_gemm_pick<true, false, false>(a, s);
+    return once ? i8_gemm_pick<false, false, true>(a, s) : i8_gemm_pick<false, false, false>(a, s);
 }
 
 // ---- the expert FFN: rows to 8 bits, w1 and w3 with silu*mul, h to 8 bits, w2 ----

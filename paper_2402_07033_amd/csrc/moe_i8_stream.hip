@@ -19,7 +19,7 @@ struct I8StreamArgs {
     int FG;   // groups of FB fragment rows
 };
 
-template <int FB, int NW, bool PACKED, bool GATED>
+template <int FB, int NW, bool PACKED, bool GATED, bool ONCE>
 __global__ __launch_bounds__(64 * NW) void i8_stream_kernel(I8StreamArgs a) {
     constexpr int U = I8S_U;
     __shared__ i32x4_t s_sum[NW][FB][64];
@@ -67,7 +67,10 @@ __global__ __launch_bounds__(64 * NW) void i8_stream_kernel(I8StreamArgs a) {
             at = at < K ? at : K - 16;  // (times x's zeros)
 #pragma unroll
             for (int r = 0; r < FB; r++)
-                w[u][r] = __builtin_nontemporal_load((const i32x4_t*)(wp[r] + (PACKED ? (size_t)(k0 + u) * 1024 : (size_t)at)));
+            {
+                const i32x4_t* q = (const i32x4_t*)(wp[r] + (PACKED ? (size_t)(k0 + u) * 1024 : (size_t)at));
+                w[u][r] = ONCE ? __builtin_nontemporal_load(q) : *q;
+            }
         }
 #pragma unroll
         for (int u = 0; u < U; u++) {
@@ -250,9 +253,13 @@ template <int NW, bool PACKED, bool GATED>
 static void i8_stream_go(I8StreamArgs& a, size_t tiles, hipStream_t s) {
     constexpr int FB = 2;
     a.FG = (a.NR + FB - 1) / FB;
-    hipLaunchKernelGGL((i8_stream_kernel<FB, NW, PACKED, GATED>), dim3((unsigned)(tiles * a.FG)), dim3(64 * NW), 0, s, a);
+    auto* kernel = moe_i8_streams(a.p, a.NR) ? i8_stream_kernel<FB, NW, PACKED, GATED, true> : i8_stream_kernel<FB, NW, PACKED, GATED, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles * a.FG)), dim3(64 * NW), 0, s, a);
 }
 
+// Waves of a workgroup by the reduction, which they share.  us with (channels, waves) (32, 4) / (32, 8) / (16, 8) / (16, 16): second
+// projection of one token's two experts (f 14336) 22.3 / 20.2 / 20.4 / 21.4, of 39 experts with f 1408 23.5 / 29.1 / 30.3 / 60.4; first
+// projections (32, 4) / (32, 8) / (64, 8): one token (d 4096) 38.1 / 39.7 / 45.5, 39 experts (d 2048) 40.1 / 47.1 / 41.8.
 template <bool PACKED, bool GATED>
 static void i8_stream_pick(I8StreamArgs& a, size_t tiles, hipStream_t s) {
     if (a.KS > 64) i8_stream_go<8, PACKED, GATED>(a, tiles, s);

@@ -402,10 +402,24 @@ def _opt(t: Optional[torch.Tensor], dtype, dev: int, n: int, what: str):
     return _arg(t, dtype, dev, what)
 
 
+# A layer of a few tokens allocates seven outputs: 0.75 us each by this function, 1.4 .. 1.8 by new_empty.
+_emptyStrided = getattr(getattr(getattr(torch._C, "_dynamo", None), "guards", None), "_empty_strided_cuda", None)
+
+
+def _new(shape, dtype, like: torch.Tensor) -> torch.Tensor:
+    """A new tensor on the current device, which is `like`'s."""
+    if _emptyStrided is None or len(shape) > 2:
+        return like.new_empty(shape, dtype=dtype)
+    if len(shape) == 1:
+        return _emptyStrided((shape[0],), (1,), dtype)
+    rows, width = shape
+    return _emptyStrided((rows, width), (width, 1), dtype)
+
+
 def _out(t, shape, dtype, like: torch.Tensor, what: str):
     """The caller's output tensor, or a new one where `like` is."""
     if t is None:
-        return like.new_empty(shape, dtype=dtype)
+        return _new(shape, dtype, like)
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{what}: expected {list(shape)}")
     return t
@@ -925,27 +939,27 @@ def moe_layer_int8(W: PackedWeights, x, logits: torch.Tensor, k: int, idx=None, 
         raise ValueError(f"expected x [T,{d}] and logits [T,{W.E}]")
     if not 1 <= k <= min(E, _MAX_K) or N >= _MAX_N:
         raise MoeError(_INVALID_ARG, "moe_layer_int8")  # before N rows are allocated
-    i32 = torch.int32
-    if idx is None:
-        idx = logits.new_empty((T, k), dtype=i32)
-    if weights is None:
-        weights = logits.new_empty((T, k))
-    if out is None:
-        out = tuple(logits.new_empty(n, dtype=i32) for n in (E, E + 1, N, N))
-    counts, offsets, perm, inv_perm = out[:4]
+    i32, f32 = torch.int32, torch.float32
     if workspace is None:
         workspace = _scratch(moe_layer_int8_workspace(T, E, k, d, W.f), x.device, stream)
-    if y is None:
-        y = x.new_empty((T, d), dtype=dtype if dtype is not None else torch.bfloat16 if scales is not None else x.dtype)
-    p = []
-    for t, n, dt, what in ((idx, N, i32, "idx"), (weights, N, torch.float32, "weights"), (counts, E, i32, "counts"),
-                           (offsets, E + 1, i32, "offsets"), (perm, N, i32, "perm"), (inv_perm, N, i32, "inv_perm"),
-                           (workspace, 0, workspace.dtype, "workspace"), (y, T * d, y.dtype, "y")):
-        if t.numel() < n:
-            raise ValueError(f"{what}: {t.numel()} elements, {n} are written")
-        p.append(_arg(t, dt, dev, what))
+    ydt = y.dtype if y is not None else dtype if dtype is not None else torch.bfloat16 if scales is not None else x.dtype
+    counts, offsets, perm, inv_perm = out[:4] if out is not None else (None,) * 4
+    p, made = [], []
+    for t, shape, n, dt, what in ((idx, (T, k), N, i32, "idx"), (weights, (T, k), N, f32, "weights"), (counts, (E,), E, i32, "counts"),
+                                  (offsets, (E + 1,), E + 1, i32, "offsets"), (perm, (N,), N, i32, "perm"),
+                                  (inv_perm, (N,), N, i32, "inv_perm"), (workspace, None, 0, workspace.dtype, "workspace"),
+                                  (y, (T, d), T * d, ydt, "y")):
+        if t is None:
+            t = _new(shape, dt, logits)
+            p.append(t.data_ptr())
+        else:
+            if t.numel() < n:
+                raise ValueError(f"{what}: {t.numel()} elements, {n} are written")
+            p.append(_arg(t, dt, dev, what))
+        made.append(t)
+    idx, weights, counts, offsets, perm, inv_perm, workspace, y = made
     _check(lib().moe_layer_int8(W.handle, xp, xdt, sp, lp, T, k, *p[:7], workspace.numel() * workspace.element_size(), p[7],
-                                _float_type(y.dtype), _stream(stream)), "moe_layer_int8")
+                                _float_type(ydt), _stream(stream)), "moe_layer_int8")
     return dict(idx=idx, w=weights, counts=counts, offsets=offsets, perm=perm, inv_perm=inv_perm, y=y)
 
 
@@ -978,10 +992,12 @@ def moe_block_norm(x: torch.Tensor, y=None, norm_after: bool = False, gain_after
         cp, sp = _arg(codes, torch.int8, dev, "codes"), _arg(scales, f32, dev, "scales")
     elif codes is not None or scales is not None:
         raise ValueError("codes and scales are outputs of int8=True")
-    _check(lib().moe_block_norm(xp, xdt, yp, ydt, T, d, norm_after, _opt(gain_after, f32, dev, d, "gain_after"),
-                                _opt(gate, f32, dev, d, "gate"), _opt(row_gate, f32, dev, T, "row_gate"), residual_scale,
-                                _opt(gain_before, f32, dev, d, "gain_before"), eps, xop, hp, hdt, cp, sp, _stream(stream)),
-           "moe_block_norm")
+    ga = None if gain_after is None else _opt(gain_after, f32, dev, d, "gain_after")
+    gp = None if gate is None else _opt(gate, f32, dev, d, "gate")
+    rp = None if row_gate is None else _opt(row_gate, f32, dev, T, "row_gate")
+    gb = None if gain_before is None else _opt(gain_before, f32, dev, d, "gain_before")
+    _check(lib().moe_block_norm(xp, xdt, yp, ydt, T, d, norm_after, ga, gp, rp, residual_scale, gb, eps, xop, hp, hdt, cp, sp,
+                                _stream(stream)), "moe_block_norm")
     return dict(x=x if x_out is None else x_out, h=h, codes=codes, scales=scales)
 
 

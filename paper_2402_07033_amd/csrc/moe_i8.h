@@ -62,7 +62,8 @@ struct I8Coder {
 #pragma unroll
             for (int i = 0; i < 4; i++) q[i] = (unsigned)exact(u[i]);
         }
-        return (q[0] & 255u) | ((q[1] & 255u) << 8) | ((q[2] & 255u) << 16) | (q[3] << 24);
+        // (the low bytes of the four)
+        return __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0400u) | __builtin_amdgcn_perm(q[3], q[2], 0x04000c0cu);
     }
 };
 

@@ -205,13 +205,17 @@ int moe_i8_rows_back_launch(const int8_t* codes, const float* scales, int T, int
 // magnitudes and the codes: such matrices are read once.  Longer reductions are read again, from the last-level cache.  The
 // two halves of a 128-byte line go to workgroups of one XCD.  Codes leave as 16 bytes a channel, 128 bytes and more of a
 // channel side by side.
+// Threads and bytes of a row, 8 x 4096 x 14336 in bf16 / in fp32, us: 512 and 64 454 / 701, 512 and 32 475 / 807, 1024 and 64 534 / 660,
+// 1024 and 32 506 / 723 (floor 275 / 458).  Scales and codes in two launches, in groups that the last-level cache holds: 600.
+// What bounds it is the access to narrow strips of long rows: a launch that only reads them for the scales gets 3.5 TB/s.
 #define I8_QT 512
-#define I8_SEG 32
+#define I8_SEG 64
+#define I8_SIDE (128 / I8_SEG)  // strips of a line, on one XCD
 template <bool BF16, int V>
 struct I8Quant {
     static constexpr int LC = I8_SEG / (V * (BF16 ? 2 : 4));  // lanes across the channels
     static constexpr int RG = I8_QT / LC;                 // groups of 16 indices of a round
-    static constexpr int HOLD = BF16 && V == 4 ? 2 : BF16 ? 4 : 2;
+    static constexpr int HOLD = BF16 && V < 4 ? 4 : 2;
     static constexpr int BYTES = V * (BF16 ? 2 : 4);      // of a thread's channels in a row
     typedef std::conditional_t<BYTES == 8, uint2, std::conditional_t<BYTES == 4, unsigned, uint16_t>> Word;
     struct Elems {
@@ -240,7 +244,7 @@ __global__ __launch_bounds__(I8_QT) void i8_quantize_kernel(const void* __restri
     constexpr int LC = Q::LC, HOLD = Q::HOLD;
     __shared__ unsigned s_top[I8_QT / 64][LC * V];
     const size_t e = blockIdx.y;
-    const int strip = (blockIdx.x & ~31) + (blockIdx.x & 7) * 4 + ((blockIdx.x >> 3) & 3);
+    const int strip = (blockIdx.x & ~(8 * I8_SIDE - 1)) + (blockIdx.x & 7) * I8_SIDE + ((blockIdx.x >> 3) & (I8_SIDE - 1));
     if (strip >= strips) return;
     const int cl = threadIdx.x % LC, rg0 = threadIdx.x / LC, wave = threadIdx.x >> 6;
     const int c0 = (strip * LC + cl) * V;
@@ -318,7 +322,7 @@ int moe_i8_quantize_launch(const void* w, moe_dtype_t w_dtype, int E, int K, int
     const int wide = I8_SEG / (bf16 ? 2 : 4), strips = (C + wide - 1) / wide;
     auto* kernel = bf16 ? (V == 4 ? i8_quantize_kernel<true, 4> : V == 2 ? i8_quantize_kernel<true, 2> : i8_quantize_kernel<true, 1>)
                         : (V == 2 ? i8_quantize_kernel<false, 2> : i8_quantize_kernel<false, 1>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(strips + 31) & ~31u, (unsigned)E), dim3(I8_QT), 0, s, w, K, C, strips, codes, scales);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(strips + 8 * I8_SIDE - 1) & ~(8u * I8_SIDE - 1), (unsigned)E), dim3(I8_QT), 0, s, w, K, C, strips, codes, scales);
     return moe_launch_status();
 }
 

@@ -307,7 +307,8 @@ int moe_int8_matmul(const int8_t* x_codes, const float* x_scales, int M, const i
         ranges_overlap(y, yb, w_codes, (size_t)E * C * K) || ranges_overlap(y, yb, w_scales, (size_t)E * C * 4) ||
         ranges_overlap(y, yb, offsets, (size_t)(E + 1) * 4))
         return MOE_ERR_INVALID_ARG;
-    if (!moe_i8_product_supported(M, E, K, C)) return MOE_ERR_UNSUPPORTED;
+    const int path = moe_i8_auto_path(M, E);
+    if (!moe_i8_product_supported(M, E, K, C, false, path)) return MOE_ERR_UNSUPPORTED;
     I8Product p = {};
     p.x = x_codes;
     p.xs = x_scales;
@@ -321,7 +322,7 @@ int moe_int8_matmul(const int8_t* x_codes, const float* x_scales, int M, const i
     p.ws = w_scales;
     p.y = y;
     p.y_bf16 = y_dtype == MOE_BF16;
-    return moe_i8_product_launch(p, moe_i8_auto_path(M, E), (hipStream_t)stream);
+    return moe_i8_product_launch(p, path, (hipStream_t)stream);
 }
 
 int moe_weights_pack_int8(const int8_t* w1_codes, const float* w1_scales, const int8_t* w3_codes, const float* w3_scales,
@@ -374,6 +375,7 @@ int moe_layer_int8(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, c
         if (ranges_overlap(logits, (size_t)T * E * 4, o.p, o.bytes) || ranges_overlap(x, xb, o.p, o.bytes) ||
             ranges_overlap(x_scales, (size_t)T * 4, o.p, o.bytes))
             return MOE_ERR_INVALID_ARG;
+    if (W->device != moe_current_device()) return MOE_ERR_INVALID_ARG;
 
     I8Front fr = {};
     fr.logits = logits;

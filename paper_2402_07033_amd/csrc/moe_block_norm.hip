@@ -190,6 +190,8 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(MoeBlockNorm a) {
     }
 }
 
+#define BN_LAUNCH_ROWS (1 << 20)
+
 // Two chunks a thread: a row's requests are all out at once and its passes short.  4096 rows of 4096 (fp32, bf16 -> fp32,
 // bf16) with 1 / 2 / 4 / 8 chunks a thread (1024 .. 128 threads) 67.7 / 50.7 / 54.7 / 57.5 us, 1000 rows (8-bit codes too) 21.8 /
 // 16.4 / 15.2 / 16.8, 301 of 2048 6.7 / 6.0 / 7.9 / 10.8, one 5.6 / 4.8 / 5.1 / 6.9; 2000 of 8192 - / 58.4 / 55.7 / 52.8.
@@ -198,6 +200,21 @@ int moe_block_norm_launch(const MoeBlockNorm& a, hipStream_t s) {
     const bool held = d4 <= 1024 * V;
     const int waves = held ? (d4 + 64 * V - 1) / (64 * V) : 16;
     auto* kernel = !held ? block_norm_kernel<1, false> : V == 2 ? block_norm_kernel<2, true> : block_norm_kernel<4, true>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)a.T), dim3(64 * waves), 0, s, a);
+    // (a launch has fewer than 2^32 threads)
+    MoeBlockNorm part = a;
+    const size_t xb = a.x_bf16 ? 2 : 4, yb = a.y_bf16 ? 2 : 4, hb = a.h_bf16 ? 2 : 4;
+    for (int t = 0; t < a.T; t += part.T) {
+        const size_t at = (size_t)t * a.d;
+        auto step = [&](const void* p, size_t bytes) { return p ? (const char*)p + bytes : nullptr; };
+        part.T = a.T - t < BN_LAUNCH_ROWS ? a.T - t : BN_LAUNCH_ROWS;
+        part.x = step(a.x, at * xb);
+        part.y = step(a.y, at * yb);
+        part.row_gate = (const float*)step(a.row_gate, (size_t)t * 4);
+        part.x_out = (void*)step(a.x_out, at * xb);
+        part.h = (void*)step(a.h, at * hb);
+        part.codes = (unsigned*)step(a.codes, at);
+        part.scales = (float*)step(a.scales, (size_t)t * 4);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)part.T), dim3(64 * waves), 0, s, part);
+    }
     return moe_launch_status();
 }

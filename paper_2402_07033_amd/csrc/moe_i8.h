@@ -125,7 +125,7 @@ struct I8Product {
 int moe_i8_stream_launch(const I8Product& p, hipStream_t s);
 bool moe_i8_streams(const I8Product& p, int NR);  // do loads of the matrices (NR fragment rows each) go past the caches?
 int moe_i8_product_launch(const I8Product& p, int path, hipStream_t s);  // path: as moe_i8_auto_path names it
-bool moe_i8_product_supported(int N, int E, int K, int C);
+bool moe_i8_product_supported(int N, int E, int K, int C, bool gated, int path);
 
 int moe_i8_auto_path(int N, int E);  // MOE_FFN_STREAM or MOE_FFN_GROUPED
 

@@ -237,10 +237,6 @@ static inline size_t i8_tiles(int N, int E, int rows) {
     return ((size_t)N + (size_t)(rows - 1) * used) / rows;
 }
 
-bool moe_i8_product_supported(int N, int E, int K, int C) {
-    return K <= I8_MAX_K && ((long long)i8_tiles(N, E, 64) + 1) * ((2ll * C + 15) / 16 / 16 + 1) < (1ll << 28);
-}
-
 template <int WT, int WF, int FB, int NS, int RBM, bool PACKED, bool GATED, bool ONCE>
 static int i8_gemm_go(I8GemmArgs& a, hipStream_t s) {
     a.FT = (a.NR + WF * FB - 1) / (WF * FB);
@@ -275,6 +271,15 @@ static I8Shape i8_shape(int N, int E, int NR) {
     };
     if (N > 128 * used && fills(256, 256)) return {256, 256};
     return fills(128, 128) ? I8Shape{128, 128} : I8Shape{32, 128};
+}
+
+// A launch has fewer than 2^32 threads.
+bool moe_i8_product_supported(int N, int E, int K, int C, bool gated, int path) {
+    if (K > I8_MAX_K) return false;
+    const int NR = gated ? 2 * (C / 16) : (C + 15) / 16;
+    if (path == MOE_FFN_STREAM) return i8_tiles(N, E, 16) * ((NR + 1) / 2) < ((size_t)1 << 32) / 512;
+    const I8Shape sh = i8_shape(N, E, NR);
+    return (i8_tiles(N, E, sh.rows) * ((NR * 16 + sh.channels - 1) / sh.channels) + 8) < ((size_t)1 << 32) / 512;
 }
 
 // ONCE: matrices that most tiles read alone go past the caches (a plain read streams at 6.9 TB/s that way, at 6.0 otherwise).
@@ -342,7 +347,8 @@ int moe_i8_auto_path(int N, int E) {
     return N <= (E == 1 ? 32 : 8 * used) ? MOE_FFN_STREAM : MOE_FFN_GROUPED;
 }
 bool moe_i8_ffn_supported(int path, int N, int E, int d, int f) {
-    return (path == MOE_FFN_GROUPED || path == MOE_FFN_STREAM) && moe_i8_product_supported(N, E, d, f) && moe_i8_product_supported(N, E, f, d);
+    return (path == MOE_FFN_GROUPED || path == MOE_FFN_STREAM) && moe_i8_product_supported(N, E, d, f, true, path) &&
+           moe_i8_product_supported(N, E, f, d, false, path);
 }
 int moe_i8_ffn_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan) {
     if (!moe_i8_ffn_supported(plan->path, N, E, d, f)) return MOE_ERR_UNSUPPORTED;

@@ -38,6 +38,8 @@ CASES = [
     (2304, 2048, [150, 140, 160, 133] * 8, 192),           # the tile of 192 rows
     (2048, 2048, [240, 256, 255, 233] * 4, 192),
     (2048, 2048, [6500], 256),                             # one expert
+    (4096, 4096, [2200, 2000], 256),                       # left-over tiles of both projections cut along the reduction
+    (4096, 4096, [300, 0, 1900, 77, 1999, 1], 256),
 ]
 
 
@@ -80,3 +82,47 @@ def test_layer(moe, T, k):
     small = torch.empty(moe.moe_layer_int8_workspace(T, E, k, d, f) - 1, dtype=torch.uint8, device="cuda")
     with pytest.raises(moe.MoeError):
         moe.moe_layer_int8(W, x, logits, k, workspace=small)
+
+
+# ---- more rows than a launch takes, and offsets past 32 bits: the last rows are what a call on them alone gives ----
+
+def test_product_past_4_gib(moe):
+    M, K, C = 1100000, 4096, 64
+    g = torch.Generator("cuda").manual_seed(1)
+    x = torch.empty((M, K), dtype=torch.int8, device="cuda")
+    x[:2000] = torch.randint(-127, 128, (2000, K), dtype=torch.int8, device="cuda", generator=g)
+    x[2000:-2000] = 1
+    x[-2000:] = torch.randint(-127, 128, (2000, K), dtype=torch.int8, device="cuda", generator=g)
+    xs = torch.rand(M, device="cuda", generator=g)
+    w = (torch.randint(-127, 128, (1, C, K), dtype=torch.int8, device="cuda", generator=g), torch.rand((1, C), device="cuda", generator=g))
+    y = moe.moe_int8_matmul((x, xs), w, dtype=F32)
+    for part in (slice(0, 2000), slice(M - 2000, M)):
+        assert torch.equal(y[part], moe.moe_int8_matmul((x[part].clone(), xs[part].clone()), w, dtype=F32))
+
+
+def test_experts_past_4_gib(moe):
+    N, d, f = 80000, 512, 14336  # h: 4.6 GB
+    W = _handle(moe, 1, d, f, 3)
+    x = torch.randn((N, d), device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+    y = moe.moe_expert_ffn(W, x, _dev(np.array([0, N], dtype=np.int32)))
+    for part in (slice(0, 40), slice(N - 700, N)):
+        n = part.stop - part.start
+        assert torch.equal(y[part], moe.moe_expert_ffn(W, x[part].clone(), _dev(np.array([0, n], dtype=np.int32))))
+
+
+def test_rows_past_a_launch(moe):
+    T, d = (1 << 20) + 37, 64
+    g = torch.Generator("cuda").manual_seed(4)
+    x, y = (torch.randn((T, d), device="cuda", generator=g) for _ in range(2))
+    gate = torch.rand(T, device="cuda", generator=g)
+    whole = moe.moe_block_norm(x, y, norm_after=True, row_gate=gate, int8=True, h_dtype=BF16)
+    codes, scales = moe.moe_int8_quantize_rows(x)
+    back = moe.moe_int8_dequantize_rows(codes, scales, dtype=F32)
+    part = slice((1 << 20) - 5, T)
+    px, py, pg = x[part].clone(), y[part].clone(), gate[part].clone()
+    alone = moe.moe_block_norm(px, py, norm_after=True, row_gate=pg, int8=True, h_dtype=BF16)
+    for n in ("x", "h", "codes", "scales"):
+        assert torch.equal(whole[n][part], alone[n])
+    q, s = moe.moe_int8_quantize_rows(px)
+    assert torch.equal(codes[part], q) and torch.equal(scales[part], s)
+    assert torch.equal(back[part], moe.moe_int8_dequantize_rows(q, s, dtype=F32))

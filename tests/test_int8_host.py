@@ -125,6 +125,10 @@ def test_other_calls_on_a_handle(L, at):  # noqa: F811
     assert L.moe_expert_ffn_plan(4096, 8, 4096, 14336, INT8, 0, C.byref(plan)) == 0 and plan.path == 2 and plan.n_parts == 1
     assert L.moe_expert_ffn_plan(4096, 8, 4096, 14336, INT8, 3, C.byref(plan)) == UNSUPPORTED
     assert L.moe_expert_ffn_plan(4096, 8, 1 << 18, 14336, INT8, 0, C.byref(plan)) == UNSUPPORTED
+    # more threads than a launch may have
+    assert L.moe_expert_ffn_plan((1 << 24) - 1, 8, 4096, 14336, INT8, 1, C.byref(plan)) == UNSUPPORTED
+    assert L.moe_expert_ffn_plan((1 << 24) - 1, 8, 1 << 17, 1 << 17, INT8, 0, C.byref(plan)) == UNSUPPORTED
+    assert L.moe_expert_ffn_plan(1 << 20, 8, 4096, 14336, INT8, 0, C.byref(plan)) == 0 and plan.up_tile_rows == 256
     assert L.moe_expert_ffn_workspace(1, 1, 1 << 18, 64, F32) > 0   # (no 8-bit handle has such rows)
 
 

@@ -203,13 +203,13 @@ size_t moe_expert_ffn_workspace(int N, int E, int d, int f, moe_dtype_t act_dtyp
  *     yg[i,:] = ( silu(xg[i,:] . w1_e) * (xg[i,:] . w3_e) ) . w2_e
  * with fp32 accumulation.  offsets is read on the device: the call never
  * learns the per-expert sizes on the host.
- *   W         packed handle (bf16, fp32 or MXFP4 weights)
+ *   W         packed handle (bf16, fp32, MXFP4 or 8-bit weights)
  *   xg        [N,d] of act_dtype (fp32 weights need fp32 activations)
  *   offsets   [E+1] int32 DEVICE, offsets[0] = 0, non-decreasing, offsets[E] = N
  *   workspace >= moe_expert_ffn_workspace(...) bytes, 256-byte aligned; contents
  *             are scratch (may be reused by the next call on the same stream)
  *   yg        [N,d] fp32 out
- * bf16-weight kernels multiply on the bf16 matrix cores (4-bit weights: above): fp32 activations are
+ * bf16-weight kernels multiply on the bf16 matrix cores (4-bit and 8-bit weights: above): fp32 activations are
  * split into bf16 high and low parts (STREAM path, ~2^-16 relative) or rounded
  * to bf16 (GROUPED, MID); the intermediate silu(a)*b is kept in fp32 (STREAM)
  * or bf16 (GROUPED, MID).  Every path adds its partial sums in a fixed order: the
@@ -268,7 +268,7 @@ size_t moe_expert_ffn_noalloc_max_bytes(void);
  *            count w1 and w3 columns together.  By the rows per expert, which only the device
  *            knows, the kernel may take tiles of 160 rows x 192..512 features instead:
  *            moe_expert_ffn_tiles says when.  (MXFP4 handles: the tiles of bf16 rows; fp32 rows take
- *            the second projection's for both.)
+ *            the second projection's for both.  8-bit handles: up to 192 or 256 rows x 256 features, whatever the counts.)
  * Returns MOE_ERR_UNSUPPORTED if a forced family cannot run the shape.
  */
 typedef struct {

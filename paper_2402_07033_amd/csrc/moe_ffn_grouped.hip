@@ -145,6 +145,7 @@ struct GroupedArgs {
     const float* bscale;
     const float* wscale;
     unsigned* top;
+    int KS_w;    // fragments of a weight row: KS, or fewer (the last steps' tokens are zeros, whatever weights they meet)
 };
 
 // s_waitcnt with only one counter constrained (gfx9 encoding: vmcnt = bits 3:0 and
@@ -407,7 +408,7 @@ __device__ __forceinline__ unsigned gg_h_off(int lane) {
 }
 
 #ifdef GG_INT8
-// Eight 32-bit values: where the lane's 16-byte store goes inside a tile of rows of C floats, or behind the descriptor.
+// Does the tile have fragment row j of this wave?
 template <int FRW, bool FLEX>
 __device__ __forceinline__ bool gg_int8_has(const TileInfo& ti, int wave, int j) {
     return !FLEX || wave + (j / 4) * 4 < ti.groups;
@@ -576,16 +577,18 @@ __device__ __forceinline__ void gg_gemm_body(const GroupedArgs& a, int NT, int t
     // per step) and the lane's 16 bytes of the fragment.  A: row j of this wave.  B: block 4v + wave
     // of the tile is request v of this wave; blocks past the tile's last one repeat it (every wave always has its requests, their products are never stored).  (Offsets
     // inside a tile: at most 32 rows of f/32 <= 32768 fragments, 1 GiB.)
-    const unsigned row_bytes = (unsigned)a.KS * 1024u;  // one fragment row / token block
+    const unsigned row_bytes = (unsigned)a.KS * 1024u;  // one token block
+    const int KS_w = GG_I8 ? a.KS_w : a.KS;
+    const unsigned w_row_bytes = (unsigned)KS_w * 1024u;  // one fragment row
     const unsigned voff = (unsigned)lane * 16u;
     // the lane's offset of a weight request: behind the descriptor, which returns zeros without a memory access,
     // for a group of rows that the tile does not have
     auto has = [&](const TileInfo& ti, int j) GG_INLINE -> bool { return !FLEX || wave + (j / 4) * 4 < ti.groups; };
     auto a_voff = [&](const TileInfo& ti, int j) GG_INLINE -> unsigned { return has(ti, j) ? voff : GG_RSRC_BYTES; };
-    auto a_row = [&](int j) GG_INLINE -> unsigned { return (unsigned)gg_wave_row<FRW, FLEX>(0, j) * row_bytes; };
+    auto a_row = [&](int j) GG_INLINE -> unsigned { return (unsigned)gg_wave_row<FRW, FLEX>(0, j) * w_row_bytes; };
     auto a_base = [&](const TileInfo& ti) GG_INLINE -> const char* {
         return (const char*)a.wfrag +
-               (((size_t)ti.si.e * a.FR + (size_t)ti.frow + gg_wave_row<FRW, FLEX>(wave, 0)) * a.KS + ti.k_lo) * 1024;
+               (((size_t)ti.si.e * a.FR + (size_t)ti.frow + gg_wave_row<FRW, FLEX>(wave, 0)) * KS_w + ti.k_lo) * 1024;
     };
     auto b_base = [&](const TileInfo& ti) GG_INLINE -> const char* {
         return (const char*)a.bfrag + ((size_t)(ti.si.bbase + ti.blk0) * a.KS + ti.k_lo) * 1024;

@@ -399,7 +399,8 @@ int moe_i8_pack_impl(const int8_t* const codes[3], const float* const scales[3],
         return MOE_ERR_HIP;
     }
     const size_t n = (size_t)E * d * f;
-    const size_t bytes[4] = {2 * n, n, (size_t)E * 2 * f * 4, (size_t)E * d * 4};
+    // (the persistent loop's steps come in fours and read up to three fragments behind the last, times zeros)
+    const size_t bytes[4] = {2 * n + 3 * 1024, n + 3 * 1024, (size_t)E * 2 * f * 4, (size_t)E * d * 4};
     void** dst[4] = {&W->w13, &W->w2, &W->s13, &W->s2};
     for (int i = 0; i < 4; i++) {
         if (hipMalloc(dst[i], bytes[i]) != hipSuccess) {

@@ -206,7 +206,7 @@ __device__ __forceinline__ void i8_gemm_tile(const I8GemmArgs& a, const I8Tile& 
 }
 
 template <int WT, int WF, int FB, int NS, int RBM, bool PACKED, bool GATED, bool ONCE>
-__global__ __launch_bounds__(64 * WT * WF, WT * WF == 8 ? 2 : 2) void i8_gemm_kernel(I8GemmArgs a) {
+__global__ __launch_bounds__(64 * WT * WF, 2) void i8_gemm_kernel(I8GemmArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

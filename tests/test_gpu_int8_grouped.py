@@ -40,6 +40,9 @@ CASES = [
     (2048, 2048, [6500], 256),                             # one expert
     (4096, 4096, [2200, 2000], 256),                       # left-over tiles of both projections cut along the reduction
     (4096, 4096, [300, 0, 1900, 77, 1999, 1], 256),
+    (2048, 1408, [370, 0, 400, 391, 383] * 8, 256),        # a reduction that is no multiple of 256: steps filled with zeros
+    (2304, 1152, [2900, 3100, 17, 1111], 256),
+    (3840, 4992, [1700, 1900], 256),
 ]
 
 

@@ -182,7 +182,7 @@ int moe_int8_matmul(const int8_t* x_codes, const float* x_scales, int M, const i
  * moe_layer and moe_layer_int8 below; the decode calls (moe_decode_layer, moe_decode_block) are unsupported.
  * Rows x and h = silu(a)*b are each brought to 8 bits with a scale per row; everything else is fp32.  A value of h
  * within fp32 rounding of a border between two codes may take either.
- * Rows that offsets do not cover are left as they were.
+ * Rows that offsets do not cover are left as they were.  The current device must be the handle's (MOE_ERR_INVALID_ARG).
  */
 int moe_weights_pack_int8(const int8_t* w1_codes, const float* w1_scales, const int8_t* w3_codes, const float* w3_scales,
                           const int8_t* w2_codes, const float* w2_scales, int E, int d, int f, moe_weights_t** out,
@@ -268,7 +268,8 @@ size_t moe_expert_ffn_noalloc_max_bytes(void);
  *            count w1 and w3 columns together.  By the rows per expert, which only the device
  *            knows, the kernel may take tiles of 160 rows x 192..512 features instead:
  *            moe_expert_ffn_tiles says when.  (MXFP4 handles: the tiles of bf16 rows; fp32 rows take
- *            the second projection's for both.  8-bit handles: up to 192 or 256 rows x 256 features, whatever the counts.)
+ *            the second projection's for both.
+ *            8-bit handles: the same tiles whatever the counts.)
  * Returns MOE_ERR_UNSUPPORTED if a forced family cannot run the shape.
  */
 typedef struct {
@@ -371,7 +372,8 @@ size_t moe_layer_mxfp4_workspace(int T, int E, int k, int d, int f);
  *     (as moe_int8_quantize_rows or moe_block_norm leave them)
  *   idx, weights, counts, offsets, perm, inv_perm: as moe_route / moe_permute, all written
  *   workspace >= moe_layer_int8_workspace(T, E, k, d, f) bytes, 256-byte aligned
- *   y [T,d] of y_dtype (fp32 or bf16) out.  No output and no byte of the workspace may overlap x, x_scales or logits.
+ *   y [T,d] of y_dtype (fp32 or bf16) out.  No output and no byte of the workspace may overlap x, x_scales, logits or
+ *   one another.
  * T == 0 writes counts and offsets only.  Logits that hold NaN: as moe_layer_mxfp4.
  */
 int moe_layer_int8(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, const float* x_scales, const float* logits,
@@ -385,7 +387,7 @@ size_t moe_layer_int8_workspace(int T, int E, int k, int d, int f);
  *     u[t,:]  = norm_after ? y[t,:] / sqrt(mean(y[t,:]^2) + eps) * gain_after : y[t,:]
  *     x'[t,:] = x[t,:] + residual_scale * row_gate[t] * gate * u[t,:]            (y NULL: x' = x)
  *     h[t,:]  = x'[t,:] / sqrt(mean(x'[t,:]^2) + eps) * gain_before
- * computed in 64 bits, every output rounded once from there (h from the x' before its rounding).
+ * computed in 64 bits, every output rounded from there, bf16 ones by way of fp32 (h from the x' before its rounding).
  *   x [T,d] of x_dtype, y [T,d] of y_dtype (fp32 or bf16), y or NULL (then norm_after 0 and no gain_after, gates or x_out
  *   needed); gain_after [d], gain_before [d], gate [d], row_gate [T]: fp32, each or NULL for ones
  *   x_out [T,d] of x_dtype out or NULL; may be x itself

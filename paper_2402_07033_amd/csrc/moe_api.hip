@@ -89,6 +89,7 @@ static int ffn_args(const moe_weights_t* W, const void* xg, moe_dtype_t act_dtyp
     } else if (W->dtype == MOE_INT8) {
         if (path == MOE_FFN_AUTO) path = moe_i8_auto_path(N, W->E);
         served = moe_i8_ffn_supported(path, N, W->E, W->d, W->f);
+        if (served && W->device != moe_current_device()) return MOE_ERR_INVALID_ARG;
     } else {
         if (path == MOE_FFN_AUTO) path = moe_ffn_auto_path(N, W->E, W->d, W->f);
         served = path == MOE_FFN_STREAM ? moe_ffn_stream_serves(N, W->E, W->d, W->f)
@@ -371,10 +372,15 @@ int moe_layer_int8(const moe_weights_t* W, const void* x, moe_dtype_t x_dtype, c
     const struct { const void* p; size_t bytes; } out[8] = {
         {idx, n4}, {weights, n4}, {counts, e4}, {offsets, e4 + 4}, {perm, n4}, {inv_perm, n4},
         {y, float_bytes(y_dtype, td)}, {workspace, workspace_bytes}};
-    for (const auto& o : out)
-        if (ranges_overlap(logits, (size_t)T * E * 4, o.p, o.bytes) || ranges_overlap(x, xb, o.p, o.bytes) ||
-            ranges_overlap(x_scales, (size_t)T * 4, o.p, o.bytes))
+    for (int o = 0; o < 8; o++) {
+        const void* p = out[o].p;
+        const size_t bytes = out[o].bytes;
+        if (ranges_overlap(logits, (size_t)T * E * 4, p, bytes) || ranges_overlap(x, xb, p, bytes) ||
+            ranges_overlap(x_scales, (size_t)T * 4, p, bytes))
             return MOE_ERR_INVALID_ARG;
+        for (int q = 0; q < o; q++)
+            if (ranges_overlap(out[q].p, out[q].bytes, p, bytes)) return MOE_ERR_INVALID_ARG;
+    }
     if (W->device != moe_current_device()) return MOE_ERR_INVALID_ARG;
 
     I8Front fr = {};

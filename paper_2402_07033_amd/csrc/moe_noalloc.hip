@@ -59,6 +59,7 @@ int moe_expert_ffn_noalloc(const moe_weights_t* W, const void* xg, moe_dtype_t a
     else if (path == MOE_FFN_STREAM) need = moe_ffn_stream_workspace(N, W->E, W->d, W->f);
     else need = moe_ffn_grouped_workspace(N, W->E, W->d, W->f);
     if (need > MOE_NOALLOC_SCRATCH_BYTES) return MOE_ERR_WORKSPACE;  // beyond the static scratch
+    if (i8 && W->device != moe_current_device()) return MOE_ERR_INVALID_ARG;
     void* ptr = noalloc_scratch_ptr();
     if (!ptr) return MOE_ERR_HIP;
     hipStream_t s = (hipStream_t)stream;

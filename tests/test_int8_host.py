@@ -132,6 +132,39 @@ def test_other_calls_on_a_handle(L, at):  # noqa: F811
     assert L.moe_expert_ffn_workspace(1, 1, 1 << 18, 64, F32) > 0   # (no 8-bit handle has such rows)
 
 
+def test_outputs_over_one_another(L, at):  # noqa: F811
+    """(On a handle of a device that is not the current one: nothing is launched whatever the checks let through.)"""
+    W = _handle()
+    W.device = 1 << 20
+    need = L.moe_layer_int8_workspace(4, 8, 2, 256, 512)
+    outs = dict(idx=32, w=32, cnt=32, off=36, perm=32, inv=32, ws=need, y=4096)
+
+    def call(**change):
+        a = dict(zip(outs, at[2:]), **change)
+        return L.moe_layer_int8(C.byref(W), at[0], F32, None, at[1], 4, 2, a["idx"], a["w"], a["cnt"], a["off"], a["perm"], a["inv"],
+                                a["ws"], need, a["y"], F32, None)
+
+    for n, p in zip(outs, at[2:]):
+        for o, q in zip(outs, at[2:]):
+            if n != o and n != "ws":
+                assert call(**{n: _off(q, outs[o] // 16 * 16 - 16 if o != "cnt" else 0)}) == INVALID, (n, o)
+    assert call() == INVALID  # the device
+
+
+def test_handle_of_another_device(L, at):  # noqa: F811
+    W = _handle()
+    W.device = 1 << 20
+    p = at[:14]
+    big = C.c_size_t(1 << 30)
+    assert L.moe_expert_ffn(C.byref(W), p[0], F32, p[1], 4, p[2], big, p[3], None) == INVALID
+    assert L.moe_expert_ffn_path(C.byref(W), p[0], BF16, p[1], 4, p[2], big, p[3], 1, None) == INVALID
+    assert L.moe_expert_ffn_tokens(C.byref(W), p[0], F32, 2, 2, p[4], p[1], p[2], big, p[3], None) == INVALID
+    assert L.moe_expert_ffn_noalloc(C.byref(W), p[0], F32, p[1], 4, p[3], None) == INVALID
+    stage = C.c_int(-1)
+    assert L.moe_layer(C.byref(W), p[0], F32, 256, p[1], 2, 8, 2, 0, *p[2:8], p[8], p[9], big, p[10], p[11], C.byref(stage), None) == INVALID
+    assert stage.value == 2
+
+
 def test_block_norm_refuses(L, at):  # noqa: F811
     x, y, ga, g, rg, gb, xo, h, q, s = at[:10]
     ok = dict(x=x, xt=F32, y=y, yt=BF16, T=4, d=128, after=1, ga=ga, g=g, rg=rg, r=0.5, gb=gb, eps=1e-5, xo=xo, h=h, ht=BF16, q=q, s=s)

@@ -83,7 +83,7 @@ __device__ __forceinline__ void i8_gemm_tile(const I8GemmArgs& a, const I8Tile& 
     constexpr int NW = WT * WF, XF = WT * RB, WFR = WF * FB;
     constexpr int XL = (XF + NW - 1) / NW, WL = (WFR + NW - 1) / NW;  // requests of a wave and step
     constexpr int STAGE = (XF + WFR) * 1024, D = NS - 1;
-    static_assert(WFR % NW == 0 && (D - 1) * (XL + WL) < 64, "requests");
+    static_assert((D - 1) * (XL + WL) < 64, "requests");
     const I8Product& p = a.p;
     const int K = p.K;
     const int wt = wave / WF, wf = wave % WF;
@@ -104,7 +104,7 @@ __device__ __forceinline__ void i8_gemm_tile(const I8GemmArgs& a, const I8Tile& 
     }
 #pragma unroll
     for (int i = 0; i < WL; i++) {
-        int fr = fr0 + i * NW + wave;
+        int fr = fr0 + (i * NW + wave < WFR ? i * NW + wave : WFR - 1);  // (past the last: the last again)
         if (PACKED) {
             fr = fr < a.NR ? fr : a.NR - 1;
             wp[i] = p.w + ((size_t)ti.e * a.NR + fr) * a.KS * 1024 + lane * 16;
@@ -121,9 +121,10 @@ __device__ __forceinline__ void i8_gemm_tile(const I8GemmArgs& a, const I8Tile& 
         at = at < last ? at : last;
 #pragma unroll
         for (int i = 0; i < WL; i++) {
+            const int f = i * NW + wave < WFR ? i * NW + wave : WFR - 1;
             __builtin_amdgcn_global_load_lds(
                 (const __attribute__((address_space(1))) void*)(wp[i] + (PACKED ? (size_t)kc * 1024 : (size_t)at)),
-                (__attribute__((address_space(3))) void*)(smem + slot * STAGE + (i * NW + wave) * 1024), 16, 0, ONCE ? 2 : 0);
+                (__attribute__((address_space(3))) void*)(smem + slot * STAGE + f * 1024), 16, 0, ONCE ? 2 : 0);
         }
 #pragma unroll
         for (int i = 0; i < XL; i++) {
@@ -260,16 +261,21 @@ static int i8_gemm_go(I8GemmArgs& a, hipStream_t s) {
 // 128 where those do; else 32 x 128.  us with 32 x 128 / 128 x 128 / 256 x 256: first projection (d 4096, f 14336) of 8
 // experts of 24 rows 159 / 157 / 165, of 64 207 / 175 / 178, of 128 338 / 214 / 204, of 512 1190 / 658 / 518; the second of 24 rows 82 / 83 /
 // 104, of 128 185 / 116 / 151, of 512 649 / 317 / 239; one 4096 x 4096 matrix, 77 rows 15 / 22 / 31, 512 28 / 28 / 61, 1024 49 / 30 / 63,
-// 4096 193 / 96 / 79.
+// 4096 193 / 96 / 79.  256 x 224 where that takes less of whole rounds of 256 compute units (by more than the sixteenth that it costs in
+// shared operands): 3000 rows (K 4096, C 14336) 225 -> 213 us, 2048 159 -> 149, 4096 (K 2048, C 10000) 131 -> 121, 4096 (K 4096, C 14336)
+// 325 -> 312 to 330, by power.  Only for products: w1 and w3 come in pairs of fragment rows.
 struct I8Shape {
     int rows, channels;
 };
-static I8Shape i8_shape(int N, int E, int NR) {
+static I8Shape i8_shape(int N, int E, int NR, bool gated) {
     const int used = N < E ? N : E;
     auto fills = [&](int rows, int channels) {
         return ((long long)N / rows + used) * ((NR * 16 + channels - 1) / channels) >= 200;
     };
-    if (N > 128 * used && fills(256, 256)) return {256, 256};
+    if (N > 128 * used && fills(256, 256)) {
+        auto cost = [&](int channels) { return (i8_tiles(N, E, 256) * ((NR * 16 + channels - 1) / channels) + 255) / 256 * channels; };
+        return {256, !gated && cost(224) * 17 < cost(256) * 16 ? 224 : 256};
+    }
     return fills(128, 128) ? I8Shape{128, 128} : I8Shape{32, 128};
 }
 
@@ -278,16 +284,20 @@ bool moe_i8_product_supported(int N, int E, int K, int C, bool gated, int path) 
     if (K > I8_MAX_K) return false;
     const int NR = gated ? 2 * (C / 16) : (C + 15) / 16;
     if (path == MOE_FFN_STREAM) return i8_tiles(N, E, 16) * ((NR + 1) / 2) < ((size_t)1 << 32) / 512;
-    const I8Shape sh = i8_shape(N, E, NR);
+    const I8Shape sh = i8_shape(N, E, NR, gated);
     return (i8_tiles(N, E, sh.rows) * ((NR * 16 + sh.channels - 1) / sh.channels) + 8) < ((size_t)1 << 32) / 512;
 }
 
 // ONCE: matrices that most tiles read alone go past the caches (a plain read streams at 6.9 TB/s that way, at 6.0 otherwise).
 template <bool PACKED, bool GATED, bool ONCE>
 static int i8_gemm_pick(I8GemmArgs& a, hipStream_t s) {
-    const int rows = i8_shape(a.p.N, a.p.E, a.NR).rows;
+    const I8Shape sh = i8_shape(a.p.N, a.p.E, a.NR, GATED);
+    const int rows = sh.rows;
     if (rows == 32) return i8_gemm_go<1, 4, 2, 4, 2, PACKED, GATED, ONCE>(a, s);
     if (rows == 128) return i8_gemm_go<2, 2, 4, 4, 4, PACKED, GATED, ONCE>(a, s);
+    if constexpr (!GATED) {
+        if (sh.channels == 224) return i8_gemm_go<4, 2, 7, 3, 4, PACKED, false, false>(a, s);
+    }
     return i8_gemm_go<2, 4, 4, 3, 8, PACKED, GATED, false>(a, s);
 }
 
@@ -318,7 +328,7 @@ struct I8FfnSpace {
 };
 // Do both projections take the persistent loop?
 static bool i8_persistent(int N, int E, int d, int f) {
-    return i8_shape(N, E, f / 8).rows == 256 && i8_shape(N, E, d / 16).rows == 256 && moe_i8_grouped_supported(N, E, d, f);
+    return i8_shape(N, E, f / 8, true).rows == 256 && i8_shape(N, E, d / 16, false).rows == 256 && moe_i8_grouped_supported(N, E, d, f);
 }
 
 static I8FfnSpace i8_ffn_space(int N, int E, int d, int f) {
@@ -353,7 +363,7 @@ bool moe_i8_ffn_supported(int path, int N, int E, int d, int f) {
 int moe_i8_ffn_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan) {
     if (!moe_i8_ffn_supported(plan->path, N, E, d, f)) return MOE_ERR_UNSUPPORTED;
     if (plan->path == MOE_FFN_STREAM) return MOE_OK;
-    const I8Shape up = i8_shape(N, E, f / 8), down = i8_shape(N, E, d / 16);
+    const I8Shape up = i8_shape(N, E, f / 8, true), down = i8_shape(N, E, d / 16, false);
     const bool persistent = i8_persistent(N, E, d, f);
     plan->up_tile_rows = persistent ? moe_i8_grouped_tile_rows(N, E) : up.rows;
     plan->up_tile_features = up.channels;

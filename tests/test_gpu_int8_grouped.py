@@ -87,6 +87,31 @@ def test_layer(moe, T, k):
         moe.moe_layer_int8(W, x, logits, k, workspace=small)
 
 
+@pytest.mark.parametrize("M,K,C", [(2048, 128, 14336), (3000, 144, 14272), (2817, 4096, 10001)])
+def test_products_of_whole_rounds(moe, M, K, C):
+    """Tiles of 224 channels: the last rows and channels of a product are what a call on a few rows gives."""
+    g = torch.Generator("cuda").manual_seed(M)
+    x = torch.randint(-127, 128, (M, K), dtype=torch.int8, device="cuda", generator=g)
+    w = torch.randint(-127, 128, (1, C, K), dtype=torch.int8, device="cuda", generator=g)
+    s, t = torch.rand(M, device="cuda", generator=g) + 0.5, torch.rand((1, C), device="cuda", generator=g) + 0.5
+    y = moe.moe_int8_matmul((x, s), (w, t), dtype=F32)
+    for r in (0, 240, M // 64 * 32, (M - 1) // 32 * 32):
+        n = min(32, M - r)
+        assert torch.equal(y[r:r + n], moe.moe_int8_matmul((x[r:r + n], s[r:r + n]), (w, t), dtype=F32))
+
+
+def test_second_projection_of_whole_rounds(moe):
+    N, d, f = 2048, 14272, 64
+    assert moe.moe_expert_ffn_plan(N, 1, d, f, moe.MOE_INT8, moe.MOE_FFN_GROUPED)["down_tile_features"] == 224
+    W = _handle(moe, 1, d, f, 5)
+    x = torch.randn((N, d), device="cuda", generator=torch.Generator("cuda").manual_seed(6))
+    off = torch.tensor([0, N - 3], dtype=torch.int32, device="cuda")
+    got, want = (torch.full((N, d), 4.0, device="cuda") for _ in range(2))
+    moe.moe_expert_ffn(W, x, off, yg=got, path=moe.MOE_FFN_GROUPED)
+    moe.moe_expert_ffn(W, x, off, yg=want, path=moe.MOE_FFN_STREAM)
+    assert torch.equal(got, want) and (got[N - 3:] == 4.0).all()
+
+
 # ---- more rows than a launch takes, and offsets past 32 bits: the last rows are what a call on them alone gives ----
 
 def test_product_past_4_gib(moe):

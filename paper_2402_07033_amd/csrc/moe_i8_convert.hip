@@ -202,12 +202,13 @@ int moe_i8_rows_back_launch(const int8_t* codes, const float* scales, int T, int
 //
 // To codes: a workgroup takes the channels of 64 bytes of a row and all of K.  A thread takes V neighbouring channels of 16
 // consecutive indices at a time, all requested at once and, up to HOLD times, kept in registers between the largest
-// magnitudes and the codes: such matrices are read once.  Longer reductions are read again, from the last-level cache.  The
+// magnitudes and the codes: such matrices are read once.  The others are read again, from the last-level cache.  The
 // two halves of a 128-byte line go to workgroups of one XCD.  Codes leave as 16 bytes a channel, 128 bytes and more of a
 // channel side by side.
 // Threads and bytes of a row, 8 x 4096 x 14336 in bf16 / in fp32, us: 512 and 64 454 / 701, 512 and 32 475 / 807, 1024 and 64 534 / 660,
-// 1024 and 32 506 / 723 (floor 275 / 458).  Scales and codes in two launches, in groups that the last-level cache holds: 600.
-// What bounds it is the access to narrow strips of long rows: a launch that only reads them for the scales gets 3.5 TB/s.
+// 1024 and 32 506 / 723, 512 and 128 508 / 688 (floor 275 / 458).  Scales and codes in two launches: below, for long reductions; in groups of
+// experts that the last-level cache holds 530 to 630.  What bounds it is the access to narrow strips of long rows: a plain
+// read of strips of 64 / 128 / 256 bytes runs at 4.1 / 5.5 / 6.1 TB/s.
 #define I8_QT 512
 #define I8_SEG 64
 #define I8_SIDE (128 / I8_SEG)  // strips of a line, on one XCD
@@ -315,10 +316,129 @@ __global__ __launch_bounds__(I8_QT) void i8_quantize_kernel(const void* __restri
     }
 }
 
+// Long reductions in two launches.  The scales alone: a workgroup takes the channels of SEG bytes of a row and all of K.
+template <bool BF16, int V, int SEG>
+__global__ __launch_bounds__(I8_QT) void i8_scales_kernel(const void* __restrict__ w, int K, int C, float* __restrict__ scales) {
+    typedef I8Quant<BF16, V> Q;
+    constexpr int LC = SEG / Q::BYTES, RG = I8_QT / LC, HOLD = 2;
+    __shared__ unsigned s_top[RG][LC * V];
+    const size_t e = blockIdx.y;
+    const int cl = threadIdx.x % LC, rg = threadIdx.x / LC, groups = K / 16;
+    const int c0 = (blockIdx.x * LC + cl) * V, c = c0 < C ? c0 : C - V;  // (C is a multiple of V)
+    const size_t base = e * K * C + c;
+    unsigned top[V];
+#pragma unroll
+    for (int n = 0; n < V; n++) top[n] = 0u;
+    for (int g = rg; g < groups; g += HOLD * RG) {
+        typename Q::Elems v[HOLD][16];
+#pragma unroll
+        for (int h = 0; h < HOLD; h++)  // (past the end: the last again)
+            Q::load(w, base + (size_t)(g + h * RG < groups ? g + h * RG : groups - 1) * 16 * C, C, v[h]);
+#pragma unroll
+        for (int h = 0; h < HOLD; h++)
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+#pragma unroll
+                for (int n = 0; n < V; n++) {
+                    const unsigned o = __float_as_uint(v[h][i].at(n)) & 0x7FFFFFFFu;
+                    top[n] = top[n] > o ? top[n] : o;
+                }
+    }
+#pragma unroll
+    for (int n = 0; n < V; n++) s_top[rg][cl * V + n] = top[n];
+    __syncthreads();
+    const int ch = blockIdx.x * (LC * V) + threadIdx.x;
+    if (threadIdx.x >= LC * V || ch >= C) return;
+    unsigned t = 0u;
+    for (int i = 0; i < RG; i++) t = t > s_top[i][threadIdx.x] ? t : s_top[i][threadIdx.x];
+    scales[e * C + ch] = i8_scale(t);
+}
+
+// The codes by the scales: a tile of 64 channels by 256 indices through LDS.  Neighbouring workgroups take the tiles of the same
+// channels: those of the same indices would write lines a channel's row apart, 4096 bytes in K = 4096, which share
+// memory channels (8 x 4096 x 14336 in bf16: 385 us that way, 300 this way).
+#define I8_CODE_K 256
+#define I8_CODE_C 64
+template <bool BF16, int V>
+__global__ __launch_bounds__(512) void i8_codes_kernel(const void* __restrict__ w, const float* __restrict__ scales, int K, int C,
+                                                       int8_t* __restrict__ codes) {
+    constexpr int LC = I8_CODE_C / V, RG = 512 / LC;
+    __shared__ __align__(16) unsigned s_q[I8_CODE_C][I8_CODE_K / 4 + 1];
+    const size_t e = blockIdx.z;
+    const int c0 = (int)blockIdx.y * I8_CODE_C, k0 = (int)blockIdx.x * I8_CODE_K;
+    const int kn = K - k0 < I8_CODE_K ? K - k0 : I8_CODE_K;
+    const int cl = threadIdx.x % LC, rg = threadIdx.x / LC;
+    const int cc = c0 + cl * V, c = cc < C ? cc : C - V;  // (C is a multiple of V)
+    typedef std::conditional_t<BF16, uint16_t, float> T;
+    typedef T Vec __attribute__((ext_vector_type(V)));
+    constexpr int R = I8_CODE_K / 4 / RG;  // groups of four indices of a thread
+    Vec v[R][4];
+    const T* p = (const T*)w + (e * K + k0) * C + c;
+#pragma unroll
+    for (int r = 0; r < R; r++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int k = (rg + r * RG) * 4 + i;
+            v[r][i] = *(const Vec*)(p + (size_t)(k < kn ? k : kn - 1) * C);
+        }
+#pragma unroll
+    for (int n = 0; n < V; n++) {
+        const I8Coder code(scales[e * C + c + n]);
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            float f[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                if constexpr (BF16) f[i] = __uint_as_float((unsigned)v[r][i][n] << 16);
+                else f[i] = v[r][i][n];
+            }
+            s_q[cl * V + n][rg + r * RG] = code(make_float4(f[0], f[1], f[2], f[3]));
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < I8_CODE_C * (I8_CODE_K / 16) / 512; i++) {
+        const int at = threadIdx.x + i * 512, ch = at / (I8_CODE_K / 16), b = at % (I8_CODE_K / 16);
+        if (c0 + ch >= C || b * 16 >= kn) continue;
+        u32x4_t q;
+#pragma unroll
+        for (int j = 0; j < 4; j++) q[j] = s_q[ch][b * 4 + j];
+        *(u32x4_t*)(codes + (e * C + c0 + ch) * K + k0 + b * 16) = q;
+    }
+}
+
+template <bool BF16, int V, int SEG>
+static void i8_scales_go(const void* w, int E, int K, int C, float* scales, hipStream_t s) {
+    constexpr int wide = SEG / (BF16 ? 2 : 4);
+    hipLaunchKernelGGL((i8_scales_kernel<BF16, V, SEG>), dim3((unsigned)((C + wide - 1) / wide), (unsigned)E), dim3(I8_QT), 0, s, w, K, C, scales);
+}
+template <bool BF16, int V>
+static void i8_scales_pick(const void* w, int E, int K, int C, float* scales, hipStream_t s) {
+    // wide strips read at 5.2 TB/s, strips of 64 bytes at 4.0; but there have to be enough of them
+    if ((long long)E * C * (BF16 ? 2 : 4) >= 128 * 256) i8_scales_go<BF16, V, 256>(w, E, K, C, scales, s);
+    else i8_scales_go<BF16, V, 64>(w, E, K, C, scales, s);
+}
+template <bool BF16, int V>
+static void i8_codes_go(const void* w, const float* scales, int E, int K, int C, int8_t* codes, hipStream_t s) {
+    const dim3 grid((unsigned)((K + I8_CODE_K - 1) / I8_CODE_K), (unsigned)((C + I8_CODE_C - 1) / I8_CODE_C), (unsigned)E);
+    hipLaunchKernelGGL((i8_codes_kernel<BF16, V>), grid, dim3(512), 0, s, w, scales, K, C, codes);
+}
+
 int moe_i8_quantize_launch(const void* w, moe_dtype_t w_dtype, int E, int K, int C, int8_t* codes, float* scales,
                            hipStream_t s) {
     const bool bf16 = w_dtype == MOE_BF16;
     const int V = bf16 && C % 4 == 0 ? 4 : C % 2 == 0 ? 2 : 1;
+    // One launch keeps 1024 or 2048 indices of a channel in registers and reads the others twice, in narrow strips: one / two
+    // launches 8 x 4096 x 14336 in bf16 461 / 477 us, in fp32 715 / 761, 4 x 6144 x 4096 118 / 98 and 167 / 159, 4 x 14336 x 4096
+    // 333 / 258 and 470 / 398, 14336 x 1024 131 / 46, 4 x 4096 x 4095 102 / 99.
+    if (K > 4096) {
+        if (bf16) V == 4 ? i8_scales_pick<true, 4>(w, E, K, C, scales, s) : V == 2 ? i8_scales_pick<true, 2>(w, E, K, C, scales, s)
+                                                                                    : i8_scales_pick<true, 1>(w, E, K, C, scales, s);
+        else V == 2 ? i8_scales_pick<false, 2>(w, E, K, C, scales, s) : i8_scales_pick<false, 1>(w, E, K, C, scales, s);
+        if (bf16) C % 4 == 0 ? i8_codes_go<true, 4>(w, scales, E, K, C, codes, s) : i8_codes_go<true, 1>(w, scales, E, K, C, codes, s);
+        else C % 4 == 0 ? i8_codes_go<false, 4>(w, scales, E, K, C, codes, s) : i8_codes_go<false, 1>(w, scales, E, K, C, codes, s);
+        return moe_launch_status();
+    }
     const int wide = I8_SEG / (bf16 ? 2 : 4), strips = (C + wide - 1) / wide;
     auto* kernel = bf16 ? (V == 4 ? i8_quantize_kernel<true, 4> : V == 2 ? i8_quantize_kernel<true, 2> : i8_quantize_kernel<true, 1>)
                         : (V == 2 ? i8_quantize_kernel<false, 2> : i8_quantize_kernel<false, 1>);

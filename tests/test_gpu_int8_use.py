@@ -157,3 +157,22 @@ def test_norms_and_conversions_captured(moe, d):  # noqa: F811
             torch.cuda.synchronize()
             for a, b in zip(out, want):
                 assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("E,K,C", [(1, 4112, 1), (2, 4112, 66), (1, 5120, 8202), (3, 4352, 100), (2, 4112, 4098), (1, 14336, 63), (4, 4128, 4100)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_long_reductions_to_codes(moe, E, K, C, dtype):  # noqa: F811
+    """Matrices whose channels are too long for one workgroup's registers (scales and codes in a launch each), with
+    channels of zeros, of one large value and with a NaN or an infinity."""
+    rng = _rng(22, E, K, C)
+    w = _values(rng, (E, K, C), dtype, K ** -0.5)
+    w[0, :, 0] = 0.0
+    if C > 8:
+        w[0, K - 1, C - 1] = -1000.0
+        w[-1, 7, 3], w[-1, K - 2, 5] = np.nan, np.inf
+    bad = ~np.isfinite(w).all(axis=1)
+    q, s = ref.matrix(np.where(bad[:, None], 0, w).astype(np.float32))
+    codes, scales = (_host(t) for t in moe.moe_int8_quantize(_dev(w, dtype)))
+    assert np.array_equal(np.isnan(scales), bad)
+    _same(scales[~bad], s[~bad])
+    _same(codes, q)  # (codes 0 where the scale is NaN)

@@ -491,17 +491,17 @@ int moe_i8_dequantize_launch(const int8_t* codes, const float* scales, int E, in
 
 // -------------------------------------------------------------------- handle ----
 // codes [E][C][K] -> fragments [E][C/16][nmat][K/64], this launch fills matrix slot `mat`, and the scales beside
-// them.  One thread writes one 16-byte chunk; the four chunks of 64 bytes of a feature go to lanes 16 apart.
+// them.  One thread writes one 16-byte chunk, a wave a fragment: sixteen features' 64 bytes.
 __global__ __launch_bounds__(256) void i8_pack_kernel(const int8_t* __restrict__ src, const float* __restrict__ scales,
                                                       u32x4_t* __restrict__ dst, float* __restrict__ dscale, int E, int K, int C,
                                                       int nmat, int mat) {
     const size_t KS = (size_t)i8_frags(K), total = (size_t)E * C * KS * 4;
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
-        const int j = (int)(i & 3);
-        const size_t ks = (i >> 2) % KS, c = (i >> 2) / KS;  // feature, counted through the experts
+        const int l = (int)(i & 63), j = l >> 4;
+        const size_t ks = (i >> 6) % KS, b = (i >> 6) / KS, c = b * 16 + (l & 15);  // feature, counted through the experts
         const u32x4_t v = *(const u32x4_t*)(src + c * K + ks * I8_FRAG_K + 16 * j);
-        dst[(((c / 16) * nmat + mat) * KS + ks) * 64 + 16 * j + (c & 15)] = v;
-        if (ks == 0 && j == 0) dscale[((c / 16) * nmat + mat) * 16 + (c & 15)] = scales[c];
+        dst[((b * nmat + mat) * KS + ks) * 64 + l] = v;
+        if (ks == 0 && j == 0) dscale[(b * nmat + mat) * 16 + l] = scales[c];
     }
 }
 

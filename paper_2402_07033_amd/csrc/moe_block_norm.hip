@@ -12,13 +12,20 @@
 
 #include "moe_i8.h"
 
+// ONCE: read past the caches (4096 rows of 4096, fp32 and bf16 to fp32 and bf16: 47.8 -> 43.5 us; h, which the next kernel reads, is
+// left in them: 43.1 otherwise).
+template <bool ONCE>
 __device__ __forceinline__ float4 bn_load4(const void* p, bool bf16, size_t chunk) {
     if (bf16) {
-        const uint2 u = ((const uint2*)p)[chunk];
+        typedef unsigned Pair __attribute__((ext_vector_type(2)));
+        const Pair* q = (const Pair*)p + chunk;
+        const Pair u = ONCE ? __builtin_nontemporal_load(q) : *q;
         return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
                            __uint_as_float(u.y & 0xFFFF0000u));
     }
-    return ((const float4*)p)[chunk];
+    const f32x4_t* q = (const f32x4_t*)p + chunk;
+    const f32x4_t v = ONCE ? __builtin_nontemporal_load(q) : *q;
+    return make_float4(v[0], v[1], v[2], v[3]);
 }
 __device__ __forceinline__ void bn_store4(void* p, bool bf16, size_t chunk, const double (&v)[4]) {
     if (bf16) {
@@ -100,9 +107,9 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(MoeBlockNorm a) {
             for (int c = threadIdx.x; c < d4; c += n) f(0, c);
         }
     };
-    auto load_y = [&](int c) __attribute__((always_inline)) { return a.y ? bn_load4(a.y, a.y_bf16, base + c) : zero; };
+    auto load_y = [&](int c) __attribute__((always_inline)) { return a.y ? bn_load4<HELD>(a.y, a.y_bf16, base + c) : zero; };
     if (HELD) {
-        each([&](int i, int c) __attribute__((always_inline)) { hx[i] = bn_load4(a.x, a.x_bf16, base + c); });
+        each([&](int i, int c) __attribute__((always_inline)) { hx[i] = bn_load4<HELD>(a.x, a.x_bf16, base + c); });
         each([&](int i, int c) __attribute__((always_inline)) { hy[i] = load_y(c); });
     }
     double r_after = 1.0;
@@ -116,7 +123,7 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(MoeBlockNorm a) {
     }
     const double scale_y = a.y ? (double)a.residual_scale * (a.row_gate ? (double)a.row_gate[t] : 1.0) * r_after : 0.0;
     auto stream = [&](int i, int c, double (&v)[4]) __attribute__((always_inline)) {
-        const float4 x = HELD ? hx[i] : bn_load4(a.x, a.x_bf16, base + c), y = HELD ? hy[i] : load_y(c);
+        const float4 x = HELD ? hx[i] : bn_load4<HELD>(a.x, a.x_bf16, base + c), y = HELD ? hy[i] : load_y(c);
         const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
         double g[4], q[4];
         gain_after.get(c, g);
@@ -193,7 +200,7 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(MoeBlockNorm a) {
 #define BN_LAUNCH_ROWS (1 << 20)
 
 // Two chunks a thread: a row's requests are all out at once and its passes short.  4096 rows of 4096 (fp32, bf16 -> fp32,
-// bf16) with 1 / 2 / 4 / 8 chunks a thread (1024 .. 128 threads) 67.7 / 50.7 / 54.7 / 57.5 us, 1000 rows (8-bit codes too) 21.8 /
+// bf16; cached reads) with 1 / 2 / 4 / 8 chunks a thread (1024 .. 128 threads) 67.7 / 50.7 / 54.7 / 57.5 us, 1000 rows (8-bit codes too) 21.8 /
 // 16.4 / 15.2 / 16.8, 301 of 2048 6.7 / 6.0 / 7.9 / 10.8, one 5.6 / 4.8 / 5.1 / 6.9; 2000 of 8192 - / 58.4 / 55.7 / 52.8.
 int moe_block_norm_launch(const MoeBlockNorm& a, hipStream_t s) {
     const int d4 = a.d / 4, V = d4 <= 2048 ? 2 : 4;

@@ -278,7 +278,7 @@ int moe_int8_dequantize(const int8_t* codes, const float* scales, int E, int K, 
     return rc != MOE_OK ? rc : moe_i8_dequantize_launch(codes, scales, E, K, C, w, w_dtype, (hipStream_t)stream);
 }
 
-static bool int8_rows_ok(int T, int K) { return T >= 0 && int8_k_ok(K); }
+static bool int8_rows_ok(int T, int K) { return T >= 0 && int8_k_ok(K) && (long long)T * K < 1LL << 40; }
 
 int moe_int8_quantize_rows(const void* x, moe_dtype_t x_dtype, int T, int K, int8_t* codes, float* scales, void* stream) {
     if (!int8_rows_ok(T, K) || !float_dtype(x_dtype)) return MOE_ERR_INVALID_ARG;

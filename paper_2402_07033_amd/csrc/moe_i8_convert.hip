@@ -5,6 +5,7 @@
 
 #include "moe_gate_wave.h"
 #include "moe_i8.h"
+#include "moe_rows.h"
 
 // ---------------------------------------------------------------------- rows ----
 // A workgroup takes a row: V chunks of four values a thread, kept in registers between the largest
@@ -78,10 +79,10 @@ template <bool BF16, int V>
 __global__ __launch_bounds__(1024) void i8_rows_kernel(const void* __restrict__ x, int T, int K4, unsigned* __restrict__ codes,
                                                        float* __restrict__ scales) {
     __shared__ unsigned s_top[16];
-    for (int t = blockIdx.x; t < T; t += gridDim.x) {
+    each_row(blockIdx.x, gridDim.x, T, [&](int t) __attribute__((always_inline)) {
         i8_row<BF16, V>(x, t, K4, codes, scales, s_top);
         __syncthreads();
-    }
+    });
 }
 
 // Four chunks of a row a thread: rows of 4096 in bf16, 4096 / 1024 of them, with 1 / 2 / 4 / 8 chunks 33.6 / 18.1 / 16.0 / 18.7 us and
@@ -173,7 +174,7 @@ int moe_i8_front_launch(const I8Front& f, moe_dtype_t x_dtype, hipStream_t s) {
 template <bool BF16>
 __global__ __launch_bounds__(256) void i8_rows_back_kernel(const unsigned* __restrict__ codes, const float* __restrict__ scales,
                                                            int T, int K4, void* __restrict__ x) {
-    for (int t = blockIdx.y; t < T; t += gridDim.y) {
+    each_row(blockIdx.y, gridDim.y, T, [&](int t) __attribute__((always_inline)) {
         const float s = scales[t];
         for (int c = blockIdx.x * 256 + threadIdx.x; c < K4; c += gridDim.x * 256) {
             const size_t at = (size_t)t * K4 + c;
@@ -187,7 +188,7 @@ __global__ __launch_bounds__(256) void i8_rows_back_kernel(const unsigned* __res
                 ((float4*)x)[at] = v;
             }
         }
-    }
+    });
 }
 
 int moe_i8_rows_back_launch(const int8_t* codes, const float* scales, int T, int K, void* x, moe_dtype_t x_dtype,

@@ -390,7 +390,7 @@ size_t moe_layer_int8_workspace(int T, int E, int k, int d, int f);
  * computed in 64 bits, every output rounded from there, bf16 ones by way of fp32 (h from the x' before its rounding).
  *   x [T,d] of x_dtype, y [T,d] of y_dtype (fp32 or bf16), y or NULL (then norm_after 0 and no gain_after, gates or x_out
  *   needed); gain_after [d], gain_before [d], gate [d], row_gate [T]: fp32, each or NULL for ones
- *   x_out [T,d] of x_dtype out or NULL; may be x itself
+ *   x_out [T,d] of x_dtype out or NULL; may be x itself (then no other input may lie there)
  *   h [T,d] of h_dtype (fp32 or bf16) out or NULL
  *   h_codes [T,d] int8, h_scales [T] fp32 out, both or neither: h in 8 bits (see moe_int8_quantize_rows)
  *   eps > 0; d a multiple of 64 up to 2^20 (2^17 with h_codes).  At least one output; no other overlap between arguments.

@@ -422,8 +422,8 @@ int moe_block_norm(const void* x, moe_dtype_t x_dtype, const void* y, moe_dtype_
     for (int o = 0; o < 4; o++) {
         if (!out[o].p) continue;
         if (!moe_aligned16(out[o].p)) return MOE_ERR_INVALID_ARG;
-        for (const auto& i : in)  // (x_out may be x: a thread reads what it writes before it writes it)
-            if (!(o == 0 && x_out == x && i.p == x) && ranges_overlap(i.p, i.bytes, out[o].p, out[o].bytes))
+        for (const auto& i : in)  // (x_out may be x: a thread reads what it writes before it writes it; no other input has that order)
+            if (!(o == 0 && x_out == x && &i == in) && ranges_overlap(i.p, i.bytes, out[o].p, out[o].bytes))
                 return MOE_ERR_INVALID_ARG;
         for (int q = 0; q < o; q++)
             if (ranges_overlap(out[q].p, out[q].bytes, out[o].p, out[o].bytes)) return MOE_ERR_INVALID_ARG;

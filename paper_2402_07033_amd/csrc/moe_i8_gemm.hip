@@ -363,11 +363,13 @@ bool moe_i8_ffn_supported(int path, int N, int E, int d, int f) {
 int moe_i8_ffn_plan(int N, int E, int d, int f, moe_ffn_plan_t* plan) {
     if (!moe_i8_ffn_supported(plan->path, N, E, d, f)) return MOE_ERR_UNSUPPORTED;
     if (plan->path == MOE_FFN_STREAM) return MOE_OK;
-    const I8Shape up = i8_shape(N, E, f / 8, true), down = i8_shape(N, E, d / 16, false);
+    // (the persistent loop's tiles: 256 features in both projections, whatever whole rounds i8_shape would make)
+    const I8Shape loop = {moe_i8_grouped_tile_rows(N, E), 256};
     const bool persistent = i8_persistent(N, E, d, f);
-    plan->up_tile_rows = persistent ? moe_i8_grouped_tile_rows(N, E) : up.rows;
+    const I8Shape up = persistent ? loop : i8_shape(N, E, f / 8, true), down = persistent ? loop : i8_shape(N, E, d / 16, false);
+    plan->up_tile_rows = up.rows;
     plan->up_tile_features = up.channels;
-    plan->down_tile_rows = persistent ? plan->up_tile_rows : down.rows;
+    plan->down_tile_rows = down.rows;
     plan->down_tile_features = down.channels;
     return MOE_OK;
 }

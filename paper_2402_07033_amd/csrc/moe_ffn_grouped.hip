@@ -408,11 +408,6 @@ __device__ __forceinline__ unsigned gg_h_off(int lane) {
 }
 
 #ifdef GG_INT8
-// Does the tile have fragment row j of this wave?
-template <int FRW, bool FLEX>
-__device__ __forceinline__ bool gg_int8_has(const TileInfo& ti, int wave, int j) {
-    return !FLEX || wave + (j / 4) * 4 < ti.groups;
-}
 // h of fragment rows (w1, w3) at fr and fr + 1, or y of one: four channels of a row, and the bits of their largest magnitude.
 __device__ __forceinline__ f32x4_t gg_int8_h(const i32x4_t& a, const i32x4_t& b, float sx, const f32x4_t& sa, const f32x4_t& sb,
                                              unsigned& top) {
@@ -433,18 +428,17 @@ __device__ __forceinline__ unsigned gg_int8_top(unsigned v) {
     return b[0] > b[1] ? b[0] : b[1];
 }
 // A whole tile's results; returns the number of stores.
-template <bool UP, int B, int FRW, bool FLEX>
+template <bool UP, int B, int FRW>
 __device__ __forceinline__ int gg_int8_epilogue(const GroupedArgs& a, const TileInfo& cur, int wave, int lane,
                                                 gg_acc_t (&acc)[B][FRW]) {
     const int t = lane & 15, r0 = cur.blk0 * 16, rows = cur.si.rows - r0;
-    const int frow = cur.frow + gg_wave_row<FRW, FLEX>(wave, 0);
+    const int frow = cur.frow + FRW * wave;
     f32x4_t ws[FRW];
     float sx[B];
     const float* wsp = a.wscale + ((size_t)cur.si.e * a.FR + frow) * 16 + 4 * (lane >> 4);
     const float* bsp = a.bscale + (size_t)(cur.si.bbase + cur.blk0) * 16 + t;
 #pragma unroll
-    for (int j = 0; j < FRW; j++)
-        ws[j] = gg_int8_has<FRW, FLEX>(cur, wave, j) ? *(const f32x4_t*)(wsp + gg_wave_row<FRW, FLEX>(0, j) * 16) : f32x4_t{};
+    for (int j = 0; j < FRW; j++) ws[j] = *(const f32x4_t*)(wsp + j * 16);
 #pragma unroll
     for (int i = 0; i < B; i++) sx[i] = bsp[(i < cur.nblk ? i : 0) * 16];
     // first row and channel of the tile
@@ -456,18 +450,15 @@ __device__ __forceinline__ int gg_int8_epilogue(const GroupedArgs& a, const Tile
         if constexpr (UP) {
 #pragma unroll
             for (int jj = 0; jj < FRW / 4; jj++) {
-                const bool has = gg_int8_has<FRW, FLEX>(cur, wave, 4 * jj);
                 unsigned top = 0u;
 #pragma unroll
                 for (int q = 0; q < 2; q++) {
                     const int j = 4 * jj + 2 * q;
                     const f32x4_t h = gg_int8_h(acc[i][j], acc[i][j + 1], sx[i], ws[j], ws[j + 1], top);
-                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, h), rs, has ? row : GG_RSRC_BYTES,
-                                                           gg_wave_row<FRW, FLEX>(0, j) * 32, 0);
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, h), rs, row, j * 32, 0);
                 }
                 top = gg_int8_top(top);
-                if (lane < 16 && has && i * 16 + t < rows)
-                    a.top[(size_t)((frow + gg_wave_row<FRW, FLEX>(0, 4 * jj)) / 4) * a.N + cur.si.row0 + r0 + i * 16 + t] = top;
+                if (lane < 16 && i * 16 + t < rows) a.top[(size_t)(frow / 4 + jj) * a.N + cur.si.row0 + r0 + i * 16 + t] = top;
             }
         } else {
 #pragma unroll
@@ -475,9 +466,7 @@ __device__ __forceinline__ int gg_int8_epilogue(const GroupedArgs& a, const Tile
                 f32x4_t y;
 #pragma unroll
                 for (int q = 0; q < 4; q++) y[q] = i8_value(acc[i][j][q], sx[i], ws[j][q]);
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, y), rs,
-                                                       gg_int8_has<FRW, FLEX>(cur, wave, j) ? row : GG_RSRC_BYTES,
-                                                       gg_wave_row<FRW, FLEX>(0, j) * 64, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, y), rs, row, j * 64, 0);
             }
         }
     }
@@ -804,7 +793,8 @@ __device__ __forceinline__ void gg_gemm_body(const GroupedArgs& a, int NT, int t
             }
             stores = B * FRW;
         } else if constexpr (GG_I8) {
-            stores = gg_int8_epilogue<UP, B, FRW, FLEX>(a, cur, wave, lane_e, acc);
+            static_assert(!FLEX, "8 bits: whole tiles");
+            stores = gg_int8_epilogue<UP, B, FRW>(a, cur, wave, lane_e, acc);
         } else if (UP) {
             // fragment rows 4jj..4jj+3 of this wave: w1, w3 of an even and of the next column block
             const int ks_o = (cur.frow + gg_wave_row<FRW, FLEX>(wave, 0)) / 4;  // h fragment column of jj = 0
@@ -894,9 +884,11 @@ __global__ __launch_bounds__(GG_THREADS) void gg_gemm_kernel(GroupedArgs a) {
     __syncthreads();
     const int NT = SMALL && small ? small : a.NT, total = n_tok * NT;
     const bool turned = gg_turned(s_seg, threadIdx.x & 63, total, NT, a.KS);
-    if (SMALL && small) {  // whole tiles only
-        gg_gemm_body<UP, GG_SMALL_BLOCKS, 8, true, 1, GG_U, GG_WIDE_LA, GG_NS>(a, NT, total, 0, turned, s_seg);
-        return;
+    if constexpr (SMALL) {
+        if (small) {  // whole tiles only
+            gg_gemm_body<UP, GG_SMALL_BLOCKS, 8, true, 1, GG_U, GG_WIDE_LA, GG_NS>(a, NT, total, 0, turned, s_seg);
+            return;
+        }
     }
     gg_gemm_body<UP, NBW, FRW, false, UP ? 1 : 0, U, LA, NS>(a, NT, total, a.split, turned, s_seg);
     if (UP) {
@@ -984,7 +976,7 @@ __global__ __launch_bounds__(256) void gg_fixup_kernel(GroupedArgs a, int wgs, i
             tb.blk0 = blk;
             tb.nblk = 1;
             tb.frow = ti.nt * FROWS;
-            gg_int8_epilogue<UP, 1, FRW, false>(a, tb, wave, lane, one);
+            gg_int8_epilogue<UP, 1, FRW>(a, tb, wave, lane, one);
         } else if (UP) {
             const int ks_o = ti.nt * (FROWS / 4) + (FRW / 4) * wave;
             unsigned char* dst = (unsigned char*)a.out + ((size_t)(ti.si.bbase + blk) * a.KS_out + ks_o) * 1024 +

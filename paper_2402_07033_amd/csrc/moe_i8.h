@@ -145,8 +145,8 @@ struct I8Combine {
     void* y;
     bool y_bf16;
 };
-// The second projection of a few rows, h in fp32 with the largest magnitudes that the first one leaves (ytop); yg or, with c,
-// the layer's y, or both.
+// The second projection of a few rows, h in fp32 with the largest magnitudes that the first one leaves (ytop): yg, or, with c,
+// the layer's y.
 bool moe_i8_down_small_serves(int N, int K);
 int moe_i8_down_small_launch(const moe_weights* W, const float* h, const unsigned* htop, const int32_t* offsets, int N, float* yg,
                              const I8Combine* c, hipStream_t s);

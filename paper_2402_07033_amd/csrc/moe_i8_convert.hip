@@ -85,8 +85,9 @@ __global__ __launch_bounds__(1024) void i8_rows_kernel(const void* __restrict__ 
     });
 }
 
-// Four chunks of a row a thread: rows of 4096 in bf16, 4096 / 1024 of them, with 1 / 2 / 4 / 8 chunks 33.6 / 18.1 / 16.0 / 18.7 us and
-// 9.7 / 6.8 / 7.2 / 9.9; a wave per row with 16 chunks 22.5 and 16.0.
+// Four chunks of a row a thread: rows of 4096 in bf16 that the last-level cache holds, 4096 / 1024 of them, with 1 / 2 / 4 / 8 chunks
+// 33.6 / 18.1 / 16.0 / 18.7 us and 9.7 / 6.8 / 7.2 / 9.9; a wave per row with 16 chunks 22.5 and 16.0.  From memory, with the four that are kept,
+// 18.2 .. 21.3 and 8.3 (their bytes: 9.9 and 2.5).
 static int i8_row_threads(int K4) {
     int threads = 64;
     while (threads < 1024 && threads * 4 < K4) threads *= 2;
